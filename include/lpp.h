@@ -339,6 +339,100 @@ int lpp_snapshot_plan_destroy(lpp_snap_plan* plan);
 int lpp_kernel_snapshot_noalloc(const lpp_snap_conv* convs, int n_convs, long d, int dtype, long wbuf_elems,
                                 const float* x, float* v, void* wbuf, void* stream);
 
+/*
+ * 8-bit activation checkpoints.  A matrix of `rows` rows of `cols` values
+ * (float32 or bf16, rows ld >= cols elements apart: activations are rows of
+ * channels, one row a pixel) is kept in 8 bits between the forward and the
+ * backward pass.  Groups of 32 successive columns of a row (the last one may
+ * be shorter) share a power-of-two step: with amax the group's largest
+ * magnitude and s the biased exponent of the smallest power of two for which
+ * rint(amax * 2^(133-s)) <= 127, within [7, 254],
+ *     code = rint(x * 2^(133-s)) (ties to even),  value = code * 2^(s-133).
+ * A value is off by at most half a step; a step is between amax/127 and
+ * amax/63.5.  Values are exact in float32 and bf16.  With keep_sign a nonzero
+ * x never takes code 0 (it takes +-1, up to a whole step off), so that ReLU
+ * decisions x > 0 read off the checkpoint are those of x.  A group that holds
+ * an infinity or NaN has s = 255 and all its values are NaN.
+ * Buffer (lpp_act8_bytes(rows, cols) bytes of device memory, 16-byte aligned):
+ * int8 codes [rows][pitch], pitch = cols rounded up to 16, the padding codes
+ * 0, then the bytes s [rows][(cols + 31) / 32].  lpp_act8_bytes returns -1
+ * for rows < 0, cols < 1 or a matrix of 2^40 elements and more.
+ *   lpp_kernel_act8_pack: x into q.
+ *   lpp_kernel_act8_unpack: q's values into x (other elements of x, between
+ *     its rows, are left as they are).
+ *   lpp_kernel_act8_wgrad: the weight gradient of a 1x1 convolution or linear
+ *     layer whose input X [rows][cin] is held in q: dw[o][i] = sum over rows
+ *     of dy[row][o] * X[row][i], dw float32 [cout][cin], written.  Products
+ *     are exact and sums float32, in a fixed order, for both types of dy.  ws:
+ *     ws_floats >= lpp_act8_wgrad_ws(rows, cout, cin) floats of device memory
+ *     (16-byte aligned, may be NULL where that is 0), scratch of this call
+ *     until it has run: calls that may overlap need their own.
+ * All pointers are device pointers on the current device; stream may be NULL
+ * (default stream).  The calls enqueue and return, allocate nothing and may be
+ * captured into a graph.  rows == 0 is valid (dw becomes 0).  LPP_EINVAL before
+ * anything is launched for null, unaligned or too small buffers and bad sizes.
+ */
+long lpp_act8_bytes(long rows, int cols);
+int lpp_kernel_act8_pack(const void* x, int dtype, long rows, int cols, long ld, int keep_sign, void* q, void* stream);
+int lpp_kernel_act8_unpack(const void* q, long rows, int cols, void* x, int dtype, long ld, void* stream);
+long lpp_act8_wgrad_ws(long rows, int cout, int cin);
+int lpp_kernel_act8_wgrad(const void* dy, int dtype, long rows, int cout, long ld, const void* q, int cin, float* dw,
+                          float* ws, long ws_floats, void* stream);
+
+/*
+ * Root-mean-square norm over the columns (channels) of each row, after a
+ * residual addition if res is given:
+ *     h = x (+ res, rounded to the storage type),
+ *     rstd = 1 / sqrt(mean over columns of h^2 + eps),  y = h * rstd * gamma.
+ * h (wanted or NULL; only with res), y (wanted or NULL) and q (y's 8-bit
+ * checkpoint, from the unrounded y; wanted or NULL, keep_sign as above) are
+ * written, y or q at least; rstd: float32 [rows] or NULL.  h may be x or res.
+ * The gradient, with g = dy * gamma:
+ *     dx = rstd * (g - h * rstd^2 * mean over columns of (g * h)) (+ dres),
+ *     dgamma = sum over rows of dy * h * rstd,
+ * from h or, with h NULL, from h's 8-bit checkpoint q.  dx (storage type; it
+ * may be dy or dres) or dgamma (float32 [cols], written) may be NULL.  ws: as
+ * above, lpp_rmsnorm_bwd_ws(rows, cols) floats, needed for dgamma.
+ * Statistics and sums are float32, in a fixed order.  dtype: enum lpp_dtype of
+ * every matrix; gamma float32 [cols]; at most 16384 columns
+ * (LPP_EUNSUPPORTED).  Streams, capture and errors as above.
+ */
+typedef struct {
+    const void* x;
+    const void* res;
+    void* h;
+    void* y;
+    void* q;
+    long ldx, ldres, ldh, ldy;   /* elements between rows, where the matrix is given */
+    const float* gamma;
+    float* rstd;
+    long rows;
+    int cols;
+    int dtype;
+    float eps;
+    int keep_sign;
+} lpp_rmsnorm_args;
+int lpp_kernel_rmsnorm(const lpp_rmsnorm_args* args, void* stream);
+
+typedef struct {
+    const void* dy;
+    const void* h;
+    const void* q;
+    const void* dres;
+    void* dx;
+    long lddy, ldh, lddres, lddx;
+    const float* gamma;
+    const float* rstd;
+    float* dgamma;
+    float* ws;
+    long ws_floats;
+    long rows;
+    int cols;
+    int dtype;
+} lpp_rmsnorm_bwd_args;
+long lpp_rmsnorm_bwd_ws(long rows, int cols);
+int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

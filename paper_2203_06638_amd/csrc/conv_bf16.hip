@@ -44,6 +44,7 @@
 #include "bnacc.h"
 #include "kernels.h"
 #include "launch.h"
+#include "ldstile.h"
 
 namespace lpp {
 
@@ -784,13 +785,8 @@ __global__ __launch_bounds__(256) void wgrad_bf16_k(const bf16* __restrict__ dY,
 // so that the 8 rows a half-wave's reads touch (p0 .. p0 + 3 and p0 + 8 ..
 // p0 + 11) hit all 64 banks once: with 16 chunks a row the pair index is
 // XORed with row bits 0, 1 and 3; with 8 (128-byte rows, two rows a bank
-// cycle) with bits 1 and 3.  The operand loads run through the same NS-buffer
+// cycle) with bits 1 and 3 (wg_chunk, ldstile.h).  The operand loads run through the same NS-buffer
 // pipeline as the forward kernel's.
-template <int W>   // chunks (8 channels) per pixel row
-__device__ __forceinline__ int wg_chunk(int c, int row) {
-    const int f = W >= 16 ? ((row & 3) | (((row >> 3) & 1) << 2)) : (((row >> 1) & 1) | (((row >> 3) & 1) << 1));
-    return (((c >> 1) ^ f) << 1) | (c & 1);
-}
 
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef short s8v __attribute__((ext_vector_type(8)));

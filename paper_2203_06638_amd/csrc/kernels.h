@@ -392,4 +392,68 @@ constexpr int kMaxReplicas = 16;
 struct RepPtrs { float* p[kMaxReplicas]; };
 hipError_t launch_average(const RepPtrs& reps, int n_rep, long n, hipStream_t st);
 
+// ---- 8-bit activation checkpoints (act8.h: format and buffer layout) ----
+// x: `rows` rows of C values, ld elements apart, of type dt; q: act8_bytes(rows, C)
+// bytes, 16-byte aligned.
+hipError_t launch_act8_pack(int dt, const void* x, long ld, long rows, int C, bool keep_sign, uint8_t* q,
+                            hipStream_t st);
+hipError_t launch_act8_unpack(int dt, const uint8_t* q, long rows, int C, void* x, long ld, hipStream_t st);
+// dW[O][I] = dY^T X of a checkpoint X [rows][I]: partials [splits][part_floats] over
+// runs of rps rows (bo x bi: the tile of a workgroup); launch_act8_wgrad sums them into
+// dw (ws: splits * part_floats floats, unused with one split)
+struct Act8WgPlan {
+    int bo, bi, splits;
+    long rps, part_floats;
+};
+Act8WgPlan act8_wgrad_plan(long rows, int O, int I);
+hipError_t launch_act8_wgrad_part(int dt, const void* dY, long ld, const uint8_t* q, long rows, int O, int I,
+                                  float* part, const Act8WgPlan& p, hipStream_t st);
+hipError_t launch_act8_wgrad(int dt, const void* dY, long ld, const uint8_t* q, long rows, int O, int I, float* dw,
+                             float* ws, hipStream_t st);
+// out[i] = sum_s part[s * stride + i] for i < n, fixed order (stride a multiple of 4)
+hipError_t launch_part_sums(const float* part, long stride, int S, long n, float* out, hipStream_t st);
+
+// ---- RMS norm (rmsnorm.hip) ----
+// Tensors of type dt with their row distances in elements; null pointers: not there /
+// not wanted.  h is written only with res.  q: y's checkpoint.  The fields after the
+// blank line are set by the launcher.
+constexpr int kRmsMaxC = 16384;   // a row stays in the registers of 1024 threads
+struct RmsArgs {
+    const void *x, *res;
+    void *h, *y;
+    uint8_t* q;
+    long ldx, ldres, ldh, ldy;
+    const float* gamma;
+    float* rstd;
+    long rows;
+    int C;
+    float eps;
+    bool keep_sign;
+
+    uint8_t* exps;
+    int pitch, G;
+};
+hipError_t launch_rmsnorm(int dt, RmsArgs p, hipStream_t st);
+// h (type dt) or, where it is null, its checkpoint q.  dx, dx2 (same row distance): the
+// same gradient twice, the second added to what is there with acc2.  part:
+// rmsnorm_bwd_parts(rows, C) rows of C rounded up to 4 floats, for dgamma.
+struct RmsBwdArgs {
+    const void *dy, *h;
+    const uint8_t* q;
+    const void* dres;
+    void *dx, *dx2;
+    long lddy, ldh, lddres, lddx;
+    const float *gamma, *rstd;
+    float* part;
+    long rows;
+    int C;
+    bool acc2;
+
+    const uint8_t* exps;
+    int pitch, G;
+    long pstride;
+};
+int rmsnorm_bwd_parts(long rows, int C);
+hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, float* dgamma, hipStream_t st);
+
 }  // namespace lpp

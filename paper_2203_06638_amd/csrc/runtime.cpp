@@ -20,6 +20,7 @@
 #include <vector>
 
 #include "../../include/lpp.h"
+#include "act8.h"
 #include "kernels.h"
 #include "launch.h"
 
@@ -2127,6 +2128,155 @@ int lpp_kernel_average(float* const* replicas, int n_rep, long n, void* stream) 
     }
     hipError_t e = lpp::launch_average(rp, n_rep, n, (hipStream_t)stream);
     if (e != hipSuccess) return fail(LPP_EHIP, std::string("average: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------
+// Stand-alone operators on caller buffers: 8-bit checkpoints, RMS norm
+
+namespace {
+int elem_size(int dtype) { return dtype == LPP_BF16 ? 2 : 4; }
+// message for a [rows][cols] matrix that the kernels cannot take, or nullptr
+const char* bad_matrix(const void* p, int dtype, long rows, int cols, long ld) {
+    if (dtype != LPP_FP32 && dtype != LPP_BF16) return "unknown dtype";
+    if (rows < 0 || cols < 1) return "rows must be at least 0 and cols at least 1";
+    if (!p && rows > 0) return "null buffer";
+    if ((uintptr_t)p % elem_size(dtype)) return "buffers must be aligned to their elements";
+    if (ld < cols || ld > (1L << 40) / std::max(rows, 1L)) return "the row distance must be at least cols (and the matrix under 2^40 elements)";
+    return nullptr;
+}
+const char* bad_act8(const void* q, long rows, int cols) {
+    if (lpp_act8_bytes(rows, cols) < 0) return "rows must be at least 0, cols at least 1, and the matrix under 2^40 elements";
+    if (!q && rows > 0) return "null checkpoint buffer";
+    if ((uintptr_t)q & 15) return "checkpoint buffers must be 16-byte aligned";
+    return nullptr;
+}
+}  // namespace
+
+extern "C" {
+
+long lpp_act8_bytes(long rows, int cols) {
+    if (rows < 0 || cols < 1 || cols > (1 << 24) || rows > (1L << 40) / cols) return -1;
+    return lpp::act8_bytes(rows, cols);
+}
+
+int lpp_kernel_act8_pack(const void* x, int dtype, long rows, int cols, long ld, int keep_sign, void* q,
+                         void* stream) {
+    if (const char* e = bad_matrix(x, dtype, rows, cols, ld)) return fail(LPP_EINVAL, e);
+    if (const char* e = bad_act8(q, rows, cols)) return fail(LPP_EINVAL, e);
+    hipError_t e = lpp::launch_act8_pack(dtype, x, ld, rows, cols, keep_sign != 0, (uint8_t*)q, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("act8_pack: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+int lpp_kernel_act8_unpack(const void* q, long rows, int cols, void* x, int dtype, long ld, void* stream) {
+    if (const char* e = bad_matrix(x, dtype, rows, cols, ld)) return fail(LPP_EINVAL, e);
+    if (const char* e = bad_act8(q, rows, cols)) return fail(LPP_EINVAL, e);
+    hipError_t e = lpp::launch_act8_unpack(dtype, (const uint8_t*)q, rows, cols, x, ld, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("act8_unpack: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+long lpp_act8_wgrad_ws(long rows, int cout, int cin) {
+    if (lpp_act8_bytes(rows, cin) < 0 || lpp_act8_bytes(rows, cout) < 0 || (long)cout * cin > (1L << 31)) return -1;
+    const lpp::Act8WgPlan p = lpp::act8_wgrad_plan(rows, cout, cin);
+    return p.splits > 1 ? p.splits * p.part_floats : 0;
+}
+
+int lpp_kernel_act8_wgrad(const void* dy, int dtype, long rows, int cout, long ld, const void* q, int cin, float* dw,
+                          float* ws, long ws_floats, void* stream) {
+    if (const char* e = bad_matrix(dy, dtype, rows, cout, ld)) return fail(LPP_EINVAL, e);
+    if (const char* e = bad_act8(q, rows, cin)) return fail(LPP_EINVAL, e);
+    const long need = lpp_act8_wgrad_ws(rows, cout, cin);
+    if (need < 0) return fail(LPP_EINVAL, "the gradient must be under 2^31 elements");
+    if (!dw || (uintptr_t)dw % 4) return fail(LPP_EINVAL, "dw must be a buffer of floats");
+    if (need > 0 && (!ws || ((uintptr_t)ws & 15) || ws_floats < need))
+        return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_act8_wgrad_ws floats");
+    hipError_t e = lpp::launch_act8_wgrad(dtype, dy, ld, (const uint8_t*)q, rows, cout, cin, dw, ws,
+                                          (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("act8_wgrad: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+int lpp_kernel_rmsnorm(const lpp_rmsnorm_args* a, void* stream) {
+    if (!a) return fail(LPP_EINVAL, "args is NULL");
+    if (a->cols > lpp::kRmsMaxC) return fail(LPP_EUNSUPPORTED, "RMS norm takes at most 16384 columns");
+    if (!(a->eps >= 0.f) || !std::isfinite(a->eps)) return fail(LPP_EINVAL, "eps must be >= 0 and finite");
+    if (!a->y && !a->q && a->rows > 0) return fail(LPP_EINVAL, "neither y nor q is wanted");
+    if (a->h && !a->res) return fail(LPP_EINVAL, "h is written only with a residual");
+    struct { const void* p; long ld; bool want; } m[] = {
+        {a->x, a->ldx, true}, {a->res, a->ldres, a->res != nullptr}, {a->h, a->ldh, a->h != nullptr},
+        {a->y, a->ldy, a->y != nullptr}};
+    for (auto& t : m)
+        if (t.want)
+            if (const char* e = bad_matrix(t.p, a->dtype, a->rows, a->cols, t.ld)) return fail(LPP_EINVAL, e);
+    if (a->q)
+        if (const char* e = bad_act8(a->q, a->rows, a->cols)) return fail(LPP_EINVAL, e);
+    if (!a->gamma || (uintptr_t)a->gamma % 4 || (uintptr_t)a->rstd % 4)
+        return fail(LPP_EINVAL, "gamma and rstd must be buffers of floats");
+    lpp::RmsArgs p{};
+    p.x = a->x;
+    p.res = a->res;
+    p.h = a->h;
+    p.y = a->y;
+    p.q = (uint8_t*)a->q;
+    p.ldx = a->ldx;
+    p.ldres = a->ldres;
+    p.ldh = a->ldh;
+    p.ldy = a->ldy;
+    p.gamma = a->gamma;
+    p.rstd = a->rstd;
+    p.rows = a->rows;
+    p.C = a->cols;
+    p.eps = a->eps;
+    p.keep_sign = a->keep_sign != 0;
+    hipError_t e = lpp::launch_rmsnorm(a->dtype, p, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("rmsnorm: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+long lpp_rmsnorm_bwd_ws(long rows, int cols) {
+    if (lpp_act8_bytes(rows, cols) < 0) return -1;
+    return (long)lpp::rmsnorm_bwd_parts(rows, cols) * ((cols + 3) / 4 * 4);
+}
+
+int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* a, void* stream) {
+    if (!a) return fail(LPP_EINVAL, "args is NULL");
+    if (a->cols > lpp::kRmsMaxC) return fail(LPP_EUNSUPPORTED, "RMS norm takes at most 16384 columns");
+    if (!a->dx && !a->dgamma && a->rows > 0) return fail(LPP_EINVAL, "neither dx nor dgamma is wanted");
+    if ((a->h != nullptr) == (a->q != nullptr) && a->rows > 0) return fail(LPP_EINVAL, "give h or its checkpoint q");
+    struct { const void* p; long ld; bool want; } m[] = {
+        {a->dy, a->lddy, true}, {a->h, a->ldh, a->h != nullptr}, {a->dres, a->lddres, a->dres != nullptr},
+        {a->dx, a->lddx, a->dx != nullptr}};
+    for (auto& t : m)
+        if (t.want)
+            if (const char* e = bad_matrix(t.p, a->dtype, a->rows, a->cols, t.ld)) return fail(LPP_EINVAL, e);
+    if (a->q)
+        if (const char* e = bad_act8(a->q, a->rows, a->cols)) return fail(LPP_EINVAL, e);
+    if (!a->gamma || (uintptr_t)a->gamma % 4 || (!a->rstd && a->rows > 0) || (uintptr_t)a->rstd % 4 ||
+        (uintptr_t)a->dgamma % 4)
+        return fail(LPP_EINVAL, "gamma, rstd and dgamma must be buffers of floats");
+    if (a->dgamma && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < lpp_rmsnorm_bwd_ws(a->rows, a->cols)))
+        return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_rmsnorm_bwd_ws floats");
+    lpp::RmsBwdArgs p{};
+    p.dy = a->dy;
+    p.h = a->h;
+    p.q = (const uint8_t*)a->q;
+    p.dres = a->dres;
+    p.dx = a->dx;
+    p.lddy = a->lddy;
+    p.ldh = a->ldh;
+    p.lddres = a->lddres;
+    p.lddx = a->lddx;
+    p.gamma = a->gamma;
+    p.rstd = a->rstd;
+    p.part = a->ws;
+    p.rows = a->rows;
+    p.C = a->cols;
+    hipError_t e = lpp::launch_rmsnorm_bwd(a->dtype, p, a->dgamma, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("rmsnorm_bwd: ") + hipGetErrorString(e));
     return LPP_OK;
 }
 

@@ -64,6 +64,20 @@ class SnapConv(C.Structure):
                 ("kw", C.c_int), ("dst_f", C.c_long), ("dst_d", C.c_long)]
 
 
+class RmsNormArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("res", C.c_void_p), ("h", C.c_void_p), ("y", C.c_void_p), ("q", C.c_void_p),
+                ("ldx", C.c_long), ("ldres", C.c_long), ("ldh", C.c_long), ("ldy", C.c_long), ("gamma", C.c_void_p),
+                ("rstd", C.c_void_p), ("rows", C.c_long), ("cols", C.c_int), ("dtype", C.c_int), ("eps", C.c_float),
+                ("keep_sign", C.c_int)]
+
+
+class RmsNormBwdArgs(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("h", C.c_void_p), ("q", C.c_void_p), ("dres", C.c_void_p), ("dx", C.c_void_p),
+                ("lddy", C.c_long), ("ldh", C.c_long), ("lddres", C.c_long), ("lddx", C.c_long),
+                ("gamma", C.c_void_p), ("rstd", C.c_void_p), ("dgamma", C.c_void_p), ("ws", C.c_void_p),
+                ("ws_floats", C.c_long), ("rows", C.c_long), ("cols", C.c_int), ("dtype", C.c_int)]
+
+
 class ModelInfo(C.Structure):
     _fields_ = [("d", C.c_long), ("P", C.c_int), ("block_lo", C.c_long * 65), ("block_hi", C.c_long * 65),
                 ("fwd_flops", C.c_double), ("bwd_flops", C.c_double * 65)]
@@ -112,6 +126,17 @@ def lib():
             "lpp_snapshot_plan_destroy": ([C.c_void_p], C.c_int),
             "lpp_kernel_snapshot_noalloc": ([C.POINTER(SnapConv), C.c_int, C.c_long, C.c_int, C.c_long, C.c_void_p,
                                              C.c_void_p, C.c_void_p, C.c_void_p], C.c_int),
+            "lpp_act8_bytes": ([C.c_long, C.c_int], C.c_long),
+            "lpp_kernel_act8_pack": ([C.c_void_p, C.c_int, C.c_long, C.c_int, C.c_long, C.c_int, C.c_void_p,
+                                      C.c_void_p], C.c_int),
+            "lpp_kernel_act8_unpack": ([C.c_void_p, C.c_long, C.c_int, C.c_void_p, C.c_int, C.c_long, C.c_void_p],
+                                       C.c_int),
+            "lpp_act8_wgrad_ws": ([C.c_long, C.c_int, C.c_int], C.c_long),
+            "lpp_kernel_act8_wgrad": ([C.c_void_p, C.c_int, C.c_long, C.c_int, C.c_long, C.c_void_p, C.c_int,
+                                       C.c_void_p, C.c_void_p, C.c_long, C.c_void_p], C.c_int),
+            "lpp_kernel_rmsnorm": ([C.POINTER(RmsNormArgs), C.c_void_p], C.c_int),
+            "lpp_rmsnorm_bwd_ws": ([C.c_long, C.c_int], C.c_long),
+            "lpp_kernel_rmsnorm_bwd": ([C.POINTER(RmsNormBwdArgs), C.c_void_p], C.c_int),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -332,3 +357,160 @@ def kernel_snapshot_noalloc(convs, d, dtype, wbuf_elems, x, v, wbuf, stream=None
     arr = _snap_convs(convs)
     _check(lib().lpp_kernel_snapshot_noalloc(arr, len(convs), d, dtype, wbuf_elems, x.data_ptr(), v.data_ptr(),
                                              wbuf.data_ptr(), _stream_handle(stream)))
+
+
+# -- 8-bit activation checkpoints and RMS norm on device tensors (include/lpp.h) --
+# Matrices are 2-D float32 or bfloat16 tensors on the current device whose rows are
+# contiguous (any row distance); checkpoints are 1-D contiguous uint8 tensors of
+# act8_bytes(rows, cols) bytes; gamma, rstd, gradients of parameters and
+# workspaces are contiguous float32 tensors.  Buffers are checked and nothing
+# is allocated; tensors used on a stream other than the one they were
+# allocated on must outlive the call's work.
+
+_TORCH = None
+
+
+def _torch():
+    """(module, {dtype: lpp dtype}, float32, uint8), imported on first use."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = (torch, {torch.float32: FP32, torch.bfloat16: BF16}, torch.float32, torch.uint8)
+    return _TORCH
+
+
+def _need(ok, what):
+    if not ok:
+        raise LppError(EINVAL, what)
+
+
+def _current_device(t):
+    """The current device, where `t` is a tensor on one."""
+    torch = _torch()[0]
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, "expected a tensor on the current device")
+    return torch.cuda.current_device()
+
+
+def _matrix(t, what, dev, like=None):
+    """(pointer, row distance, dtype) of a 2-D tensor."""
+    dt = _torch()[1].get(t.dtype)
+    if dt is None or t.dim() != 2 or t.get_device() != dev:
+        raise LppError(EINVAL, what + " must be a 2-D float32 or bfloat16 tensor on the current device")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if cols > 1 and t.stride(1) != 1 or ld < cols or cols > 1 << 24:
+        raise LppError(EINVAL, what + " must have contiguous rows, of at most 2^24 columns, that do not overlap")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise LppError(EINVAL, what + " must have the other matrices' shape and type")
+    return t.data_ptr(), ld, dt
+
+
+def _floats(t, n, what, dev):
+    if t.dtype != _torch()[2] or not t.is_contiguous() or t.numel() < n or t.get_device() != dev:
+        raise LppError(EINVAL, "%s must be a contiguous float32 tensor of at least %d elements on the current device"
+                       % (what, n))
+    return t.data_ptr()
+
+
+def _act8(q, rows, cols, dev):
+    if q.dtype != _torch()[3] or not q.is_contiguous() or q.numel() != act8_bytes(rows, cols) or q.get_device() != dev:
+        raise LppError(EINVAL, "q must be a contiguous uint8 tensor of act8_bytes(rows, cols) elements on the current "
+                               "device")
+    return q.data_ptr()
+
+
+def act8_bytes(rows, cols):
+    """Bytes of the 8-bit checkpoint of a [rows][cols] matrix."""
+    n = lib().lpp_act8_bytes(rows, cols) if cols <= 1 << 24 else -1
+    _need(n >= 0, "rows must be at least 0, cols at least 1, and the matrix under 2^40 elements")
+    return n
+
+
+def kernel_act8_pack(x, q, keep_sign=False, stream=None):
+    """q = the 8-bit checkpoint of x (keep_sign: nonzero values stay nonzero)."""
+    dev = _current_device(x)
+    p, ld, dt = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    _check(lib().lpp_kernel_act8_pack(p, dt, rows, cols, ld, int(keep_sign), _act8(q, rows, cols, dev),
+                                      _stream_handle(stream)))
+
+
+def kernel_act8_unpack(q, x, stream=None):
+    """x = the values of checkpoint q."""
+    dev = _current_device(x)
+    p, ld, dt = _matrix(x, "x", dev)
+    rows, cols = x.shape
+    _check(lib().lpp_kernel_act8_unpack(_act8(q, rows, cols, dev), rows, cols, p, dt, ld, _stream_handle(stream)))
+
+
+def act8_wgrad_ws(rows, cout, cin):
+    """Floats of the workspace of kernel_act8_wgrad."""
+    n = lib().lpp_act8_wgrad_ws(rows, cout, cin) if max(cout, cin) <= 1 << 24 else -1
+    _need(n >= 0, "bad sizes")
+    return n
+
+
+def kernel_act8_wgrad(dy, q, dw, ws=None, stream=None):
+    """dw [cout][cin] = dy^T X, dy [rows][cout], q the checkpoint of X [rows][cin];
+    ws: act8_wgrad_ws(rows, cout, cin) floats (None where that is 0)."""
+    dev = _current_device(dy)
+    p, ld, dt = _matrix(dy, "dy", dev)
+    rows, cout = dy.shape
+    _need(dw.dim() == 2 and dw.shape[0] == cout, "dw must be [cout][cin]")
+    cin = dw.shape[1]
+    wp = _floats(ws, 0, "ws", dev) if ws is not None else None
+    _check(lib().lpp_kernel_act8_wgrad(p, dt, rows, cout, ld, _act8(q, rows, cin, dev), cin,
+                                       _floats(dw, cout * cin, "dw", dev), wp, ws.numel() if ws is not None else 0,
+                                       _stream_handle(stream)))
+
+
+def kernel_rmsnorm(x, gamma, rstd=None, eps=1e-5, res=None, h=None, y=None, q=None, keep_sign=False, stream=None):
+    """RMS norm of x (+ res) over the columns into y and / or its checkpoint q;
+    h: the sum x + res; rstd [rows]."""
+    dev = _current_device(x)
+    a = RmsNormArgs()
+    a.x, a.ldx, a.dtype = _matrix(x, "x", dev)
+    a.rows, a.cols = x.shape
+    if res is not None:
+        a.res, a.ldres, _ = _matrix(res, "res", dev, x)
+    if h is not None:
+        a.h, a.ldh, _ = _matrix(h, "h", dev, x)
+    if y is not None:
+        a.y, a.ldy, _ = _matrix(y, "y", dev, x)
+    if q is not None:
+        a.q = _act8(q, a.rows, a.cols, dev)
+    a.gamma = _floats(gamma, a.cols, "gamma", dev)
+    if rstd is not None:
+        a.rstd = _floats(rstd, a.rows, "rstd", dev)
+    a.eps, a.keep_sign = eps, int(keep_sign)
+    _check(lib().lpp_kernel_rmsnorm(C.byref(a), _stream_handle(stream)))
+
+
+def rmsnorm_bwd_ws(rows, cols):
+    """Floats of the workspace of kernel_rmsnorm_bwd."""
+    n = lib().lpp_rmsnorm_bwd_ws(rows, cols) if cols <= 1 << 24 else -1
+    _need(n >= 0, "bad sizes")
+    return n
+
+
+def kernel_rmsnorm_bwd(dy, gamma, rstd, dx=None, dgamma=None, ws=None, h=None, q=None, dres=None, stream=None):
+    """Gradient of kernel_rmsnorm from its h (x where there was no residual) or from
+    h's checkpoint q: dx (+ dres) and dgamma (with ws: rmsnorm_bwd_ws(rows, cols) floats)."""
+    dev = _current_device(dy)
+    a = RmsNormBwdArgs()
+    a.dy, a.lddy, a.dtype = _matrix(dy, "dy", dev)
+    a.rows, a.cols = dy.shape
+    if h is not None:
+        a.h, a.ldh, _ = _matrix(h, "h", dev, dy)
+    if q is not None:
+        a.q = _act8(q, a.rows, a.cols, dev)
+    if dres is not None:
+        a.dres, a.lddres, _ = _matrix(dres, "dres", dev, dy)
+    if dx is not None:
+        a.dx, a.lddx, _ = _matrix(dx, "dx", dev, dy)
+    a.gamma, a.rstd = _floats(gamma, a.cols, "gamma", dev), _floats(rstd, a.rows, "rstd", dev)
+    if dgamma is not None:
+        a.dgamma = _floats(dgamma, a.cols, "dgamma", dev)
+    if ws is not None:
+        a.ws, a.ws_floats = _floats(ws, 0, "ws", dev), ws.numel()
+    _check(lib().lpp_kernel_rmsnorm_bwd(C.byref(a), _stream_handle(stream)))
