@@ -31,7 +31,7 @@
  *   - Flat parameter vectors are float32 in the model's canonical order: the
  *     layers' parameter tensors in layer order, each flattened in its natural
  *     layout: conv W[cout][cin][k][k] then bias[cout]; batch-norm gamma[c]
- *     then beta[c]; linear W[out][in] then bias[out].
+ *     then beta[c]; RMS norm gamma[c]; linear W[out][in] then bias[out].
  *   - worker w in [0, K*P) belongs to replica q = w / P; its default block is
  *     w % P + 1 (the paper's rank(u^q), Sec. 3 "Block Selection Rule").  Any
  *     worker may run any partition; the selection rule is caller policy.
@@ -62,7 +62,9 @@ enum lpp_op {
     LPP_MAXPOOL = 4, /* k x k window, stride, pad; padding never wins         */
     LPP_GAP = 5,     /* mean over H x W                                       */
     LPP_LINEAR = 6,  /* y = x W^T + b on the flattened input; params W, b     */
-    LPP_CONCAT = 7   /* channels of in0 followed by channels of in1 (same H, W) */
+    LPP_CONCAT = 7,  /* channels of in0 followed by channels of in1 (same H, W) */
+    LPP_RMSNORM = 8  /* root-mean-square norm over the channels of every pixel;
+                        param gamma (see lpp_kernel_rmsnorm)                  */
 };
 
 enum lpp_dtype { LPP_FP32 = 0, LPP_BF16 = 1 };
@@ -72,11 +74,22 @@ enum lpp_dtype { LPP_FP32 = 0, LPP_BF16 = 1 };
  * updaters); batch-norm sums are merged by fp64 atomic adds, whose order
  * varies, so runs agree to rounding but not bit for bit. */
 enum lpp_mode { LPP_SEQUENTIAL = 0, LPP_ASYNC = 1 };
+/* Added (|) to the mode: activations are kept between the forward and the
+ * backward pass as 8-bit checkpoints (see lpp_kernel_act8_pack) instead of in
+ * the activation type, and their buffers and their gradients' are shared
+ * by layers that are not in use at once.  The forward pass, its loss and its
+ * logits are unchanged to the bit; gradients are those of the rounded
+ * activations, with the exact ReLU decisions.  Weight gradients of 1x1
+ * stride-1 convs and RMS norm gradients read the checkpoints as they are;
+ * other layers' inputs are unpacked first.  Inputs of batch norms stay in
+ * the activation type.  lpp_get_activation and lpp_get_activation_grad return
+ * LPP_ESTATE. */
+enum { LPP_ACT8 = 0x100 };
 
 typedef struct {
     int op;          /* enum lpp_op                                              */
     int in0, in1;    /* producer layer indices (< this layer); -1 = image batch  */
-    int cin, cout;   /* conv/linear channels; bn: cout = channels                */
+    int cin, cout;   /* conv/linear channels; norms: cout = channels             */
     int k, stride, pad; /* conv and maxpool geometry                             */
     int bias;        /* conv/linear: 1 if the layer has a bias vector            */
     int block;       /* 1..P for a layer that owns parameters, else ignored      */
@@ -93,11 +106,11 @@ typedef struct {
                                 master parameters                              */
     float momentum;          /* heavy-ball momentum, 0 = plain SGD             */
     float weight_decay;      /* coupled L2 (g + wd*x), block-restricted        */
-    float bn_eps;
+    float bn_eps;            /* of batch norms and RMS norms                   */
 } lpp_model_desc;
 
 typedef struct {
-    int mode;                     /* enum lpp_mode                              */
+    int mode;                     /* enum lpp_mode, | LPP_ACT8                  */
     void* const* worker_streams;  /* host array of K*P hipStream_t, or NULL: the
                                      library creates its own streams (default
                                      priority)                                  */
@@ -213,6 +226,8 @@ int lpp_get_activation(lpp_ctx* ctx, int worker, int layer, float* host, long n)
 int lpp_get_activation_grad(lpp_ctx* ctx, int worker, int layer, float* host, long n);
 
 long lpp_num_params(const lpp_ctx* ctx);
+/* Bytes of device memory that each of the K*P workers holds for its steps. */
+long lpp_workspace_bytes(const lpp_ctx* ctx);
 int lpp_block_range(const lpp_ctx* ctx, int i, long* lo, long* hi);
 /* Current value of replica q's shared iteration counter C^q (Sec. 2). */
 long lpp_counter(const lpp_ctx* ctx, int replica);

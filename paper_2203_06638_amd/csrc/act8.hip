@@ -164,53 +164,6 @@ hipError_t launch_act8_unpack(int dt, const uint8_t* q, long rows, int C, void* 
     return dt == DT_BF16 ? unpack_rows(q, rows, C, (bf16*)x, ld, st) : unpack_rows(q, rows, C, (float*)x, ld, st);
 }
 
-// ---------------------------------------------------------------- column sums
-//
-// out[i] = sum over s, in a fixed order, of part[s * stride + i], i < n (part 16-byte
-// aligned, stride a multiple of 4 and at least n rounded up to 4): 256 / L quads a
-// workgroup, L lanes over the partials, lane sums added pairwise in LDS.
-template <int L>
-__global__ __launch_bounds__(256) void part_sums_k(const float* __restrict__ part, long stride, int S, long n,
-                                                   float* __restrict__ out) {
-    constexpr int Q = 256 / L;
-    __shared__ f4 lds[L][Q];
-    const int c = threadIdx.x % Q, l = threadIdx.x / Q;
-    const long q = (long)blockIdx.x * Q + c;
-    f4 a = f4{0.f, 0.f, 0.f, 0.f};
-    if (q * 4 < n) {
-        const f4* p = (const f4*)part + q;
-        const long st4 = stride / 4;
-        int s = l;
-        for (; s + 3 * L < S; s += 4 * L) {
-            const f4 v0 = p[s * st4], v1 = p[(s + L) * st4], v2 = p[(s + 2 * L) * st4], v3 = p[(s + 3 * L) * st4];
-            a += (v0 + v1) + (v2 + v3);
-        }
-        for (; s < S; s += L) a += p[s * st4];
-    }
-    lds[l][c] = a;
-#pragma unroll
-    for (int h = L / 2; h > 0; h /= 2) {
-        __syncthreads();
-        if (l < h) lds[l][c] += lds[l + h][c];
-    }
-    if (l == 0 && q * 4 < n) {
-        const f4 v = lds[0][c];
-        for (int j = 0; j < 4; ++j)
-            if (q * 4 + j < n) out[q * 4 + j] = v[j];
-    }
-}
-
-hipError_t launch_part_sums(const float* part, long stride, int S, long n, float* out, hipStream_t st) {
-    if (n <= 0) return hipSuccess;
-    const long quads = (n + 3) / 4;
-    // (few columns: more lanes over the partials, so that there are workgroups enough)
-    if (quads <= 2048 && S > 16)
-        launch((part_sums_k<64>), dim3((unsigned)((quads + 3) / 4)), dim3(256), 0, st, part, stride, S, n, out);
-    else
-        launch((part_sums_k<8>), dim3((unsigned)((quads + 31) / 32)), dim3(256), 0, st, part, stride, S, n, out);
-    return hipGetLastError();
-}
-
 // ---------------------------------------------------------------- weight gradient
 //
 // dW[o][i] = sum over rows of dY[row][o] * X[row][i], X the values of a checkpoint.
@@ -427,7 +380,7 @@ hipError_t launch_act8_wgrad(int dt, const void* dY, long ld, const uint8_t* q, 
                              float* ws, hipStream_t st) {
     const Act8WgPlan p = act8_wgrad_plan(rows, O, I);
     hipError_t e = launch_act8_wgrad_part(dt, dY, ld, q, rows, O, I, p.splits > 1 ? ws : dw, p, st);
-    if (e == hipSuccess && p.splits > 1) e = launch_part_sums(ws, p.part_floats, p.splits, (long)O * I, dw, st);
+    if (e == hipSuccess && p.splits > 1) e = launch_part_sums(ws, p.splits, (int)((long)O * I), dw, st);
     return e;
 }
 

@@ -2111,4 +2111,11 @@ hipError_t launch_wgrad_reduce_multi(const WgRedTable& t, hipStream_t st) {
     return hipGetLastError();
 }
 
+hipError_t launch_part_sums(const float* part, int S, int n, float* out, hipStream_t st) {
+    WgRedTable t{};
+    const int n4 = (int)(((long)n + 3) / 4 * 4);
+    if (!wgred_add(t, part, S, 1, n4, n, n4, 1, 1, out)) return hipErrorInvalidValue;
+    return launch_wgrad_reduce_multi(t, st);
+}
+
 }  // namespace lpp

@@ -152,6 +152,8 @@ struct WgRedTable { WgRedJob job[kWgRedMaxJobs]; int n, wgs; };
 bool wgred_add(WgRedTable& t, const float* part, int splits, int Cout, int Ktot, int Cin, int Cin_p, int R, int S,
                float* g);
 hipError_t launch_wgrad_reduce_multi(const WgRedTable& t, hipStream_t st);
+// one such sum: out[i] = sum over s < S of part[s][i], i < n, rows of n rounded up to 4 floats
+hipError_t launch_part_sums(const float* part, int S, int n, float* out, hipStream_t st);
 
 // ---- bf16 convolution passes (conv_bf16.hip): bf16 source, weights and
 // output, float32 accumulation; geometry as for the float32 passes.  The
@@ -410,8 +412,6 @@ hipError_t launch_act8_wgrad_part(int dt, const void* dY, long ld, const uint8_t
                                   float* part, const Act8WgPlan& p, hipStream_t st);
 hipError_t launch_act8_wgrad(int dt, const void* dY, long ld, const uint8_t* q, long rows, int O, int I, float* dw,
                              float* ws, hipStream_t st);
-// out[i] = sum_s part[s * stride + i] for i < n, fixed order (stride a multiple of 4)
-hipError_t launch_part_sums(const float* part, long stride, int S, long n, float* out, hipStream_t st);
 
 // ---- RMS norm (rmsnorm.hip) ----
 // Tensors of type dt with their row distances in elements; null pointers: not there /
@@ -434,9 +434,10 @@ struct RmsArgs {
     int pitch, G;
 };
 hipError_t launch_rmsnorm(int dt, RmsArgs p, hipStream_t st);
-// h (type dt) or, where it is null, its checkpoint q.  dx, dx2 (same row distance): the
-// same gradient twice, the second added to what is there with acc2.  part:
-// rmsnorm_bwd_parts(rows, C) rows of C rounded up to 4 floats, for dgamma.
+// h (type dt) or, where it is null, its checkpoint q.  dx, dx2 (same row distance; null:
+// not wanted): the same gradient twice, each added to what is there with acc1 / acc2.
+// part (null: not wanted): dgamma's partials, rmsnorm_bwd_parts(rows, C) rows of C
+// rounded up to 4 floats, whose sum is dgamma.
 struct RmsBwdArgs {
     const void *dy, *h;
     const uint8_t* q;
@@ -447,13 +448,13 @@ struct RmsBwdArgs {
     float* part;
     long rows;
     int C;
-    bool acc2;
+    bool acc1, acc2;
 
     const uint8_t* exps;
     int pitch, G;
     long pstride;
 };
 int rmsnorm_bwd_parts(long rows, int C);
-hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, float* dgamma, hipStream_t st);
+hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st);
 
 }  // namespace lpp

@@ -116,6 +116,20 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
     }
 }
 
+// v, added to what is there with acc
+template <bool A, typename T>
+__device__ __forceinline__ void st_sum(T* p, int n, const float* v, bool acc) {
+    constexpr int V = 16 / (int)sizeof(T);
+    float e[V];
+    if (acc) {
+        ld_chunk<A>(p, n, e);
+#pragma unroll
+        for (int j = 0; j < V; ++j) e[j] += v[j];
+        v = e;
+    }
+    st_chunk<A>(p, n, v);
+}
+
 // The gradient.  dgamma: every thread sums its channels over the rows it walks
 // over, the workgroup's row lanes meet in LDS, and each workgroup writes one row of
 // partials [workgroup][stride], summed in a fixed order by launch_part_sums.
@@ -193,16 +207,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
 #pragma unroll
                 for (int j = 0; j < V; ++j) dy[c][j] += e[j];
             }
-            if (p.dx) st_chunk<A>((T*)p.dx + r * p.lddx + ch, n, dy[c]);
-            if (p.dx2) {
-                if (p.acc2) {
-                    float e[V];
-                    ld_chunk<A>((const T*)p.dx2 + r * p.lddx + ch, n, e);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) dy[c][j] += e[j];
-                }
-                st_chunk<A>((T*)p.dx2 + r * p.lddx + ch, n, dy[c]);
-            }
+            if (p.dx) st_sum<A>((T*)p.dx + r * p.lddx + ch, n, dy[c], p.acc1);
+            if (p.dx2) st_sum<A>((T*)p.dx2 + r * p.lddx + ch, n, dy[c], p.acc2);
         }
     }
     if (!p.part) return;
@@ -308,10 +314,9 @@ int rmsnorm_bwd_parts(long rows, int C) {
     return (int)std::max(1l, std::min(1024l, (rows + 7) / 8));
 }
 
-hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, float* dgamma, hipStream_t st) {
+hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st) {
     const int e = dt == DT_BF16 ? 2 : 4;
-    if (!dgamma) p.part = nullptr;
-    if (p.rows <= 0 && !dgamma) return hipSuccess;
+    if (p.rows <= 0 && !p.part) return hipSuccess;
     p.pitch = act8_pitch(p.C);
     p.G = act8_groups(p.C);
     p.exps = p.q ? p.q + p.rows * p.pitch : nullptr;
@@ -322,10 +327,7 @@ hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, float* dgamma, hipStream_t s
     const RowShape s = row_shape(row_chunks(dt, p.C));
     if (!s.tpr) return hipErrorInvalidValue;
     const int wgs = rmsnorm_bwd_parts(p.rows, p.C);
-    const hipError_t err =
-        dt == DT_BF16 ? rms_dispatch<true, bf16>(al, p, s, wgs, st) : rms_dispatch<true, float>(al, p, s, wgs, st);
-    if (err != hipSuccess || !dgamma) return err;
-    return launch_part_sums(p.part, p.pstride, wgs, p.C, dgamma, st);
+    return dt == DT_BF16 ? rms_dispatch<true, bf16>(al, p, s, wgs, st) : rms_dispatch<true, float>(al, p, s, wgs, st);
 }
 
 }  // namespace lpp

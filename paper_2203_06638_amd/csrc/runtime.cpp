@@ -76,6 +76,11 @@ struct Layer {
     // the two convs whose ReLUs its backward applies) is summed from, kept
     // until the backward's one launch of sums
     size_t bpart = 0;
+    // LPP_ACT8: the output's 8-bit checkpoint (bytes), and for a conv that reads
+    // its weight gradient's input from one, the product's plan
+    size_t q = 0;
+    bool wg_act8 = false;
+    lpp::Act8WgPlan wg8{};
 };
 
 struct Plan {
@@ -89,17 +94,18 @@ struct Plan {
 // Execution groups.  A group runs one fused kernel sequence and
 // materialises exactly one layer output (`out`); layers inside a group whose
 // outputs feed nothing else are never stored.
-enum GKind { G_CONV, G_BNACT, G_RELU, G_ADD, G_MAXPOOL, G_GAP, G_LINEAR, G_HEAD, G_CONCAT };
+enum GKind { G_CONV, G_BNACT, G_RELU, G_ADD, G_MAXPOOL, G_GAP, G_LINEAR, G_HEAD, G_CONCAT, G_RMS };
 
 // ops that read a second input (in1)
 inline bool two_inputs(int op) { return op == LPP_ADD || op == LPP_CONCAT; }
 struct Group {
     GKind kind = G_CONV;
     int out = -1;       // the layer whose output this group stores
-    int a = -1;         // G_CONV: conv; G_BNACT: first BN; G_HEAD: pool; else: the layer
+    int a = -1;         // G_CONV: conv; G_BNACT: first BN; G_HEAD: pool; G_RMS: norm; else: the layer
     int stats_bn = -1;  // G_CONV: BN whose batch statistics the conv epilogue computes
     int bn2 = -1;       // G_BNACT: BN of the other branch of the residual add (both normalised)
-    int add = -1;       // G_BNACT / G_CONV: the residual add, if any
+    int add = -1;       // G_BNACT / G_CONV: the residual add, if any; G_RMS: the add whose output the norm reads
+                        //   and which the group computes (and stores) as well, in0 + res
     int res = -1;       // G_BNACT / G_CONV: the residual tensor added unnormalised, if any
     int relu = -1;      // G_BNACT: the closing ReLU, if any; G_CONV: a ReLU applied by the conv's epilogue
     int lin = -1;       // G_HEAD: the linear layer
@@ -131,6 +137,12 @@ struct Model {
     // workgroups a bf16 conv pass aims for: the chip's share of one of the
     // K * P worker streams that run at once, at least a quarter of 512
     int conv_fill = 512;
+    // LPP_ACT8 (plan_act8): outputs whose buffers, and their gradients', are only
+    // held while the groups between the producer and the last consumer run
+    // (shared); those kept as a checkpoint for the backward; and those that decide a
+    // ReLU there, whose checkpoint keeps signs
+    std::vector<char> shared, ck, ck_sign;
+    std::vector<int> first_group, last_group;
 };
 
 int ceil4(int c) { return (c + 3) / 4 * 4; }
@@ -205,6 +217,14 @@ int build_model(const lpp_model_desc* desc, int P, Model& M) {
         case LPP_BN:
             if (L.cout != Y.in0.c) return fail(LPP_EINVAL, std::string(where) + "bn channels do not match the input");
             Y.np = 2L * L.cout;
+            break;
+        case LPP_RMSNORM:
+            if (L.cout != Y.in0.c) return fail(LPP_EINVAL, std::string(where) + "norm channels do not match the input");
+            if (L.cout > lpp::kRmsMaxC)
+                return fail(LPP_EUNSUPPORTED, std::string(where) + "RMS norm takes at most 16384 channels");
+            if (bf && (L.in0 < 0 || M.layers[L.in0].dt != lpp::DT_BF16))
+                return fail(LPP_EUNSUPPORTED, std::string(where) + "with bf16 an RMS norm cannot read pooled features");
+            Y.np = L.cout;
             break;
         case LPP_RELU:
             break;
@@ -413,6 +433,7 @@ void build_groups(Model& M, bool fused) {
                      : op_l == LPP_ADD     ? G_ADD
                      : op_l == LPP_MAXPOOL ? G_MAXPOOL
                      : op_l == LPP_CONCAT  ? G_CONCAT
+                     : op_l == LPP_RMSNORM ? G_RMS
                                            : G_LINEAR;
             g.a = g.out = l;
         }
@@ -494,6 +515,30 @@ void build_groups(Model& M, bool fused) {
             A.premask = B.premask = true;
         }
     }
+    // an RMS norm of a residual add that has a group of its own, and directly
+    // follows it (so that every other reader of the sum comes later, and
+    // the sum's gradient is complete when the norm's backward runs, with nothing
+    // between the two layers that writes a gradient of the add's inputs):
+    // the norm adds, stores the sum as well, and sends its gradient to both
+    if (fused) {
+        std::vector<int> group_of(n, -1);
+        for (int i = 0; i < (int)gs.size(); ++i) group_of[gs[i].out] = i;
+        std::vector<char> drop(gs.size(), 0);
+        for (auto& g : gs) {
+            if (g.kind != G_RMS) continue;
+            const int c = M.layers[g.a].L.in0;
+            if (c < 0 || c != g.a - 1 || op(c) != LPP_ADD || group_of[c] < 0 || gs[group_of[c]].kind != G_ADD ||
+                M.layers[c].L.in0 == M.layers[c].L.in1)
+                continue;
+            drop[group_of[c]] = 1;
+            g.add = c;
+            g.res = M.layers[c].L.in1;
+        }
+        std::vector<Group> kept;
+        for (int i = 0; i < (int)gs.size(); ++i)
+            if (!drop[i]) kept.push_back(gs[i]);
+        gs.swap(kept);
+    }
     // a group runs when its last layer's inputs exist: order by output layer
     std::stable_sort(gs.begin(), gs.end(), [](const Group& x, const Group& y) { return x.out < y.out; });
     M.groups = gs;
@@ -511,6 +556,9 @@ void build_groups(Model& M, bool fused) {
         // the pooled features, kept for the weight gradient; their gradient
         // goes straight to the pool's input
         if (g.kind == G_HEAD) M.stored[g.a] = 1;
+        // the sum that an RMS norm forms; its own readers' gradient is kept there,
+        // the whole one goes straight to the add's inputs
+        if (g.kind == G_RMS && g.add >= 0) M.stored[g.add] = 1;
     }
 }
 
@@ -572,6 +620,121 @@ void plan_folds(Model& M, int N) {
     }
 }
 
+// Whether the backward of a BN group takes the ReLU decision from the group's stored
+// output.  A plain BN + ReLU recomputes it from the BN input and its scale
+// and shift, except that in bf16 the apply pass does so only where the
+// stored output, which the consumer's gradient has just read, no longer lies in the
+// worker's share of the last-level cache (64 x 112x112x64, 103 MB: 81 us reading it,
+// 67 without; 64 x 56x56x64, 26 MB: 22 and 27; WRN-16-8's eight workers, 34
+// and 17 MB: 17.3 and 16.6 on average).  The sums are faster without it at
+// every size (62 -> 40 us, 10.8 -> 8.5 on 32 x 28x28x128).
+bool bnact_recomputes(const Group& G) { return G.relu >= 0 && G.bn2 < 0 && G.add < 0; }
+bool bnact_apply_reads(const Model& M, const Group& G) {
+    const Layer& Y = M.layers[G.a];
+    return bnact_recomputes(G) && M.dt == lpp::DT_BF16 &&
+           2.0 * M.desc.batch * Y.in0.h * Y.in0.w * Y.out.c < 64e6 * M.conv_fill / 512;
+}
+
+// LPP_ACT8: which outputs share buffers and which are kept as checkpoints (Model).
+// An output and its gradient are touched by the groups from its producer to
+// its last consumer only, in the forward pass and, reversed, in the backward
+// pass.  Batch-norm inputs keep buffers of their own, in full: ReLU
+// decisions are recomputed from them.  So do the small float32 tensors of
+// the head.
+void plan_act8(Model& M) {
+    const int n = (int)M.layers.size(), ng = (int)M.groups.size();
+    M.shared.assign(n, 0);
+    M.ck.assign(n, 0);
+    M.ck_sign.assign(n, 0);
+    M.first_group.assign(n, 0);
+    M.last_group.assign(n, ng - 1);
+    std::vector<int> group_of(n, -1);
+    for (int i = 0; i < ng; ++i) {
+        const Group& G = M.groups[i];
+        for (int l : {G.a, G.bn2, G.add, G.relu, G.lin, G.out})
+            if (l >= 0) group_of[l] = i;
+    }
+    for (int l = 0; l < n; ++l) {
+        const int op = M.layers[l].L.op;
+        M.shared[l] = M.stored[l] && op != LPP_GAP && op != LPP_LINEAR;
+        M.first_group[l] = M.last_group[l] = group_of[l];
+        for (int c : M.consumers[l]) {
+            if (M.layers[c].L.op == LPP_BN) M.shared[l] = 0;
+            M.last_group[l] = std::max(M.last_group[l], group_of[c]);
+        }
+    }
+    // outputs that the backward pass reads
+    auto reads = [&](int l, bool sign) {
+        if (l < 0 || !M.shared[l]) return;
+        M.ck[l] = 1;
+        if (sign) M.ck_sign[l] = 1;
+    };
+    for (const Group& G : M.groups) {
+        const Layer& Y = M.layers[G.a];
+        switch (G.kind) {
+        case G_CONV:
+            if (Y.in_bn < 0) reads(Y.L.in0, false);
+            if (G.relu >= 0) reads(G.out, true);
+            if (Y.gsum_y >= 0) reads(Y.gsum_y, true);
+            break;
+        case G_BNACT:
+            if (G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) reads(G.out, true);
+            break;
+        case G_RELU:
+            reads(Y.L.in0, true);
+            break;
+        case G_CONCAT:
+            if (G.mconv_a >= 0) {
+                reads(Y.L.in0, true);
+                reads(Y.L.in1, true);
+            }
+            break;
+        case G_RMS:
+        case G_LINEAR:
+            reads(Y.L.in0, false);
+            break;
+        default:
+            break;
+        }
+    }
+    for (const Group& G : M.groups) {
+        // (a folded group's output is never written)
+        if (G.kind == G_BNACT && G.fold) M.ck[G.out] = 0;
+        if (G.kind != G_CONV) continue;
+        Layer& Y = M.layers[G.a];
+        if (Y.pw || Y.L.k != 1 || Y.L.stride != 1 || Y.L.pad != 0 || Y.L.in0 < 0 || Y.in_bn >= 0 || !M.ck[Y.L.in0])
+            continue;
+        Y.wg_act8 = true;
+        Y.wg8 = lpp::act8_wgrad_plan((long)M.desc.batch * Y.out.h * Y.out.w, Y.L.cout, Y.L.cin);
+        Y.wg.splits = Y.wg8.splits;
+        Y.wg.part_floats = Y.wg8.splits * Y.wg8.part_floats;
+    }
+}
+
+// Offsets of buffers that are held from group `from` to group `to` each, so that
+// those held at once do not overlap: largest first, each at the lowest
+// place that is free.  Returns the bytes they take together.
+struct Held { size_t bytes; int from, to; size_t* off; };
+size_t place_held(std::vector<Held> items) {
+    std::stable_sort(items.begin(), items.end(), [](const Held& a, const Held& b) { return a.bytes > b.bytes; });
+    size_t total = 0;
+    for (size_t i = 0; i < items.size(); ++i) {
+        std::vector<std::pair<size_t, size_t>> busy;
+        for (size_t j = 0; j < i; ++j)
+            if (items[j].from <= items[i].to && items[i].from <= items[j].to)
+                busy.push_back({*items[j].off, *items[j].off + items[j].bytes});
+        std::sort(busy.begin(), busy.end());
+        size_t at = 0;
+        for (auto& b : busy) {
+            if (at + items[i].bytes <= b.first) break;
+            at = std::max(at, b.second);
+        }
+        *items[i].off = at;
+        total = std::max(total, at + items[i].bytes);
+    }
+    return total;
+}
+
 // ------------------------------------------------------------------------
 
 struct Timer {
@@ -626,6 +789,7 @@ struct lpp_ctx {
     // sequential mode merges batch-norm reductions in a fixed order (bitwise
     // reproducible); async mode through atomic accumulators
     bool fixed_order = true;
+    bool act8 = false;                       // activations kept as 8-bit checkpoints (LPP_ACT8)
     bool graphs = true;
     long ps_floats = 0;
     long wpart_floats = 0;                   // weight-gradient partials of one reduce batch
@@ -651,6 +815,8 @@ struct lpp_ctx {
     const void* wdg(Worker& w, const Layer& Y) { return (const char*)w.wbuf + Y.wd_off * lpp_dt_size(); }
     size_t lpp_dt_size() const { return M.dt == lpp::DT_BF16 ? 2 : 4; }
     float* aux(Worker& w, int l) { return (float*)(w.ws + M.layers[l].aux); }
+    uint8_t* ckpt(Worker& w, int l) { return (uint8_t*)(w.ws + M.layers[l].q); }
+    bool has_ckpt(int l) const { return act8 && l >= 0 && M.ck[l]; }
     float* bpart(Worker& w, int l) { return (float*)(w.ws + M.layers[l].bpart); }
     double* acc_fwd(Worker& w, int l) { return (double*)(w.ws + M.layers[l].acc); }
     double* acc_bwd(Worker& w, int l) {
@@ -1008,6 +1174,27 @@ int run_forward(lpp_ctx* c, Worker& w) {
                                       Mrows, C, st));
             break;
         }
+        case G_RMS: {
+            const int C = Y.out.c;
+            lpp::RmsArgs a{};
+            a.x = G.add >= 0 ? c->input(w, M.layers[G.add].L.in0) : x0;
+            if (G.add >= 0) {
+                a.res = c->act(w, G.res);
+                a.h = c->act(w, G.add);
+            }
+            a.y = c->act(w, G.a);
+            a.q = c->has_ckpt(G.a) ? c->ckpt(w, G.a) : nullptr;
+            a.keep_sign = a.q && M.ck_sign[G.a];
+            a.ldx = a.ldres = a.ldh = a.ldy = C;
+            a.gamma = w.v + Y.poff;
+            a.rstd = c->aux(w, G.a);
+            a.rows = Mrows;
+            a.C = C;
+            a.eps = M.desc.bn_eps;
+            LAUNCH("rmsnorm", ((a.res ? 4.0 : 2.0) * eb + (a.q ? 1.0 : 0.0)) * Mrows * C, st,
+                   lpp::launch_rmsnorm(dt, a, st));
+            break;
+        }
         case G_RELU:
             LAUNCH("relu", 2.0 * eb * Mrows * Y.out.c, st,
                    lpp::launch_relu_fwd(dt, x0, c->act(w, G.a), Mrows * Y.out.c, st));
@@ -1048,6 +1235,16 @@ int run_forward(lpp_ctx* c, Worker& w) {
             break;
         }
         }
+        // the outputs that the backward will read, in 8 bits (an RMS norm has
+        // written its own)
+        for (int l : {G.kind == G_RMS ? G.add : -1, G.kind == G_RMS ? -1 : G.out})
+            if (c->has_ckpt(l)) {
+                const Layer& O = M.layers[l];
+                const long rows = (long)N * O.out.h * O.out.w;
+                LAUNCH("act8_pack", (eb + 1.0) * rows * O.out.c, st,
+                       lpp::launch_act8_pack(dt, c->act(w, l), O.out.c, rows, O.out.c, M.ck_sign[l] != 0,
+                                             c->ckpt(w, l), st));
+            }
     }
     if (!loss_done) {
         const int last = (int)M.layers.size() - 1;
@@ -1097,10 +1294,41 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
         lpp::tile_sum_add(sums, pmean, ld, tiles, R, rows, C, out);
         return LPP_OK;
     };
+    // with LPP_ACT8: layer l's output, unpacked into its buffer before the first
+    // kernel that reads it there
+    std::vector<char> unpacked(M.layers.size(), 0);
+    auto restore = [&](int l) -> int {
+        if (!c->has_ckpt(l) || unpacked[l]) return LPP_OK;
+        unpacked[l] = 1;
+        const Layer& O = M.layers[l];
+        const long rows = (long)N * O.out.h * O.out.w;
+        LAUNCH("act8_unpack", (eb + 1.0) * rows * O.out.c, st,
+               lpp::launch_act8_unpack(dt, c->ckpt(w, l), rows, O.out.c, c->act(w, l), O.out.c, st));
+        return LPP_OK;
+    };
     for (int gi = (int)M.groups.size() - 1; gi >= 0; --gi) {
         const Group& G = M.groups[gi];
         if (!pl.run[G.out]) continue;
         Layer& Y = M.layers[G.a];
+        if (c->act8) {
+            int rc = LPP_OK;
+            auto want = [&](int l) {
+                if (!rc) rc = restore(l);
+            };
+            if (G.kind == G_CONV) {
+                if (G.relu >= 0 && !G.premask) want(G.out);
+                if (pl.wgrad[G.a] && Y.in_bn < 0 && !Y.wg_act8) want(Y.L.in0);
+                if (pl.din0[G.a] && Y.gsum_y >= 0) want(Y.gsum_y);
+            } else if (G.kind == G_BNACT && G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) {
+                want(G.out);
+            } else if (G.kind == G_RELU || (G.kind == G_LINEAR && pl.wgrad[G.a])) {
+                want(Y.L.in0);
+            } else if (G.kind == G_CONCAT && G.mconv_a >= 0) {
+                want(Y.L.in0);
+                want(Y.L.in1);
+            }
+            if (rc) return rc;
+        }
         const void* x0 = c->input(w, Y.L.in0);
         void* dy = c->dact(w, G.out);
         void* dx0 = pl.din0[G.a] ? c->dact(w, Y.L.in0) : nullptr;
@@ -1158,7 +1386,11 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
                                     w.g + Y.poff))
                     return fail(LPP_EINVAL, "weight-gradient reduce: unsupported shape");
                 woff += pf;
-                if (bf)
+                if (Y.wg_act8)
+                    LAUNCH("conv_wgrad", 2.0 * Y.macs, st,
+                           lpp::launch_act8_wgrad_part(dt, dy, Y.L.cout, c->ckpt(w, Y.L.in0), Mo, Y.L.cout, Y.L.cin,
+                                                       part, Y.wg8, st));
+                else if (bf)
                     LAUNCH("conv_wgrad", 2.0 * Y.macs, st,
                            lpp::launch_conv_wgrad_bf16((const uint16_t*)dy, (const uint16_t*)x0, part, N, Y.in0.h,
                                                        Y.in0.w, Y.cin_p, Y.out.h, Y.out.w, Y.L.cout, Y.L.k, Y.L.k,
@@ -1246,7 +1478,7 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
             const Layer* Y2 = b2 >= 0 ? &M.layers[b2] : nullptr;
             // plain BN + ReLU: the ReLU decision is recomputed from the BN input
             // and its scale and shift instead of read from the output
-            const bool xmask = G.relu >= 0 && G.bn2 < 0 && G.add < 0;
+            const bool xmask = bnact_recomputes(G);
             lpp::BnBwdArgs a{dy, G.relu >= 0 && !xmask ? c->act(w, G.out) : nullptr, x0, ax, ax + C,
                              want2 ? c->act(w, Y2->L.in0) : nullptr, want2 ? ax2 : nullptr,
                              want2 ? ax2 + C : nullptr, Min, C, xmask ? ax + 2 * C : nullptr};
@@ -1284,14 +1516,7 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
             void* d1 = want1 && pl.din0[G.a] ? dx0 : nullptr;
             void* d2 = want2 && pl.din0[b2] ? c->dact(w, Y2->L.in0) : nullptr;
             void* dr = want_res ? c->dact(w, G.res) : nullptr;
-            // bf16: the apply pass recomputes the mask only where the stored
-            // output, which the consumer's gradient has just read, no longer
-            // lies in the worker's share of the last-level cache (64 x
-            // 112x112x64, 103 MB: 81 us reading it, 67 without; 64 x 56x56x64,
-            // 26 MB: 22 and 27; WRN-16-8's eight workers, 34 and 17 MB: 17.3
-            // and 16.6 on average).  The sums are faster without it at every
-            // size (62 -> 40 us, 10.8 -> 8.5 on 32 x 28x28x128).
-            if (bf && xmask && eb * Min * C < 64e6 * M.conv_fill / 512) {
+            if (bnact_apply_reads(M, G)) {
                 a.mask = c->act(w, G.out);
                 a.mask_ss = nullptr;
             }
@@ -1303,6 +1528,53 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
                        lpp::launch_bn_bwd_apply(dt, a, k, d1, pl.acc0[G.a] != 0, d2, want2 && pl.acc0[b2] != 0, dr,
                                                 acc_res, st));
             }
+            break;
+        }
+        case G_RMS: {
+            const int C = Y.out.c;
+            lpp::RmsBwdArgs a{};
+            a.dy = dy;
+            if (c->has_ckpt(Y.L.in0)) a.q = c->ckpt(w, Y.L.in0);
+            else a.h = x0;
+            a.lddy = a.ldh = a.lddres = a.lddx = C;
+            a.gamma = w.v + Y.poff;
+            a.rstd = c->aux(w, G.a);
+            a.rows = Min;
+            a.C = C;
+            if (G.add >= 0 && dx0) {
+                // the sum's gradient (what its other readers left in dx0, and this
+                // norm's) goes to both of the add's inputs
+                const lpp_layer& A = M.layers[G.add].L;
+                if (pl.acc0[G.a]) a.dres = dx0;
+                if (pl.din0[G.add]) {
+                    a.dx = c->dact(w, A.in0);
+                    a.acc1 = pl.acc0[G.add] != 0;
+                }
+                if (pl.din1[G.add]) {
+                    a.dx2 = c->dact(w, A.in1);
+                    a.acc2 = pl.acc1[G.add] != 0;
+                }
+            } else if (dx0) {
+                a.dx = dx0;
+                a.acc1 = pl.acc0[G.a] != 0;
+            }
+            if (pl.wgrad[G.a]) {
+                const int parts = lpp::rmsnorm_bwd_parts(Min, C);
+                const long pf = align64((long)parts * C);
+                if (red.n == lpp::kWgRedMaxJobs || woff + pf > c->wpart_floats) {
+                    int rc = flush_reduce();
+                    if (rc) return rc;
+                }
+                a.part = w.wpart + woff;
+                if (!lpp::wgred_add(red, a.part, parts, 1, C, C, C, 1, 1, w.g + Y.poff))
+                    return fail(LPP_EINVAL, "norm gradient reduce: unsupported shape");
+                woff += pf;
+            }
+            if (a.dx || a.dx2 || a.part)
+                LAUNCH("rmsnorm_bwd",
+                       (eb * (1.0 + (a.dx ? 1 : 0) + (a.dx2 ? 1 : 0) + (a.dres ? 1 : 0) + (a.acc1 ? 1 : 0) +
+                              (a.acc2 ? 1 : 0)) + (a.q ? 1.0 : eb)) * Min * C, st,
+                       lpp::launch_rmsnorm_bwd(dt, a, st));
             break;
         }
         case G_RELU:
@@ -1460,7 +1732,8 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
     c->K = K;
     c->P = P;
     c->M.conv_fill = std::max(128, 512 / (K * std::max(P, 1)));
-    c->mode = opt ? opt->mode : LPP_SEQUENTIAL;
+    c->mode = opt ? opt->mode & ~LPP_ACT8 : LPP_SEQUENTIAL;
+    c->act8 = opt && (opt->mode & LPP_ACT8);
     c->fixed_order = c->mode == LPP_SEQUENTIAL;
     if (c->mode != LPP_SEQUENTIAL && c->mode != LPP_ASYNC) return fail(LPP_EINVAL, "unknown mode");
     build_groups(c->M, !(opt && opt->unfused));
@@ -1496,6 +1769,7 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
                                                        Y.L.k, Y.L.k, Y.L.stride, Y.L.pad);
     }
     if (!(opt && opt->unfused)) plan_folds(M, N);
+    if (c->act8) plan_act8(M);
     c->wbuf_floats = wf;
     std::vector<lpp::SnapEntry> snap_tab(2 * snaps.size() + 1);
     c->snap_tiles = lpp::snapshot_table(snaps.data(), (int)snaps.size(), d, M.dt, snap_tab.data(),
@@ -1520,14 +1794,26 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
     c->off_args = take(sizeof(lpp::StepArgs));
     c->off_img = take(eb * (size_t)N * M.desc.in_h * M.desc.in_w * M.img_cp);
     long ps = 1, wpart = 1, wsum = 0;
+    std::vector<Held> held;   // LPP_ACT8: the shared buffers
     for (int l = 0; l < (int)M.layers.size(); ++l) {
         Layer& Y = M.layers[l];
         const long rows_out = (long)N * Y.out.h * Y.out.w;
-        if (M.stored[l]) {
+        if (c->act8 && M.shared[l]) {
+            const size_t bytes = align256(dt_size(Y.dt) * (size_t)rows_out * Y.out.c);
+            held.push_back({bytes, M.first_group[l], M.last_group[l], &Y.act});
+            held.push_back({bytes, M.first_group[l], M.last_group[l], &Y.dact});
+            if (M.ck[l]) Y.q = take((size_t)lpp::act8_bytes(rows_out, Y.out.c));
+        } else if (M.stored[l]) {
             Y.act = take(dt_size(Y.dt) * (size_t)rows_out * Y.out.c);
             Y.dact = take(dt_size(Y.dt) * (size_t)rows_out * Y.out.c);
         }
         if (Y.L.op == LPP_BN) Y.aux = take(sizeof(float) * 7 * Y.out.c);
+        if (Y.L.op == LPP_RMSNORM) {
+            Y.aux = take(sizeof(float) * rows_out);   // rstd
+            const long pf = align64((long)lpp::rmsnorm_bwd_parts(rows_out, Y.out.c) * Y.out.c);
+            wpart = std::max(wpart, pf);
+            wsum += pf;
+        }
         if (Y.L.op == LPP_MAXPOOL) Y.aux = take((size_t)rows_out * Y.out.c);
         const long rin = (long)N * Y.in0.h * Y.in0.w;
         if (Y.L.op == LPP_BN) ps = std::max<long>(ps, (long)lpp::stats_tiles(rin, Y.out.c) * Y.out.c);
@@ -1570,6 +1856,10 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
     c->ps_floats = ps;
     c->off_ps = take(sizeof(float) * 3 * ps);
     c->off_wpart = take(sizeof(float) * wpart);
+    if (!held.empty()) {
+        const size_t base = take(place_held(held));
+        for (Held& h : held) *h.off += base;
+    }
     c->ws_bytes = off;
 
     // device allocations
@@ -1817,6 +2107,7 @@ static int copy_layer_nchw(lpp_ctx* c, int worker, int layer, bool grad, float* 
     int rc = check_worker(c, worker);
     if (rc) return rc;
     if (layer < 0 || layer >= (int)c->M.layers.size()) return fail(LPP_EINVAL, "layer out of range");
+    if (c->act8) return fail(LPP_ESTATE, "a context with LPP_ACT8 does not hold its activations after a step");
     const Model& M = c->M;
     const Layer& Y = M.layers[layer];
     const int N = M.desc.batch;
@@ -1897,6 +2188,8 @@ int lpp_block_range(const lpp_ctx* c, int i, long* lo, long* hi) {
     *hi = c->M.bhi[i];
     return LPP_OK;
 }
+
+long lpp_workspace_bytes(const lpp_ctx* c) { return c ? (long)c->ws_bytes : -1; }
 
 long lpp_counter(const lpp_ctx* c, int replica) {
     if (!c || replica < 0 || replica >= c->K) return -1;
@@ -2180,7 +2473,7 @@ int lpp_kernel_act8_unpack(const void* q, long rows, int cols, void* x, int dtyp
 }
 
 long lpp_act8_wgrad_ws(long rows, int cout, int cin) {
-    if (lpp_act8_bytes(rows, cin) < 0 || lpp_act8_bytes(rows, cout) < 0 || (long)cout * cin > (1L << 31)) return -1;
+    if (lpp_act8_bytes(rows, cin) < 0 || lpp_act8_bytes(rows, cout) < 0 || (long)cout * cin >= (1L << 31) - 4) return -1;
     const lpp::Act8WgPlan p = lpp::act8_wgrad_plan(rows, cout, cin);
     return p.splits > 1 ? p.splits * p.part_floats : 0;
 }
@@ -2272,10 +2565,13 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* a, void* stream) {
     p.lddx = a->lddx;
     p.gamma = a->gamma;
     p.rstd = a->rstd;
-    p.part = a->ws;
+    p.part = a->dgamma ? a->ws : nullptr;
     p.rows = a->rows;
     p.C = a->cols;
-    hipError_t e = lpp::launch_rmsnorm_bwd(a->dtype, p, a->dgamma, (hipStream_t)stream);
+    hipError_t e = lpp::launch_rmsnorm_bwd(a->dtype, p, (hipStream_t)stream);
+    if (e == hipSuccess && a->dgamma)
+        e = lpp::launch_part_sums(a->ws, lpp::rmsnorm_bwd_parts(a->rows, a->cols), a->cols, a->dgamma,
+                                  (hipStream_t)stream);
     if (e != hipSuccess) return fail(LPP_EHIP, std::string("rmsnorm_bwd: ") + hipGetErrorString(e));
     return LPP_OK;
 }

@@ -17,9 +17,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblpp.so")
 _LIB = None
 
-CONV, BN, RELU, ADD, MAXPOOL, GAP, LINEAR, CONCAT = range(8)
+CONV, BN, RELU, ADD, MAXPOOL, GAP, LINEAR, CONCAT, RMSNORM = range(9)
 FP32, BF16 = 0, 1
 SEQUENTIAL, ASYNC = 0, 1
+ACT8 = 0x100
 OK, EINVAL, ENOMEM, EHIP, ESTATE, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 STATUS = {0: "LPP_OK", -1: "LPP_EINVAL", -2: "LPP_ENOMEM", -3: "LPP_EHIP", -4: "LPP_ESTATE", -5: "LPP_EUNSUPPORTED"}
 
@@ -106,6 +107,7 @@ def lib():
             "lpp_get_activation": ([ctx, C.c_int, C.c_int, fp, C.c_long], C.c_int),
             "lpp_get_activation_grad": ([ctx, C.c_int, C.c_int, fp, C.c_long], C.c_int),
             "lpp_num_params": ([ctx], C.c_long),
+            "lpp_workspace_bytes": ([ctx], C.c_long),
             "lpp_block_range": ([ctx, C.c_int, C.POINTER(C.c_long), C.POINTER(C.c_long)], C.c_int),
             "lpp_counter": ([ctx, C.c_int], C.c_long),
             "lpp_sync": ([ctx], C.c_int),
@@ -182,11 +184,12 @@ class Context:
     """One lpp_ctx: K replicas x P workers of `model` on the current device."""
 
     def __init__(self, model, K, batch, mode=SEQUENTIAL, dtype=FP32, momentum=0.0, weight_decay=0.0,
-                 bn_eps=1e-5, streams=None, avg_stream=None, unfused=False, graphs=True):
+                 bn_eps=1e-5, streams=None, avg_stream=None, unfused=False, graphs=True, act8=False):
+        """act8: activations are kept for the backward pass in 8 bits."""
         self.model = model
         self.K, self.P, self.batch = K, model.P, batch
         self._desc = make_desc(model, batch, dtype, momentum, weight_decay, bn_eps)
-        opt = Options(mode, None, None, int(unfused), int(not graphs))
+        opt = Options(mode | (ACT8 if act8 else 0), None, None, int(unfused), int(not graphs))
         if streams is not None:
             assert len(streams) == K * model.P
             self._streams = (C.c_void_p * len(streams))(*[_stream_handle(s).value for s in streams])
@@ -259,6 +262,10 @@ class Context:
         lo, hi = C.c_long(), C.c_long()
         _check(lib().lpp_block_range(self._ctx, i, C.byref(lo), C.byref(hi)))
         return lo.value, hi.value
+
+    def workspace_bytes(self):
+        """Device memory of each worker."""
+        return int(lib().lpp_workspace_bytes(self._ctx))
 
     def counter(self, replica):
         return int(lib().lpp_counter(self._ctx, replica))

@@ -12,7 +12,7 @@ every layer.
 """
 from __future__ import annotations
 
-from .lpp import ADD, BN, CONCAT, CONV, GAP, LINEAR, MAXPOOL, RELU
+from .lpp import ADD, BN, CONCAT, CONV, GAP, LINEAR, MAXPOOL, RELU, RMSNORM
 
 
 class Model:
@@ -54,6 +54,11 @@ class Model:
         self.specs += [("bn_gamma", c, 0), ("bn_beta", c, 0)]
         return self._emit((BN, x, -1, c, c, 0, 1, 0, 0, 0), self._shape(x))
 
+    def rmsnorm(self, x):
+        c = self._shape(x)[0]
+        self.specs += [("rms_gamma", c, 0)]
+        return self._emit((RMSNORM, x, -1, c, c, 0, 1, 0, 0, 0), self._shape(x))
+
     def relu(self, x):
         return self._emit((RELU, x, -1, 0, 0, 0, 1, 0, 0, 0), self._shape(x))
 
@@ -89,7 +94,7 @@ class Model:
         assert len(unit_to_block) == self.n_units
         assert list(unit_to_block) == sorted(unit_to_block)
         for rec, u in zip(self.layers, self.unit_of):
-            rec[9] = unit_to_block[u] if rec[0] in (CONV, BN, LINEAR) else 0
+            rec[9] = unit_to_block[u] if rec[0] in (CONV, BN, LINEAR, RMSNORM) else 0
         self.P = max(unit_to_block)
         return self
 
@@ -140,6 +145,18 @@ def bottleneck_unit(m, x, mid, stride, act=True):
     y = m.bn(m.conv(y, cout, 1, 1, 0))
     sc = m.bn(m.conv(x, cout, 1, stride, 0)) if (stride != 1 or cin != cout) else x
     return relu(m.add(y, sc))
+
+
+def pre_norm_unit(m, x, expand=4, act=True):
+    """x + conv3x3(norm(x)), then x + conv1x1(ReLU(conv1x1(norm(x)))) with
+    `expand` times the channels between: RMS norms over the channels, which
+    need no statistics of the updater's batch, and biased convs.
+    act=False leaves the ReLU out."""
+    m.new_unit()
+    c = m.shapes[x][0]
+    x = m.add(m.conv(m.rmsnorm(x), c, 3, bias=True), x)
+    y = m.conv(m.rmsnorm(x), expand * c, 1, bias=True)
+    return m.add(m.conv(m.relu(y) if act else y, c, 1, bias=True), x)
 
 
 # ---------------------------------------------------------------------------
@@ -274,3 +291,20 @@ def squeezenet_p4(n_classes=10, act=True):
     forward work: {stem, fire2, fire3} {fire4, fire5} {fire6, fire7}
     {fire8, fire9, classifier}."""
     return squeezenet(n_classes, act=act, blocks=[1, 1, 1, 2, 2, 3, 3, 4, 4, 4])
+
+
+def pre_norm_net(widths=(64, 128, 256), units=2, n_classes=10, hw=32, expand=4, blocks=None, act=True):
+    """Residual net of pre_norm_units: a 3x3 stem, `units` of them a stage, a
+    norm and a 3x3/2 conv between stages, a norm, global pool and linear
+    layer at the end."""
+    m = Model("pre_norm", (3, hw, hw), n_classes)
+    x = m.conv(-1, widths[0], 3, bias=True)
+    for si, w in enumerate(widths):
+        for u in range(units):
+            x = pre_norm_unit(m, x, expand, act)
+        if si + 1 < len(widths):
+            m.new_unit()
+            x = m.conv(m.rmsnorm(x), widths[si + 1], 3, 2, bias=True)
+    m.new_unit()
+    m.linear(m.gap(m.rmsnorm(x)), n_classes)
+    return m.assign_blocks(blocks or [1] * m.n_units)

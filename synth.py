@@ -45,7 +45,7 @@ def init_params(specs, seed: int) -> np.ndarray:
       'conv_w'   -> N(0, 2 / fan_in)            (He normal)
       'linear_w' -> U(-1/sqrt(fan_in), +1/sqrt(fan_in))
       'bias'     -> 0
-      'bn_gamma' -> 1
+      'bn_gamma', 'rms_gamma' -> 1
       'bn_beta'  -> 0
     """
     rng = _rng(seed + 1_000_003)
@@ -58,7 +58,7 @@ def init_params(specs, seed: int) -> np.ndarray:
             parts.append(rng.uniform(-b, b, size=numel).astype(np.float32))
         elif kind in ("bias", "bn_beta"):
             parts.append(np.zeros(numel, np.float32))
-        elif kind == "bn_gamma":
+        elif kind in ("bn_gamma", "rms_gamma"):
             parts.append(np.ones(numel, np.float32))
         else:
             raise ValueError(kind)

@@ -147,3 +147,31 @@ def test_reference_gradient_against_differences():
         num = (loss(x + e * vx, gamma + e * vg) - loss(x - e * vx, gamma - e * vg)) / (2 * e)
         # (central differences: e^2 of the third derivative, and rounding 2^-53 / e)
         assert abs(num - (dx * vx).sum() - (dg * vg).sum()) < 1e-7 * (dx.abs().sum() + dg.abs().sum())
+
+
+# -- RMS norm layers in a model description --------------------------------------
+
+def test_describe_rmsnorm():
+    from paper_2203_06638_amd import models as PM
+    m = PM.pre_norm_net((16, 32), 1, 10, 12)
+    info = lpp.describe(m)
+    assert info.d == m.d
+    assert sum(n for kind, n, _ in m.specs if kind == "rms_gamma") == 16 * 3 + 32 * 3
+    bad = PM.Model("bad", (3, 8, 8), 4)
+    t = bad.rmsnorm(bad.conv(-1, 8, 3))
+    bad.layers[t][4] = 12
+    bad.linear(bad.gap(t), 4)
+    with pytest.raises(lpp.LppError) as e:
+        lpp.describe(bad.assign_blocks([1]))
+    assert e.value.code == lpp.EINVAL
+    wide = PM.Model("wide", (3, 2, 2), 4)
+    wide.linear(wide.gap(wide.rmsnorm(wide.conv(-1, 16388, 1, 1, 0))), 4)
+    with pytest.raises(lpp.LppError) as e:
+        lpp.describe(wide.assign_blocks([1]))
+    assert e.value.code == lpp.EUNSUPPORTED
+    pooled = PM.Model("pooled", (8, 4, 4), 4)
+    pooled.linear(pooled.gap(pooled.rmsnorm(pooled.gap(pooled.conv(-1, 8, 1, 1, 0)))), 4)
+    lpp.describe(pooled.assign_blocks([1]))
+    with pytest.raises(lpp.LppError) as e:
+        lpp.describe(pooled, dtype=lpp.BF16)
+    assert e.value.code == lpp.EUNSUPPORTED

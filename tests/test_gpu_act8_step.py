@@ -1,0 +1,272 @@
+"""RMS norm layers and the LPP_ACT8 option inside lpp_step.
+
+The norm's networks are checked against the same layer list in float64 PyTorch with
+autograd (CPU), at the bars of the other networks.  LPP_ACT8 must leave loss and
+logits as they are, bit for bit, and give the gradients of the rounded
+activations: checked at first hand where one checkpoint separates a weight from the
+loss, and on whole networks by their distance from the gradients without
+it.
+"""
+import math
+import sys
+
+import numpy as np
+import pytest
+
+import synth
+from paper_2203_06638_amd import lpp
+from paper_2203_06638_amd import models as PM
+from tests import act8ref as R
+from tests import parity as PR
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    torch.cuda.init()
+
+
+def inputs(model, batch, seed, bf16=False):
+    c, h, w = model.in_shape
+    img = synth.images(seed, batch, c, h, w)
+    if bf16:
+        img = synth.round_to_bf16(img)
+    lab = synth.labels(seed, batch, model.n_classes)
+    x = synth.init_params(model.specs, seed)
+    # norms' gammas about 1, biases about 0
+    rng, pos, tensors = np.random.default_rng(seed), 0, []
+    for kind, n, _ in model.specs:
+        if kind in ("rms_gamma", "bn_gamma", "bn_beta", "bias"):
+            x[pos:pos + n] += (0.1 * rng.standard_normal(n)).astype(np.float32)
+        tensors.append((kind, pos, n))
+        pos += n
+    return img, lab, x, tensors
+
+
+def reference(model, img, lab, x, eps=1e-5):
+    """(loss, logits, gradient) in float64."""
+    F = torch.nn.functional
+    p = torch.from_numpy(x.astype(np.float64)).requires_grad_()
+    pos, outs = 0, []
+
+    def take(*shape):
+        nonlocal pos
+        n = math.prod(shape)
+        pos += n
+        return p[pos - n:pos].view(*shape)
+    for op, a, b, cin, cout, k, stride, pad, bias, _ in model.layers:
+        t = outs[a] if a >= 0 else torch.from_numpy(img.astype(np.float64))
+        if op == lpp.CONV:
+            w = take(cout, cin, k, k)
+            t = F.conv2d(t, w, take(cout) if bias else None, stride, pad)
+        elif op == lpp.RMSNORM:
+            t = t / torch.sqrt((t * t).mean(1, keepdim=True) + eps) * take(cout).view(1, -1, 1, 1)
+        elif op == lpp.BN:
+            m, v = t.mean((0, 2, 3), keepdim=True), t.var((0, 2, 3), unbiased=False, keepdim=True)
+            t = (t - m) / torch.sqrt(v + eps) * take(cout).view(1, -1, 1, 1) + take(cout).view(1, -1, 1, 1)
+        elif op == lpp.RELU:
+            t = t.relu()
+        elif op == lpp.ADD:
+            t = t + outs[b]
+        elif op == lpp.GAP:
+            t = t.mean((2, 3), keepdim=True)
+        elif op == lpp.LINEAR:
+            w = take(cout, cin)
+            t = t.flatten(1) @ w.t() + take(cout)
+        else:
+            raise AssertionError(op)
+        outs.append(t)
+    z = outs[-1].flatten(1)
+    loss = F.cross_entropy(z, torch.from_numpy(lab.astype(np.int64)))
+    loss.backward()
+    return loss.item(), z.detach().numpy(), p.grad.numpy()
+
+
+def step(model, img, lab, x, part=0, dtype=lpp.FP32, steps=1, **kw):
+    """(loss, logits, gradient, workspace bytes) of a step at parameters x; with
+    steps > 1 the step is repeated at the same x (replays)."""
+    im, lb = torch.from_numpy(img).cuda(), torch.from_numpy(lab).cuda()
+    with lpp.Context(model, K=1, batch=len(lab), dtype=dtype, **kw) as ctx:
+        for _ in range(steps):
+            ctx.set_params(x)
+            ctx.step(0, im, lb, part, 0.1)
+            ctx.sync()
+        return ctx.get_loss(0), ctx.get_logits(0), ctx.get_grad(0), ctx.workspace_bytes()
+
+
+def mini(act=True, blocks=None, widths=(16, 32), hw=12):
+    return PM.pre_norm_net(widths, 1, 10, hw, 4, blocks, act)
+
+
+@pytest.mark.parametrize("unfused", [False, True])
+def test_pre_norm_net_against_float64(unfused):
+    m = mini(act=False)
+    img, lab, x, tensors = inputs(m, 6, 3)
+    loss, z, g = reference(m, img, lab, x)
+    got = step(m, img, lab, x, unfused=unfused)
+    assert abs(got[0] - loss) <= 1e-5 * abs(loss)
+    assert PR.relerr(got[1], z, PR.TAU_LOGITS) <= PR.TOL_LOGITS
+    for kind, lo, n in tensors:
+        assert PR.relerr(got[2][lo:lo + n], g[lo:lo + n], PR.TAU) <= PR.TOL_GRAD, (kind, lo)
+
+
+def test_pre_norm_net_with_relu_against_float64():
+    """A ReLU decision may differ where the input is within float32 rounding of 0:
+    gradients in the 2-norm."""
+    m = mini()
+    img, lab, x, tensors = inputs(m, 6, 4)
+    loss, z, g = reference(m, img, lab, x)
+    got = step(m, img, lab, x)
+    assert PR.relerr(got[1], z, PR.TAU_LOGITS) <= PR.TOL_LOGITS
+    assert np.linalg.norm(got[2] - g) <= 1e-3 * np.linalg.norm(g)
+
+
+def test_pre_norm_net_bf16():
+    m = mini(act=False)
+    img, lab, x, tensors = inputs(m, 8, 5, True)
+    loss, z, g = reference(m, img, lab, x)
+    got = step(m, img, lab, x, dtype=lpp.BF16)
+    assert PR.relerr(got[1], z, PR.TAU_BF16) <= PR.TOL_BF16
+    for kind, lo, n in tensors:
+        assert PR.relerr(got[2][lo:lo + n], g[lo:lo + n], PR.TAU_BF16) <= PR.TOL_BF16, (kind, lo)
+
+
+@pytest.mark.parametrize("act8", [False, True])
+@pytest.mark.parametrize("dtype", [lpp.FP32, lpp.BF16])
+def test_partial_is_restricted_full(dtype, act8):
+    blocks = [1, 1, 2, 3, 4]
+    m = mini(blocks=blocks)
+    assert m.P == 4 and len(blocks) == m.n_units
+    img, lab, x, _ = inputs(m, 6, 6, True)
+    full = step(m, img, lab, x, 0, dtype, act8=act8)
+    info = lpp.describe(m, 6, dtype=dtype)
+    for part in range(1, m.P + 1):
+        got = step(m, img, lab, x, part, dtype, act8=act8)
+        lo, hi = info.block_lo[part], info.block_hi[part]
+        assert np.array_equal(got[2][lo:hi], full[2][lo:hi]), part
+        assert not got[2][:lo].any() and not got[2][hi:].any()
+        assert got[0] == full[0]
+
+
+NETS = {
+    "pre_norm": lambda: PM.pre_norm_net((16, 32, 64), 1, 10, 16),
+    "resnet": lambda: PM.resnet_cifar(8, (16, 32, 64), 10, 16),
+    "wide_resnet": lambda: PM.wide_resnet(10, 1, 10, 16),
+    "bottleneck": lambda: PM.resnet_bottleneck((1, 1), (16, 32), 10, 32),
+    "squeezenet": lambda: PM.squeezenet(10, 24),
+    "tiny": lambda: PM.tiny_cnn(10, 16),
+}
+
+
+@pytest.mark.parametrize("unfused", [False, True])
+@pytest.mark.parametrize("net", sorted(NETS))
+@pytest.mark.parametrize("dtype", [lpp.FP32, lpp.BF16])
+def test_act8_keeps_the_forward_and_nearly_the_gradient(net, dtype, unfused):
+    """Rounding an activation to half a step, uniformly distributed, is a relative
+    error of amax / rms / 63.5 / sqrt(12) at most; amax of 32 values of
+    normal or ReLU'd activations is under 5 rms but for rare groups: 2.3% of an
+    activation's norm.  A layer's weight gradient takes that once; errors of the
+    norms' gradients add up below them (independent: by their squares), at most 8
+    of them here: 2.3% sqrt(9) = 7%.  A lost ReLU decision would cost
+    the square root of the share of values under half a step, 1%: 10% a layer."""
+    # (bf16 convs have channels in eights; fp32 takes the classifier of 10 as a per-pixel linear layer)
+    m = PM.squeezenet(16, 24) if net == "squeezenet" and dtype == lpp.BF16 else NETS[net]()
+    img, lab, x, tensors = inputs(m, 16, 8, True)
+    a = step(m, img, lab, x, 0, dtype, unfused=unfused)
+    b = step(m, img, lab, x, 0, dtype, unfused=unfused, act8=True, steps=3)
+    assert a[0] == b[0] and np.array_equal(a[1], b[1])
+    assert np.linalg.norm(a[2] - b[2]) <= 0.07 * np.linalg.norm(a[2])
+    for kind, lo, n in tensors:
+        d, r = a[2][lo:lo + n] - b[2][lo:lo + n], a[2][lo:lo + n]
+        if kind in ("conv_w", "linear_w", "rms_gamma"):
+            assert np.linalg.norm(d) <= 0.1 * np.linalg.norm(r), (kind, lo)
+    say(net, dtype, unfused, "workspace", a[3], "->", b[3],
+        "gradient off by", np.linalg.norm(a[2] - b[2]) / np.linalg.norm(a[2]))
+    # (the tiny net's two activations and their gradients are all in use while its second conv runs: nothing to share)
+    assert b[3] < a[3] or net == "tiny"
+
+
+def test_act8_first_hand():
+    """norm -> 1x1 conv -> pool -> linear: the conv's weight gradient is that of the
+    checkpoint of the norm's output, to the float32 sum's rounding."""
+    m = PM.Model("one", (3, 8, 8), 12)
+    t = m.conv(-1, 40, 3, bias=True)
+    t = m.conv(m.rmsnorm(t), 24, 1, 1, 0)
+    m.linear(m.gap(t), 12)
+    m.assign_blocks([1])
+    img, lab, x, tensors = inputs(m, 5, 9)
+    _, z, g = step(m, img, lab, x, act8=True)[:3]
+    with lpp.Context(m, K=1, batch=5) as ctx:
+        ctx.set_params(x)
+        ctx.step(0, torch.from_numpy(img).cuda(), torch.from_numpy(lab).cuda(), 0, 0.1)
+        y = torch.from_numpy(ctx.get_activation(0, 1, (40, 8, 8))).double()
+        dy = torch.from_numpy(ctx.get_activation_grad(0, 2, (24, 8, 8))).double()
+        plain = ctx.get_grad(0)
+    rows = y.permute(0, 2, 3, 1).reshape(-1, 40)
+    d = dy.permute(0, 2, 3, 1).reshape(-1, 24)
+    codes, s = R.pack(rows)
+    xv = R.values(codes, s, 40)
+    kind, lo, n = tensors[3]
+    assert kind == "conv_w" and n == 40 * 24
+    got = torch.from_numpy(g[lo:lo + n]).double().view(24, 40)
+    want, size = d.t() @ xv, d.abs().t() @ xv.abs()
+    assert ((got - want).abs() <= (rows.shape[0] + 64) * 2.0 ** -23 * size).all()
+    assert not np.array_equal(g[lo:lo + n], plain[lo:lo + n])
+
+
+@pytest.mark.parametrize("dtype", [lpp.FP32, lpp.BF16])
+def test_act8_graphs_and_launches_agree(dtype):
+    m = NETS["pre_norm"]()
+    img, lab, x, _ = inputs(m, 16, 10, True)
+    a = step(m, img, lab, x, 0, dtype, act8=True, graphs=False)
+    for steps in (1, 4):
+        b = step(m, img, lab, x, 0, dtype, act8=True, steps=steps)
+        assert np.array_equal(a[2], b[2]) and np.array_equal(a[1], b[1])
+
+
+def test_act8_workers_train():
+    """Four updaters of two replicas, lock-free: every block moves, the loss is
+    finite, and a worker's checkpoints are its own (a sequential rerun of one step
+    agrees with a context of one worker)."""
+    m = mini(blocks=[1, 1, 2, 2, 2])
+    img, lab, x, _ = inputs(m, 16, 11)
+    im, lb = torch.from_numpy(img).cuda(), torch.from_numpy(lab).cuda()
+    with lpp.Context(m, K=2, batch=16, mode=lpp.ASYNC, momentum=0.9, act8=True) as ctx:
+        ctx.set_params(x)
+        for _ in range(6):
+            for w in range(4):
+                ctx.step(w, im, lb, w % 2 + 1, 0.01)
+            ctx.average()
+        ctx.sync()
+        assert all(np.isfinite(ctx.get_loss(w)) for w in range(4))
+        p = ctx.get_params(1)
+        for b in (1, 2):
+            lo, hi = ctx.block_range(b)
+            assert (p[lo:hi] != x[lo:hi]).mean() > 0.5
+    with lpp.Context(m, K=2, batch=16, act8=True) as ctx:
+        ctx.set_params(x)
+        for w in (3, 0, 2):
+            ctx.step(w, im, lb, 0, 0.0)
+        one = step(m, img, lab, x, act8=True)
+        for w in (3, 0, 2):
+            assert np.array_equal(ctx.get_grad(w), one[2])
+
+
+def test_act8_holds_no_activations():
+    m = mini()
+    img, lab, x, _ = inputs(m, 4, 12)
+    with lpp.Context(m, K=1, batch=4, act8=True) as ctx:
+        ctx.set_params(x)
+        ctx.step(0, torch.from_numpy(img).cuda(), torch.from_numpy(lab).cuda(), 0, 0.1)
+        for f in (ctx.get_activation, ctx.get_activation_grad):
+            with pytest.raises(lpp.LppError) as e:
+                f(0, 1, m.shapes[1])
+            assert e.value.code == lpp.ESTATE
