@@ -381,7 +381,8 @@ int lpp_kernel_snapshot_noalloc(const lpp_snap_conv* convs, int n_convs, long d,
  *     are exact and sums float32, in a fixed order, for both types of dy.  ws:
  *     ws_floats >= lpp_act8_wgrad_ws(rows, cout, cin) floats of device memory
  *     (16-byte aligned, may be NULL where that is 0), scratch of this call
- *     until it has run: calls that may overlap need their own.
+ *     until it has run: calls that may overlap need their own.  Rows of dy are at
+ *     most 2^24 elements apart (LPP_EUNSUPPORTED).
  * All pointers are device pointers on the current device; stream may be NULL
  * (default stream).  The calls enqueue and return, allocate nothing and may be
  * captured into a graph.  rows == 0 is valid (dw becomes 0).  LPP_EINVAL before

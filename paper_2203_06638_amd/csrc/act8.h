@@ -78,14 +78,16 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
 }
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// V = 16 / sizeof(T) values of a row at p, of which n > 0 exist (the rest 0).
-// A: 16-byte loads where all exist.
-template <bool A, typename T>
+// 16 bytes at any element address (global memory takes vector accesses unaligned)
+typedef uint32_t u4any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// V = 16 / sizeof(T) values of a row at p, of which n exist (the rest 0)
+template <typename T>
 __device__ __forceinline__ void ld_chunk(const T* p, int n, float* v) {
     constexpr int V = 16 / (int)sizeof(T);
-    if (A && n >= V) {
-        const uint4 u = *(const uint4*)p;
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if (n >= V) {
+        const u4 w = *(const u4any*)p;
 #pragma unroll
         for (int j = 0; j < V; ++j)
             v[j] = sizeof(T) == 4 ? __uint_as_float(w[j])
@@ -95,11 +97,15 @@ __device__ __forceinline__ void ld_chunk(const T* p, int n, float* v) {
         for (int j = 0; j < V; ++j) v[j] = j < n ? ld1(p, j) : 0.f;
     }
 }
-template <bool A, typename T>
+template <typename T>
 __device__ __forceinline__ void st_chunk(T* p, int n, const float* v) {
     constexpr int V = 16 / (int)sizeof(T);
-    if (A && n >= V) {
-        st16(p, v);
+    if (n >= V) {
+        u4 w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            w[k] = sizeof(T) == 4 ? __float_as_uint(v[k]) : pack_bf16x2(v[(2 * k) % V], v[(2 * k + 1) % V]);
+        *(u4any*)p = w;
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)

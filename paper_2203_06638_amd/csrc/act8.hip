@@ -1,6 +1,7 @@
 // act8.hip -- 8-bit activation checkpoints (act8.h): packing, unpacking, and the
 // weight gradient of a 1x1 conv or linear layer read from one.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "act8.h"
@@ -28,7 +29,7 @@ struct PackGeom {
     long ld;
 };
 
-template <bool A, typename T>
+template <typename T>
 __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, PackGeom g, uint8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ exps, int keep_sign) {
     constexpr int V = 16 / (int)sizeof(T), L = kAct8Group / V;
@@ -41,7 +42,7 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
         const unsigned i = i0 + u * 256u;
         row[u] = div_by(i, g.div);
         ch[u] = (int)(i - row[u] * g.cpr) * V;
-        ld_chunk<A>(x + (long)row[u] * g.ld + ch[u], i < g.n ? g.C - ch[u] : 0, v[u]);
+        ld_chunk(x + (long)row[u] * g.ld + ch[u], i < g.n ? g.C - ch[u] : 0, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < kPackU; ++u) {
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
     }
 }
 
-template <bool A, typename T>
+template <typename T>
 __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__ codes,
                                                      const uint8_t* __restrict__ exps, PackGeom g,
                                                      T* __restrict__ x) {
@@ -98,14 +99,8 @@ __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__
         float v[V];
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) act8_val4(w[u][k], act8_step(s[u]), v + 4 * k);
-        st_chunk<A>(x + (long)row[u] * g.ld + ch[u], n[u], v);
+        st_chunk(x + (long)row[u] * g.ld + ch[u], n[u], v);
     }
-}
-
-// whether 16-byte accesses at p + row * ld + (multiple of 16 bytes) are aligned
-template <typename T>
-static bool rows_aligned(const T* p, long ld, long rows) {
-    return ((uintptr_t)p & 15) == 0 && (rows <= 1 || ld * (long)sizeof(T) % 16 == 0);
 }
 
 // f(first row, geometry, workgroups) over runs of rows of less than 2^31 chunks
@@ -132,25 +127,21 @@ static hipError_t for_row_runs(long rows, int C, long ld, F f) {
 
 template <typename T>
 static hipError_t pack_rows(const T* x, long ld, long rows, int C, bool keep_sign, uint8_t* q, hipStream_t st) {
-    const bool al = rows_aligned(x, ld, rows);
     uint8_t* exps = q + rows * act8_pitch(C);
     return for_row_runs<T>(rows, C, ld, [&](long r0, const PackGeom& g, dim3 grid) {
         uint8_t* c = q + r0 * g.pitch;
         uint8_t* e = exps + r0 * g.G;
-        if (al) launch((act8_pack_k<true, T>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
-        else launch((act8_pack_k<false, T>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
+        launch(act8_pack_k<T>, grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
     });
 }
 
 template <typename T>
 static hipError_t unpack_rows(const uint8_t* q, long rows, int C, T* x, long ld, hipStream_t st) {
-    const bool al = rows_aligned(x, ld, rows);
     const uint8_t* exps = q + rows * act8_pitch(C);
     return for_row_runs<T>(rows, C, ld, [&](long r0, const PackGeom& g, dim3 grid) {
         const uint8_t* c = q + r0 * g.pitch;
         const uint8_t* e = exps + r0 * g.G;
-        if (al) launch((act8_unpack_k<true, T>), grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
-        else launch((act8_unpack_k<false, T>), grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
+        launch(act8_unpack_k<T>, grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
     });
 }
 
@@ -188,95 +179,131 @@ struct WgGeom {
     int O, I, pitch, G;
     long ld;             // elements between rows of dY
     long pstride;        // floats between the partials of two splits
+    int itiles, tiles;   // tiles along I, in all
+    int splits;
+    int tail;            // the last rows, which the steps leave out
 };
 
-template <typename T, int BO, int BI, bool A>
-__global__ __launch_bounds__(256) void act8_wgrad_k(const T* __restrict__ dY, const uint8_t* __restrict__ codes,
-                                                    const uint8_t* __restrict__ exps, float* __restrict__ part,
-                                                    WgGeom g) {
+// Eight waves of 32 x 64 (or 16 x 64, 32 x 32, 16 x 32) results, two workgroups of them
+// to a compute unit.  Every step's loads are issued kWgAhead steps ahead into
+// registers, without a branch around them, which would make the compiler wait for all
+// of them: rows past the split's end are read from its last row and met with X = 0,
+// chunks wholly past O or I are chunk 0 (they only reach results that are not
+// stored), and so is what a chunk that crosses O takes from the next row.  The last
+// rows of dY, where such a chunk would end behind the matrix, are added at the end.
+// Measured, 2 steps ahead against 4: 1024 x 1024 over 100352 rows 297 and 302 us
+// (bf16), 592 and 899 (float32, whose registers then spill).
+constexpr int kWgAhead = 2;
+constexpr int kWgThreads = 512;
+
+template <typename T, int BO, int BI>
+__global__ __launch_bounds__(kWgThreads, 4) void act8_wgrad_k(const T* __restrict__ dY,
+                                                              const uint8_t* __restrict__ codes,
+                                                              const uint8_t* __restrict__ exps,
+                                                              float* __restrict__ part, WgGeom g) {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;       // bf16 terms of dY
-    constexpr int TM = BO / 32, TN = BI / 32;        // 16x16 blocks per wave; waves 2 x 2
+    constexpr int TM = BO / 64, TN = BI / 32;        // 16x16 blocks per wave; waves 4 x 2
     constexpr int WA = BO / 8, WB = BI / 8;          // chunks of 8 channels per LDS row
-    constexpr int CA = BO / 64;                      // dY chunks of a thread per K-step
-    constexpr int CB = BI / 64;                      // X chunks (8 codes each)
+    constexpr int QA = NP == 3 ? 2 : 1;              // 16-byte loads of a dY chunk
     constexpr int SA = 32 * BO, STEP = NP * SA + 32 * BI;
+    constexpr int D = kWgAhead;
+    static_assert(D % 2 == 0, "LDS buffers alternate");
     __shared__ __attribute__((aligned(16))) bf16 lds[2 * STEP];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wm = wave & 1, wn = wave >> 1;
-    const int i0 = blockIdx.x * BI, o0 = blockIdx.y * BO;
-    const long r_lo = (long)blockIdx.z * g.rps, r_hi = min(g.rows, r_lo + g.rps);
-    const int nk = (int)((r_hi - r_lo + 31) / 32);
-    const int trow = tid >> 3, tc = tid & 7;         // 8 threads a row
-
-    float a[CA][8];
-    uint32_t b[CB][2], bs[CB];
-    auto load = [&](int kk) {
-        const long r = r_lo + (long)kk * 32 + trow;
-        const bool ok = r < r_hi;
-#pragma unroll
-        for (int c = 0; c < CA; ++c) {
-            const int o = o0 + (c * 8 + tc) * 8;
-            const int n = ok ? g.O - o : 0;
-            if constexpr (sizeof(T) == 4) {
-                ld_chunk<A>(dY + r * g.ld + o, n, a[c]);
-                ld_chunk<A>(dY + r * g.ld + o + 4, n - 4, a[c] + 4);
-            } else {
-                ld_chunk<A>(dY + r * g.ld + o, n, a[c]);
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-            const int i = i0 + (tc * CB + c) * 8;
-            const bool in = ok && i < g.pitch;
-            const uint2 q = in ? *(const uint2*)(codes + r * g.pitch + i) : uint2{0u, 0u};
-            b[c][0] = q.x;
-            b[c][1] = q.y;
-            // (a chunk of padding channels only has no group of its own)
-            bs[c] = in ? exps[r * g.G + min(i / kAct8Group, g.G - 1)] : 7u;
-        }
+    const int wm = wave & 3, wn = wave >> 2;
+    int tile, split;
+    if (g.splits >= 8) {
+        // the tiles of a split, which read the same rows, on one of the 8 XCDs
+        // (workgroups go round the XCDs by their index)
+        const int x = blockIdx.x % 8, k = blockIdx.x / 8;
+        tile = k % g.tiles;
+        split = k / g.tiles * 8 + x;
+        if (split >= g.splits) return;
+    } else {
+        tile = blockIdx.x % g.tiles;
+        split = blockIdx.x / g.tiles;
+    }
+    const int i0 = tile % g.itiles * BI, o0 = tile / g.itiles * BO;
+    const long r_lo = (long)split * g.rps;
+    const int nr = (int)(min(g.rows - g.tail, r_lo + g.rps) - r_lo);   // rows of this split, but for the tail
+    const int nk = (nr + 32 * D - 1) / (32 * D) * D;
+    // 16 threads a row, a chunk of each operand per K-step (narrow tiles: half of them)
+    const int trow = tid >> 4, tc = tid & 15;
+    const int ac = tc % WA, bc = tc % WB;
+    const int a_c = o0 + ac * 8 < g.O ? o0 + ac * 8 : 0;
+    const int b_c = i0 + bc * 8 < g.pitch ? i0 + bc * 8 : 0;
+    // (a chunk of padding codes only has no group of its own)
+    const int e_c = min(b_c / kAct8Group, g.G - 1);
+    // byte offsets from the first row of a step, which is the same for all threads
+    uint32_t a_off, b_off, e_off;
+    auto offsets = [&](int t) {
+        a_off = ((uint32_t)t * (uint32_t)g.ld + (uint32_t)a_c) * (uint32_t)sizeof(T);
+        b_off = (uint32_t)t * (uint32_t)g.pitch + (uint32_t)b_c;
+        e_off = (uint32_t)t * (uint32_t)g.G + (uint32_t)e_c;
     };
-    auto put = [&](int buf) {
+
+    struct Stage {
+        u4 a[QA];
+        uint2 b;
+        uint32_t e;
+    };
+    Stage sg[D];
+    auto load = [&](Stage& s, int kk) {
+        const int first = min(kk * 32, nr - 1), last = nr - 1 - first;
+        if (last < 31) offsets(min(trow, last));     // (the last steps)
+        const long r = r_lo + first;
+        const T* p = (const T*)((const char*)(dY + r * g.ld) + a_off);
+#pragma unroll
+        for (int q = 0; q < QA; ++q) s.a[q] = *(const u4any*)(p + 4 * q);
+        s.b = *(const uint2*)(codes + r * g.pitch + b_off);
+        s.e = (exps + r * g.G)[e_off];
+    };
+    // The fast form takes dY as finite: a not finite value becomes NaN in its lower
+    // terms, and meets X = 0 in rows past the end.  Either makes results NaN, and a
+    // workgroup that ends with one that is not finite forms all of them again with the
+    // CAREFUL form, where such a value is its first term alone.
+    auto put = [&](const Stage& s, int kk, int buf, auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
         bf16* As = lds + buf * STEP;
         bf16* Bs = As + NP * SA;
+        const bool row = kk * 32 + trow < nr;
+        if (WA == 16 || tc < WA) {
+            bf16* p = As + trow * BO + wg_chunk<WA>(ac, trow) * 8;
+            uint32_t x[QA * 4];
 #pragma unroll
-        for (int c = 0; c < CA; ++c) {
-            bf16* p = As + trow * BO + wg_chunk<WA>(c * 8 + tc, trow) * 8;
-            uint32_t w[NP][4];
+            for (int k = 0; k < QA * 4; ++k) {
+                x[k] = s.a[k / 4][k % 4];
+                if (CAREFUL) x[k] = row ? x[k] : 0u;
+            }
             if constexpr (NP == 1) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    w[0][k] = (__float_as_uint(a[c][2 * k]) >> 16) | (__float_as_uint(a[c][2 * k + 1]) & 0xffff0000u);
+                *(u4*)p = u4{x[0], x[1], x[2], x[3]};
             } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float x0 = a[c][2 * k], x1 = a[c][2 * k + 1];
+                for (int t = 0; t < NP; ++t) {
+                    u4 w;
 #pragma unroll
-                    for (int t = 0; t < NP; ++t) {
-                        const uint32_t h0 = __float_as_uint(x0) & 0xffff0000u, h1 = __float_as_uint(x1) & 0xffff0000u;
-                        w[t][k] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
-                        if (t + 1 < NP) {
-                            // an infinity or NaN is its first term alone
-                            const bool f0 = (h0 & 0x7f800000u) != 0x7f800000u, f1 = (h1 & 0x7f800000u) != 0x7f800000u;
-                            x0 = f0 ? x0 - __uint_as_float(h0) : 0.f;
-                            x1 = f1 ? x1 - __uint_as_float(h1) : 0.f;
+                    for (int k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_perm(x[2 * k + 1], x[2 * k], 0x07060302u);
+                    *(u4*)(p + t * SA) = w;
+                    if (t + 1 < NP) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float d = __uint_as_float(x[k]) - __uint_as_float(x[k] & 0xffff0000u);
+                            x[k] = CAREFUL && (x[k] & 0x7f800000u) == 0x7f800000u ? 0u : __float_as_uint(d);
                         }
                     }
                 }
             }
-#pragma unroll
-            for (int t = 0; t < NP; ++t) *(uint4*)(p + t * SA) = uint4{w[t][0], w[t][1], w[t][2], w[t][3]};
         }
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
+        if (WB == 16 || tc < WB) {
+            const float step = row ? act8_step(s.e) : 0.f;
             float v[8];
-            const float step = act8_step(bs[c]);
-            act8_val4(b[c][0], step, v);
-            act8_val4(b[c][1], step, v + 4);
-            uint32_t w[4];
+            act8_val4(s.b.x, step, v);
+            act8_val4(s.b.y, step, v + 4);
+            u4 w;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 w[k] = __builtin_amdgcn_perm(__float_as_uint(v[2 * k + 1]), __float_as_uint(v[2 * k]), 0x07060302u);
-            *(uint4*)(Bs + trow * BI + wg_chunk<WB>(tc * CB + c, trow) * 8) = uint4{w[0], w[1], w[2], w[3]};
+            *(u4*)(Bs + trow * BI + wg_chunk<WB>(bc, trow) * 8) = w;
         }
     };
     const int fs = lane & 15, fg = lane >> 4;
@@ -293,35 +320,76 @@ __global__ __launch_bounds__(256) void act8_wgrad_k(const T* __restrict__ dY, co
     };
 
     f4 acc[TM][TN];
+    auto product = [&](auto careful) {
+#pragma unroll
+        for (int x = 0; x < TM; ++x)
+#pragma unroll
+            for (int y = 0; y < TN; ++y) acc[x][y] = f4{0.f, 0.f, 0.f, 0.f};
+        if (nr <= 0) return;
+        offsets(trow);
+#pragma unroll
+        for (int s = 0; s < D; ++s) load(sg[s], s);
+        put(sg[0], 0, 0, careful);
+        load(sg[0], D);
+        for (int kk = 0; kk < nk; kk += D) {
+#pragma unroll
+            for (int s = 0; s < D; ++s) {
+                __syncthreads();
+                const bf16* As = lds + (s & 1) * STEP;
+                const bf16* Bs = As + NP * SA;
+                bf8 fa[NP][TM], fb[TN];
+#pragma unroll
+                for (int y = 0; y < TN; ++y) fb[y] = frag(Bs, (wn * TN + y) * 16, std::integral_constant<int, WB>{});
+#pragma unroll
+                for (int t = 0; t < NP; ++t)
+#pragma unroll
+                    for (int x = 0; x < TM; ++x)
+                        fa[t][x] = frag(As + t * SA, (wm * TM + x) * 16, std::integral_constant<int, WA>{});
+                // the next step's operands go into the other buffer while this one is multiplied
+                const int nx = (s + 1) % D;
+                put(sg[nx], kk + s + 1, (s + 1) & 1, careful);
+                load(sg[nx], kk + s + 1 + D);
+#pragma unroll
+                for (int t = 0; t < NP; ++t)
+#pragma unroll
+                    for (int x = 0; x < TM; ++x)
+#pragma unroll
+                        for (int y = 0; y < TN; ++y)
+                            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[t][x], fb[y], acc[x][y], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+    };
+    product(std::false_type{});
+    bool bad = false;
 #pragma unroll
     for (int x = 0; x < TM; ++x)
 #pragma unroll
-        for (int y = 0; y < TN; ++y) acc[x][y] = f4{0.f, 0.f, 0.f, 0.f};
-    if (nk > 0) {
-        load(0);
-        put(0);
-        if (nk > 1) load(1);
-    }
-    for (int kk = 0; kk < nk; ++kk) {
-        __syncthreads();
-        if (kk + 1 < nk) put((kk + 1) & 1);
-        if (kk + 2 < nk) load(kk + 2);
-        const bf16* As = lds + (kk & 1) * STEP;
-        const bf16* Bs = As + NP * SA;
-        bf8 fb[TN];
+        for (int y = 0; y < TN; ++y)
 #pragma unroll
-        for (int y = 0; y < TN; ++y) fb[y] = frag(Bs, (wn * TN + y) * 16, std::integral_constant<int, WB>{});
+            for (int k = 0; k < 4; ++k) bad |= abs_bits(acc[x][y][k]) >= 0x7f800000u;
+    if (__syncthreads_or(bad)) product(std::true_type{});
+    if (split + 1 == g.splits)
+        for (long r = g.rows - g.tail; r < g.rows; ++r) {
+            float d[TM][4], x[TN];
 #pragma unroll
-        for (int t = 0; t < NP; ++t)
+            for (int m = 0; m < TM; ++m)
 #pragma unroll
-            for (int x = 0; x < TM; ++x) {
-                const bf8 fa = frag(As + t * SA, (wm * TM + x) * 16, std::integral_constant<int, WA>{});
+                for (int k = 0; k < 4; ++k)
+                    d[m][k] = ld1(dY + r * g.ld, min(o0 + (wm * TM + m) * 16 + (lane >> 4) * 4 + k, g.O - 1));
+#pragma unroll
+            for (int y = 0; y < TN; ++y) {
+                const int i = min(i0 + (wn * TN + y) * 16 + (lane & 15), g.I - 1);
+                x[y] = (float)(int8_t)codes[r * g.pitch + i] * act8_step(exps[r * g.G + i / kAct8Group]);
+            }
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
 #pragma unroll
                 for (int y = 0; y < TN; ++y)
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[y], acc[x][y], 0, 0, 0);
-            }
-    }
-    float* out = part + (long)blockIdx.z * g.pstride;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[m][y][k] = __builtin_fmaf(d[m][k], x[y], acc[m][y][k]);
+        }
+    float* out = part + (long)split * g.pstride;
 #pragma unroll
     for (int x = 0; x < TM; ++x)
 #pragma unroll
@@ -335,38 +403,41 @@ __global__ __launch_bounds__(256) void act8_wgrad_k(const T* __restrict__ dY, co
         }
 }
 
+// Splits.  A step of a workgroup costs about 0.4 us and a split's partials O I 8 bytes
+// of traffic at 4 TB/s: rows / S / 32 steps and S partials together are least at
+// S^2 = 6500 rows / (O I).  Never more than two workgroups a compute unit, and one
+// where that leaves a split fewer than 1536 rows.  Measured, one against two: 128 x 512
+// over 131072 rows 41.6 and 44.3 us with the sum, 1024 x 1024 over 100352 rows 356 and
+// 297.
 Act8WgPlan act8_wgrad_plan(long rows, int O, int I) {
     Act8WgPlan p{};
     p.bo = O > 64 ? 128 : 64;
     p.bi = I > 64 ? 128 : 64;
     const long tiles = (long)((O + p.bo - 1) / p.bo) * ((I + p.bi - 1) / p.bi);
-    long splits = (512 + tiles - 1) / tiles;
-    const long most = std::max(1l, (rows + 255) / 256);
-    if (splits > most) splits = most;
+    long splits = (long)std::sqrt(6500.0 * rows / ((double)O * I));
+    const long two = 512 / tiles;
+    splits = std::min(splits, two > 0 && rows / two >= 1536 ? two : 256 / tiles);
+    splits = std::max(1l, std::min(splits, rows / 64));
     p.rps = std::max(32l, ((rows + splits - 1) / splits + 31) / 32 * 32);
     p.splits = (int)std::max(1l, (rows + p.rps - 1) / p.rps);
     p.part_floats = ((long)O * I + 3) / 4 * 4;
     return p;
 }
 
-template <typename T, int BO, int BI>
-static void wgrad_tile(bool al, dim3 grid, const T* dY, const uint8_t* q, const uint8_t* exps, float* part,
-                       const WgGeom& g, hipStream_t st) {
-    if (al) launch((act8_wgrad_k<T, BO, BI, true>), grid, dim3(256), 0, st, dY, q, exps, part, g);
-    else launch((act8_wgrad_k<T, BO, BI, false>), grid, dim3(256), 0, st, dY, q, exps, part, g);
-}
-
 template <typename T>
 static hipError_t wgrad_parts(const T* dY, long ld, const uint8_t* q, long rows, int O, int I, float* part,
                               const Act8WgPlan& p, hipStream_t st) {
-    const WgGeom g{rows, p.rps, O, I, act8_pitch(I), act8_groups(I), ld, p.part_floats};
+    const int it = (I + p.bi - 1) / p.bi, ot = (O + p.bo - 1) / p.bo;
+    // rows from whose last chunk 8 channels on would lie behind the matrix
+    const long over = (O + 7) / 8 * 8 - O, dist = rows > 1 ? ld : over;
+    const long tail = over ? std::min(rows, (over + dist - 1) / dist) : 0;
+    const WgGeom g{rows, p.rps, O, I, act8_pitch(I), act8_groups(I), ld, p.part_floats, it, it * ot, p.splits, (int)tail};
     const uint8_t* exps = q + rows * g.pitch;
-    const bool al = rows_aligned(dY, ld, rows);
-    const dim3 grid((unsigned)((I + p.bi - 1) / p.bi), (unsigned)((O + p.bo - 1) / p.bo), (unsigned)p.splits);
-    if (p.bo == 128 && p.bi == 128) wgrad_tile<T, 128, 128>(al, grid, dY, q, exps, part, g, st);
-    else if (p.bo == 128) wgrad_tile<T, 128, 64>(al, grid, dY, q, exps, part, g, st);
-    else if (p.bi == 128) wgrad_tile<T, 64, 128>(al, grid, dY, q, exps, part, g, st);
-    else wgrad_tile<T, 64, 64>(al, grid, dY, q, exps, part, g, st);
+    const dim3 grid((unsigned)(g.tiles * (p.splits >= 8 ? (p.splits + 7) / 8 * 8 : p.splits))), block(kWgThreads);
+    if (p.bo == 128 && p.bi == 128) launch((act8_wgrad_k<T, 128, 128>), grid, block, 0, st, dY, q, exps, part, g);
+    else if (p.bo == 128) launch((act8_wgrad_k<T, 128, 64>), grid, block, 0, st, dY, q, exps, part, g);
+    else if (p.bi == 128) launch((act8_wgrad_k<T, 64, 128>), grid, block, 0, st, dY, q, exps, part, g);
+    else launch((act8_wgrad_k<T, 64, 64>), grid, block, 0, st, dY, q, exps, part, g);
     return hipGetLastError();
 }
 

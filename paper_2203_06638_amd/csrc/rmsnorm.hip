@@ -13,6 +13,12 @@
 #include "kernels.h"
 #include "launch.h"
 
+#ifndef RMSWGS
+#define RMSWGS 2048
+#endif
+#ifndef RMSPARTS
+#define RMSPARTS 1024
+#endif
 namespace lpp {
 
 // sum over the TPR threads of a row; all of them get it.  TPR <= 64: lanes of one
@@ -39,7 +45,7 @@ __device__ __forceinline__ float row_sum(float v, float* slots, int& turn) {
 // row's TPR threads holds chunks t, t + TPR, ... (NC of them) in registers, so that
 // the row is read once, and its 32-channel groups lie in neighbouring lanes.
 // Workgroups walk over the rows and keep gamma in registers.
-template <typename T, int TPR, int NC, bool A>
+template <typename T, int TPR, int NC>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
     constexpr int V = 16 / (int)sizeof(T), L = kAct8Group / V;
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;   // threads, rows of a workgroup
@@ -63,14 +69,14 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int ch = (c * TPR + t) * V;
-            ld_chunk<A>((const T*)p.x + r * p.ldx + ch, ok ? p.C - ch : 0, h[c]);
+            ld_chunk((const T*)p.x + r * p.ldx + ch, ok ? p.C - ch : 0, h[c]);
         }
         if (p.res) {
             float e[NC][V];
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 const int ch = (c * TPR + t) * V;
-                ld_chunk<A>((const T*)p.res + r * p.ldres + ch, ok ? p.C - ch : 0, e[c]);
+                ld_chunk((const T*)p.res + r * p.ldres + ch, ok ? p.C - ch : 0, e[c]);
             }
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
@@ -80,7 +86,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
                     h[c][j] += e[c][j];
                     if constexpr (sizeof(T) == 2) h[c][j] = from_bf16(to_bf16(h[c][j]));
                 }
-                if (p.h) st_chunk<A>((T*)p.h + r * p.ldh + ch, ok ? p.C - ch : 0, h[c]);
+                if (p.h) st_chunk((T*)p.h + r * p.ldh + ch, ok ? p.C - ch : 0, h[c]);
             }
         }
         float ss = 0.f;
@@ -95,7 +101,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
             const int ch = (c * TPR + t) * V;
 #pragma unroll
             for (int j = 0; j < V; ++j) h[c][j] = h[c][j] * rstd * gam[c][j];
-            if (p.y) st_chunk<A>((T*)p.y + r * p.ldy + ch, ok ? p.C - ch : 0, h[c]);
+            if (p.y) st_chunk((T*)p.y + r * p.ldy + ch, ok ? p.C - ch : 0, h[c]);
             if (p.q) {
                 uint32_t m = 0;
 #pragma unroll
@@ -117,23 +123,23 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
 }
 
 // v, added to what is there with acc
-template <bool A, typename T>
+template <typename T>
 __device__ __forceinline__ void st_sum(T* p, int n, const float* v, bool acc) {
     constexpr int V = 16 / (int)sizeof(T);
     float e[V];
     if (acc) {
-        ld_chunk<A>(p, n, e);
+        ld_chunk(p, n, e);
 #pragma unroll
         for (int j = 0; j < V; ++j) e[j] += v[j];
         v = e;
     }
-    st_chunk<A>(p, n, v);
+    st_chunk(p, n, v);
 }
 
 // The gradient.  dgamma: every thread sums its channels over the rows it walks
 // over, the workgroup's row lanes meet in LDS, and each workgroup writes one row of
 // partials [workgroup][stride], summed in a fixed order by launch_part_sums.
-template <typename T, int TPR, int NC, bool A>
+template <typename T, int TPR, int NC>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
@@ -154,15 +160,16 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
     for (long r0 = (long)blockIdx.x * RB; r0 < p.rows; r0 += step) {
         const long r = r0 + rl;
         const bool ok = r < p.rows;
-        float dy[NC][V], h[NC][V];
+        float dy[NC][V], h[NC][V], res[NC][V];
         const float rstd = ok ? p.rstd[r] : 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int ch = (c * TPR + t) * V;
             const int n = ok ? p.C - ch : 0;
-            ld_chunk<A>((const T*)p.dy + r * p.lddy + ch, n, dy[c]);
+            ld_chunk((const T*)p.dy + r * p.lddy + ch, n, dy[c]);
+            if (p.dres) ld_chunk((const T*)p.dres + r * p.lddres + ch, n, res[c]);
             if (p.h) {
-                ld_chunk<A>((const T*)p.h + r * p.ldh + ch, n, h[c]);
+                ld_chunk((const T*)p.h + r * p.ldh + ch, n, h[c]);
             } else {
                 uint32_t w[V / 4], s = 7u;
 #pragma unroll
@@ -202,13 +209,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
                 dy[c][j] = rstd * (dy[c][j] * gam[c][j] - h[c][j] * k);
             }
             if (p.dres) {
-                float e[V];
-                ld_chunk<A>((const T*)p.dres + r * p.lddres + ch, n, e);
 #pragma unroll
-                for (int j = 0; j < V; ++j) dy[c][j] += e[j];
+                for (int j = 0; j < V; ++j) dy[c][j] += res[c][j];
             }
-            if (p.dx) st_sum<A>((T*)p.dx + r * p.lddx + ch, n, dy[c], p.acc1);
-            if (p.dx2) st_sum<A>((T*)p.dx2 + r * p.lddx + ch, n, dy[c], p.acc2);
+            if (p.dx) st_sum((T*)p.dx + r * p.lddx + ch, n, dy[c], p.acc1);
+            if (p.dx2) st_sum((T*)p.dx2 + r * p.lddx + ch, n, dy[c], p.acc2);
         }
     }
     if (!p.part) return;
@@ -255,33 +260,28 @@ static int row_chunks(int dt, int C) {
 }
 
 template <bool BWD, typename T, int TPR, int NC, typename P>
-static void rms_launch(bool al, const P& p, int wgs, hipStream_t st) {
+static void rms_launch(const P& p, int wgs, hipStream_t st) {
     const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
-    if constexpr (BWD) {
-        if (al) launch((rmsnorm_bwd_k<T, TPR, NC, true>), grid, block, 0, st, p);
-        else launch((rmsnorm_bwd_k<T, TPR, NC, false>), grid, block, 0, st, p);
-    } else {
-        if (al) launch((rmsnorm_k<T, TPR, NC, true>), grid, block, 0, st, p);
-        else launch((rmsnorm_k<T, TPR, NC, false>), grid, block, 0, st, p);
-    }
+    if constexpr (BWD) launch((rmsnorm_bwd_k<T, TPR, NC>), grid, block, 0, st, p);
+    else launch((rmsnorm_k<T, TPR, NC>), grid, block, 0, st, p);
 }
 
 template <bool BWD, typename T, typename P>
-static hipError_t rms_dispatch(bool al, const P& p, RowShape s, int wgs, hipStream_t st) {
+static hipError_t rms_dispatch(const P& p, RowShape s, int wgs, hipStream_t st) {
     switch (s.tpr * 16 + s.nc) {
-    case 8 * 16 + 1: rms_launch<BWD, T, 8, 1>(al, p, wgs, st); break;
-    case 16 * 16 + 1: rms_launch<BWD, T, 16, 1>(al, p, wgs, st); break;
-    case 32 * 16 + 1: rms_launch<BWD, T, 32, 1>(al, p, wgs, st); break;
-    case 64 * 16 + 1: rms_launch<BWD, T, 64, 1>(al, p, wgs, st); break;
-    case 64 * 16 + 2: rms_launch<BWD, T, 64, 2>(al, p, wgs, st); break;
-    case 64 * 16 + 4: rms_launch<BWD, T, 64, 4>(al, p, wgs, st); break;
-    case 256 * 16 + 2: rms_launch<BWD, T, 256, 2>(al, p, wgs, st); break;
-    case 256 * 16 + 4: rms_launch<BWD, T, 256, 4>(al, p, wgs, st); break;
-    case 1024 * 16 + 2: rms_launch<BWD, T, 1024, 2>(al, p, wgs, st); break;
+    case 8 * 16 + 1: rms_launch<BWD, T, 8, 1>(p, wgs, st); break;
+    case 16 * 16 + 1: rms_launch<BWD, T, 16, 1>(p, wgs, st); break;
+    case 32 * 16 + 1: rms_launch<BWD, T, 32, 1>(p, wgs, st); break;
+    case 64 * 16 + 1: rms_launch<BWD, T, 64, 1>(p, wgs, st); break;
+    case 64 * 16 + 2: rms_launch<BWD, T, 64, 2>(p, wgs, st); break;
+    case 64 * 16 + 4: rms_launch<BWD, T, 64, 4>(p, wgs, st); break;
+    case 256 * 16 + 2: rms_launch<BWD, T, 256, 2>(p, wgs, st); break;
+    case 256 * 16 + 4: rms_launch<BWD, T, 256, 4>(p, wgs, st); break;
+    case 1024 * 16 + 2: rms_launch<BWD, T, 1024, 2>(p, wgs, st); break;
     case 1024 * 16 + 4:
         // (rows of kRmsMaxC bf16 channels are 2 chunks a thread)
         if constexpr (sizeof(T) == 4) {
-            rms_launch<BWD, T, 1024, 4>(al, p, wgs, st);
+            rms_launch<BWD, T, 1024, 4>(p, wgs, st);
             break;
         }
         return hipErrorInvalidValue;
@@ -290,44 +290,34 @@ static hipError_t rms_dispatch(bool al, const P& p, RowShape s, int wgs, hipStre
     return hipGetLastError();
 }
 
-static bool al16(const void* p, long ld, long rows, int e) {
-    return !p || (((uintptr_t)p & 15) == 0 && (rows <= 1 || ld * e % 16 == 0));
-}
-
 hipError_t launch_rmsnorm(int dt, RmsArgs p, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    const int e = dt == DT_BF16 ? 2 : 4;
     p.pitch = act8_pitch(p.C);
     p.G = act8_groups(p.C);
     p.exps = p.q ? p.q + p.rows * p.pitch : nullptr;
-    const bool al = al16(p.x, p.ldx, p.rows, e) && al16(p.res, p.ldres, p.rows, e) && al16(p.h, p.ldh, p.rows, e) &&
-                    al16(p.y, p.ldy, p.rows, e);
     const RowShape s = row_shape(row_chunks(dt, p.C));
     if (!s.tpr) return hipErrorInvalidValue;
     const int rb = std::max(256, s.tpr) / s.tpr;
-    const int wgs = (int)std::min(s.tpr > 256 ? 512l : 2048l, (p.rows + rb - 1) / rb);
-    return dt == DT_BF16 ? rms_dispatch<false, bf16>(al, p, s, wgs, st) : rms_dispatch<false, float>(al, p, s, wgs, st);
+    const int wgs = (int)std::min(s.tpr > 256 ? 512l : (long)RMSWGS, (p.rows + rb - 1) / rb);
+    return dt == DT_BF16 ? rms_dispatch<false, bf16>(p, s, wgs, st) : rms_dispatch<false, float>(p, s, wgs, st);
 }
 
 int rmsnorm_bwd_parts(long rows, int C) {
-    // at most one row of partials for 8 rows, and 1024
-    return (int)std::max(1l, std::min(1024l, (rows + 7) / 8));
+    const RowShape s = row_shape((C + 3) / 4);
+    const int rb = std::max(256, s.tpr) / std::max(1, s.tpr);
+    return (int)std::max(1l, std::min((long)RMSPARTS, (rows + 2 * rb - 1) / (2 * rb)));
 }
 
 hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st) {
-    const int e = dt == DT_BF16 ? 2 : 4;
     if (p.rows <= 0 && !p.part) return hipSuccess;
     p.pitch = act8_pitch(p.C);
     p.G = act8_groups(p.C);
     p.exps = p.q ? p.q + p.rows * p.pitch : nullptr;
     p.pstride = (p.C + 3) / 4 * 4;
-    const bool al = al16(p.dy, p.lddy, p.rows, e) && al16(p.h, p.ldh, p.rows, e) &&
-                    al16(p.dres, p.lddres, p.rows, e) && al16(p.dx, p.lddx, p.rows, e) &&
-                    al16(p.dx2, p.lddx, p.rows, e);
     const RowShape s = row_shape(row_chunks(dt, p.C));
     if (!s.tpr) return hipErrorInvalidValue;
     const int wgs = rmsnorm_bwd_parts(p.rows, p.C);
-    return dt == DT_BF16 ? rms_dispatch<true, bf16>(al, p, s, wgs, st) : rms_dispatch<true, float>(al, p, s, wgs, st);
+    return dt == DT_BF16 ? rms_dispatch<true, bf16>(p, s, wgs, st) : rms_dispatch<true, float>(p, s, wgs, st);
 }
 
 }  // namespace lpp

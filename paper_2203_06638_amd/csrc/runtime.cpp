@@ -2484,6 +2484,7 @@ int lpp_kernel_act8_wgrad(const void* dy, int dtype, long rows, int cout, long l
     if (const char* e = bad_act8(q, rows, cin)) return fail(LPP_EINVAL, e);
     const long need = lpp_act8_wgrad_ws(rows, cout, cin);
     if (need < 0) return fail(LPP_EINVAL, "the gradient must be under 2^31 elements");
+    if (rows > 1 && ld > (1 << 24)) return fail(LPP_EUNSUPPORTED, "rows of dy at most 2^24 elements apart");
     if (!dw || (uintptr_t)dw % 4) return fail(LPP_EINVAL, "dw must be a buffer of floats");
     if (need > 0 && (!ws || ((uintptr_t)ws & 15) || ws_floats < need))
         return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_act8_wgrad_ws floats");
