@@ -26,6 +26,7 @@ struct PackGeom {
     unsigned cpr;      // chunks per row, whole groups
     FastDiv div;       // by cpr
     int C, pitch, G;
+    unsigned exact;    // first of the rows whose last chunk must not be read past its values
     long ld;
 };
 
@@ -35,27 +36,29 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
     constexpr int V = 16 / (int)sizeof(T), L = kAct8Group / V;
     const unsigned i0 = blockIdx.x * (256u * kPackU) + threadIdx.x;
     unsigned row[kPackU];
-    int ch[kPackU];
-    float v[kPackU][V];
+    int ch[kPackU], n[kPackU];
+    u4 w[kPackU];
 #pragma unroll
     for (int u = 0; u < kPackU; ++u) {
-        const unsigned i = i0 + u * 256u;
+        const unsigned i = min(i0 + u * 256u, g.n - 1);
         row[u] = div_by(i, g.div);
         ch[u] = (int)(i - row[u] * g.cpr) * V;
-        ld_chunk(x + (long)row[u] * g.ld + ch[u], i < g.n ? g.C - ch[u] : 0, v[u]);
+        n[u] = g.C - ch[u];
+        w[u] = ld_chunk(x + (long)row[u] * g.ld + (n[u] > 0 ? ch[u] : 0), n[u], row[u] >= g.exact);
     }
 #pragma unroll
     for (int u = 0; u < kPackU; ++u) {
-        const unsigned i = i0 + u * 256u;
+        float v[V];
+        chunk_values<T>(chunk_mask<T>(w[u], n[u]), v);
         uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < V; ++j) m = max(m, abs_bits(v[u][j]));
+        for (int j = 0; j < V; ++j) m = max(m, abs_bits(v[j]));
         const uint32_t s = act8_exp(group_max<L>(m));
         uint32_t w[V / 4];
 #pragma unroll
         for (int k = 0; k < V / 4; ++k)
-            w[k] = s == 255u ? 0u : act8_code4(v[u] + 4 * k, act8_inv(s), keep_sign != 0);
-        if (i >= g.n) continue;
+            w[k] = s == 255u ? 0u : act8_code4(v + 4 * k, act8_inv(s), keep_sign != 0);
+        if (i0 + u * 256u >= g.n) continue;
         if (ch[u] < g.pitch) {
             uint8_t* p = codes + (long)row[u] * g.pitch + ch[u];
             if constexpr (V == 8) *(uint2*)p = uint2{w[0], w[1]};
@@ -65,7 +68,7 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
     }
 }
 
-template <typename T>
+template <typename T, bool ST>
 __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__ codes,
                                                      const uint8_t* __restrict__ exps, PackGeom g,
                                                      T* __restrict__ x) {
@@ -76,22 +79,20 @@ __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__
     uint32_t s[kPackU], w[kPackU][V / 4];
 #pragma unroll
     for (int u = 0; u < kPackU; ++u) {
-        const unsigned i = i0 + u * 256u;
+        const unsigned i = min(i0 + u * 256u, g.n - 1);
         row[u] = div_by(i, g.div);
         ch[u] = (int)(i - row[u] * g.cpr) * V;
-        n[u] = i < g.n ? g.C - ch[u] : 0;
-        s[u] = 7u;
-        if (n[u] > 0) {
-            const uint8_t* p = codes + (long)row[u] * g.pitch + ch[u];
-            if constexpr (V == 8) {
-                const uint2 q = *(const uint2*)p;
-                w[u][0] = q.x;
-                w[u][1] = q.y;
-            } else {
-                w[u][0] = *(const uint32_t*)p;
-            }
-            s[u] = exps[(long)row[u] * g.G + ch[u] / kAct8Group];
+        n[u] = i0 + u * 256u < g.n ? g.C - ch[u] : 0;
+        const int c = ch[u] < g.pitch ? ch[u] : 0;
+        const uint8_t* p = codes + (long)row[u] * g.pitch + c;
+        if constexpr (V == 8) {
+            const uint2 q = *(const uint2*)p;
+            w[u][0] = q.x;
+            w[u][1] = q.y;
+        } else {
+            w[u][0] = *(const uint32_t*)p;
         }
+        s[u] = exps[(long)row[u] * g.G + min(c / kAct8Group, g.G - 1)];
     }
 #pragma unroll
     for (int u = 0; u < kPackU; ++u) {
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__
         float v[V];
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) act8_val4(w[u][k], act8_step(s[u]), v + 4 * k);
-        st_chunk(x + (long)row[u] * g.ld + ch[u], n[u], v);
+        st_chunk<ST>(x + (long)row[u] * g.ld + ch[u], n[u], v);
     }
 }
 
@@ -117,7 +118,9 @@ static hipError_t for_row_runs(long rows, int C, long ld, F f) {
     // (the threads behind the last chunk divide their index too)
     const long run = ((1l << 31) - 256 * kPackU) / g.cpr;
     for (long r0 = 0; r0 < rows; r0 += run) {
-        g.n = (unsigned)(std::min(run, rows - r0) * g.cpr);
+        const long left = std::min(run, rows - r0);
+        g.n = (unsigned)(left * g.cpr);
+        g.exact = (unsigned)std::clamp(rows - tail_rows<T>(rows, C, ld) - r0, 0l, left);
         f(r0, g, dim3((g.n + 256 * kPackU - 1) / (256 * kPackU)));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -141,7 +144,10 @@ static hipError_t unpack_rows(const uint8_t* q, long rows, int C, T* x, long ld,
     return for_row_runs<T>(rows, C, ld, [&](long r0, const PackGeom& g, dim3 grid) {
         const uint8_t* c = q + r0 * g.pitch;
         const uint8_t* e = exps + r0 * g.G;
-        launch(act8_unpack_k<T>, grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
+        if (rows * C * (long)sizeof(T) >= kStreamBytes)
+            launch((act8_unpack_k<T, true>), grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
+        else
+            launch((act8_unpack_k<T, false>), grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
     });
 }
 
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(kWgThreads, 4) void act8_wgrad_k(const T* __restric
 
 // Splits.  A step of a workgroup costs about 0.4 us and a split's partials O I 8 bytes
 // of traffic at 4 TB/s: rows / S / 32 steps and S partials together are least at
-// S^2 = 6500 rows / (O I).  Never more than two workgroups a compute unit, and one
+// S^2 = 6500 rows / (O I) (half or twice that: within 5%).  Never more than two workgroups a compute unit, and one
 // where that leaves a split fewer than 1536 rows.  Measured, one against two: 128 x 512
 // over 131072 rows 41.6 and 44.3 us with the sum, 1024 x 1024 over 100352 rows 356 and
 // 297.

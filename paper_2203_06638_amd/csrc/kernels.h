@@ -432,6 +432,7 @@ struct RmsArgs {
 
     uint8_t* exps;
     int pitch, G;
+    long exact;
 };
 hipError_t launch_rmsnorm(int dt, RmsArgs p, hipStream_t st);
 // h (type dt) or, where it is null, its checkpoint q.  dx, dx2 (same row distance; null:
@@ -452,7 +453,7 @@ struct RmsBwdArgs {
 
     const uint8_t* exps;
     int pitch, G;
-    long pstride;
+    long exact, pstride;
 };
 int rmsnorm_bwd_parts(long rows, int C);
 hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st);
