@@ -28,6 +28,11 @@ __device__ __forceinline__ f4 ld4(const bf16* p, long q) {
     return f4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
               __uint_as_float(u.y & 0xffff0000u)};
 }
+// (the codes of an 8-bit checkpoint, act8.h: their signs are the values')
+__device__ __forceinline__ f4 ld4(const int8_t* p, long q) {
+    const uint32_t u = ((const uint32_t*)p)[q];
+    return f4{(float)(int8_t)u, (float)(int8_t)(u >> 8), (float)(int8_t)(u >> 16), (float)(int8_t)(u >> 24)};
+}
 __device__ __forceinline__ void st4(float* p, long q, f4 v) { ((f4*)p)[q] = v; }
 __device__ __forceinline__ void st4(bf16* p, long q, f4 v) {
     ((uint2*)p)[q] = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};

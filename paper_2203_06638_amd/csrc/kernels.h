@@ -281,13 +281,17 @@ hipError_t launch_head_bwd_x(int dt, const float* dz, const float* W, int Nb, in
 
 // elementwise (n multiple of 4)
 hipError_t launch_relu_fwd(int dt, const void* x, void* y, long n, hipStream_t st);
-hipError_t launch_relu_bwd(int dt, const void* dy, const void* x, void* dx, long n, bool accumulate, hipStream_t st);
+// (codes: x, or a ReLU's output y in its place, as the codes of an 8-bit checkpoint
+// without padding between rows; x / y is not read then)
+hipError_t launch_relu_bwd(int dt, const void* dy, const void* x, void* dx, long n, bool accumulate, hipStream_t st,
+                           const int8_t* codes = nullptr);
 // dy (M x C, C a multiple of 4) := dy where y > 0, else 0, in place, y a
 // ReLU's stored output; pmean[tile][c] = the tile's mean of the masked
 // column c over mask_tiles(M, C) row tiles of mask_rows(M, C) rows.
 int mask_rows(long M, int C);
 int mask_tiles(long M, int C);
-hipError_t launch_relu_mask_colsum(int dt, void* dy, const void* y, long M, int C, float* pmean, hipStream_t st);
+hipError_t launch_relu_mask_colsum(int dt, void* dy, const void* y, long M, int C, float* pmean, hipStream_t st,
+                                   const int8_t* codes = nullptr);
 // Backward of y = concat(a, b) over channels where a and b are stored ReLU
 // outputs: da / db (null: not wanted) := the slices of dy, zero where ya / yb
 // is; pmean (non-null) as launch_relu_mask_colsum's, over C = ca + cb columns.

@@ -693,8 +693,8 @@ __global__ void relu_fwd_k(const T* __restrict__ x, T* __restrict__ y, long n4) 
     }
 }
 
-template <class T>
-__global__ void relu_bwd_k(const T* __restrict__ dy, const T* __restrict__ x, T* __restrict__ dx, long n4, int acc) {
+template <class T, class Y>
+__global__ void relu_bwd_k(const T* __restrict__ dy, const Y* __restrict__ x, T* __restrict__ dx, long n4, int acc) {
     for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < n4; i += (long)gridDim.x * blockDim.x) {
         const f4 g = ld4(dy, i), v = ld4(x, i);
         f4 o = acc ? ld4(dx, i) : f4{0.f, 0.f, 0.f, 0.f};
@@ -733,8 +733,8 @@ int mask_tiles(long M, int C) {
 // Rows r0 + lr, r0 + lr + rl, ... < r1, four at a time: their loads are issued
 // together, before any is masked and stored (one at a time, with a quarter of
 // the workgroups, concat_relu_bwd took 21 us on 32768 x 128 fp32, 2.4 TB/s)
-template <class T, class Store>
-__device__ __forceinline__ f4 mask_rows4(const T* g, long gs, const T* y, long ys, long r0, long r1, int rl,
+template <class T, class Y, class Store>
+__device__ __forceinline__ f4 mask_rows4(const T* g, long gs, const Y* y, long ys, long r0, long r1, int rl,
                                          Store store) {
     f4 s = f4{0.f, 0.f, 0.f, 0.f};
     for (long r = r0; r < r1; r += 4 * rl) {
@@ -762,8 +762,8 @@ __device__ __forceinline__ f4 mask_rows4(const T* g, long gs, const T* y, long y
 // tile of mask_rows(M, C) rows the mean over the tile of each masked column,
 // pmean[tile][c] -- a conv bias gradient's partials, summed by
 // sum_from_tiles_k.
-template <class T>
-__global__ __launch_bounds__(256) void relu_mask_colsum_k(T* dy, const T* __restrict__ y, long M, int C,
+template <class T, class Y>
+__global__ __launch_bounds__(256) void relu_mask_colsum_k(T* dy, const Y* __restrict__ y, long M, int C,
                                                           int R, float* __restrict__ pmean) {
     __shared__ f4 red[256];
     const int tid = threadIdx.x;
@@ -790,14 +790,19 @@ __global__ __launch_bounds__(256) void relu_mask_colsum_k(T* dy, const T* __rest
     }
 }
 
-hipError_t launch_relu_mask_colsum(int dt, void* dy, const void* y, long M, int C, float* pmean, hipStream_t st) {
-    if (C % 4) return hipErrorInvalidValue;
+hipError_t launch_relu_mask_colsum(int dt, void* dy, const void* y, long M, int C, float* pmean, hipStream_t st,
+                                   const int8_t* codes) {
+    if (C % 4 || (codes && C % 16)) return hipErrorInvalidValue;
     const dim3 grid(mask_tiles(M, C), ((C >> 2) + 255) / 256);
     const int R = mask_rows(M, C);
-    if (dt == DT_BF16)
-        launch(relu_mask_colsum_k<bf16>, grid, dim3(256), 0, st, (bf16*)dy, (const bf16*)y, M, C, R, pmean);
+    if (dt == DT_BF16 && codes)
+        launch((relu_mask_colsum_k<bf16, int8_t>), grid, dim3(256), 0, st, (bf16*)dy, codes, M, C, R, pmean);
+    else if (dt == DT_BF16)
+        launch((relu_mask_colsum_k<bf16, bf16>), grid, dim3(256), 0, st, (bf16*)dy, (const bf16*)y, M, C, R, pmean);
+    else if (codes)
+        launch((relu_mask_colsum_k<float, int8_t>), grid, dim3(256), 0, st, (float*)dy, codes, M, C, R, pmean);
     else
-        launch(relu_mask_colsum_k<float>, grid, dim3(256), 0, st, (float*)dy, (const float*)y, M, C, R, pmean);
+        launch((relu_mask_colsum_k<float, float>), grid, dim3(256), 0, st, (float*)dy, (const float*)y, M, C, R, pmean);
     return hipGetLastError();
 }
 
@@ -866,13 +871,19 @@ hipError_t launch_relu_fwd(int dt, const void* x, void* y, long n, hipStream_t s
                            n / 4);
     return hipGetLastError();
 }
-hipError_t launch_relu_bwd(int dt, const void* dy, const void* x, void* dx, long n, bool accumulate, hipStream_t st) {
-    if (dt == DT_BF16)
-        launch(relu_bwd_k<bf16>, dim3(ew_grid(n / 4)), dim3(256), 0, st, (const bf16*)dy, (const bf16*)x,
-                           (bf16*)dx, n / 4, (int)accumulate);
+hipError_t launch_relu_bwd(int dt, const void* dy, const void* x, void* dx, long n, bool accumulate, hipStream_t st,
+                           const int8_t* codes) {
+    const dim3 grid(ew_grid(n / 4)), block(256);
+    const int acc = accumulate;
+    if (dt == DT_BF16 && codes)
+        launch((relu_bwd_k<bf16, int8_t>), grid, block, 0, st, (const bf16*)dy, codes, (bf16*)dx, n / 4, acc);
+    else if (dt == DT_BF16)
+        launch((relu_bwd_k<bf16, bf16>), grid, block, 0, st, (const bf16*)dy, (const bf16*)x, (bf16*)dx, n / 4, acc);
+    else if (codes)
+        launch((relu_bwd_k<float, int8_t>), grid, block, 0, st, (const float*)dy, codes, (float*)dx, n / 4, acc);
     else
-        launch(relu_bwd_k<float>, dim3(ew_grid(n / 4)), dim3(256), 0, st, (const float*)dy,
-                           (const float*)x, (float*)dx, n / 4, (int)accumulate);
+        launch((relu_bwd_k<float, float>), grid, block, 0, st, (const float*)dy, (const float*)x, (float*)dx, n / 4,
+               acc);
     return hipGetLastError();
 }
 hipError_t launch_add_fwd(int dt, const void* a, const void* b, void* y, long n, hipStream_t st) {

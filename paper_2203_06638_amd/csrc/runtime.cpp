@@ -681,7 +681,9 @@ void plan_act8(Model& M) {
             if (G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) reads(G.out, true);
             break;
         case G_RELU:
-            reads(Y.L.in0, true);
+            // (its output says as well as its input where it clipped, and a conv
+            // that reads it wants it kept anyway)
+            reads(G.out, true);
             break;
         case G_CONCAT:
             if (G.mconv_a >= 0) {
@@ -817,6 +819,10 @@ struct lpp_ctx {
     float* aux(Worker& w, int l) { return (float*)(w.ws + M.layers[l].aux); }
     uint8_t* ckpt(Worker& w, int l) { return (uint8_t*)(w.ws + M.layers[l].q); }
     bool has_ckpt(int l) const { return act8 && l >= 0 && M.ck[l]; }
+    // the checkpoint's codes where they lie as the elements do, for ReLU decisions
+    const int8_t* signs(Worker& w, int l) {
+        return has_ckpt(l) && M.layers[l].out.c % 16 == 0 ? (const int8_t*)ckpt(w, l) : nullptr;
+    }
     float* bpart(Worker& w, int l) { return (float*)(w.ws + M.layers[l].bpart); }
     double* acc_fwd(Worker& w, int l) { return (double*)(w.ws + M.layers[l].acc); }
     double* acc_bwd(Worker& w, int l) {
@@ -1316,12 +1322,14 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
                 if (!rc) rc = restore(l);
             };
             if (G.kind == G_CONV) {
-                if (G.relu >= 0 && !G.premask) want(G.out);
+                if (G.relu >= 0 && !G.premask && !c->signs(w, G.out)) want(G.out);
                 if (pl.wgrad[G.a] && Y.in_bn < 0 && !Y.wg_act8) want(Y.L.in0);
                 if (pl.din0[G.a] && Y.gsum_y >= 0) want(Y.gsum_y);
             } else if (G.kind == G_BNACT && G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) {
                 want(G.out);
-            } else if (G.kind == G_RELU || (G.kind == G_LINEAR && pl.wgrad[G.a])) {
+            } else if (G.kind == G_RELU && !c->signs(w, G.out)) {
+                want(G.out);
+            } else if (G.kind == G_LINEAR && pl.wgrad[G.a]) {
                 want(Y.L.in0);
             } else if (G.kind == G_CONCAT && G.mconv_a >= 0) {
                 want(Y.L.in0);
@@ -1342,13 +1350,14 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
             const bool bias_fused = G.relu >= 0 && !Y.pw && Y.L.bias && pl.wgrad[G.a];
             if (bias_fused && !G.premask) {
                 LAUNCH("relu", 3.0 * eb * Mo * Y.out.c, st,
-                       lpp::launch_relu_mask_colsum(dt, dy, c->act(w, G.out), Mo, Y.L.cout, c->bpart(w, G.a), st));
+                       lpp::launch_relu_mask_colsum(dt, dy, c->act(w, G.out), Mo, Y.L.cout, c->bpart(w, G.a), st,
+                                                    c->signs(w, G.out)));
                 int rc = add_sum(c->bpart(w, G.a), Y.L.cout, lpp::mask_tiles(Mo, Y.L.cout),
                                  lpp::mask_rows(Mo, Y.L.cout), Mo, Y.L.cout, w.g + Y.poff + Y.wcount);
                 if (rc) return rc;
             } else if (G.relu >= 0 && !G.premask) {
                 LAUNCH("relu", 3.0 * eb * Mo * Y.out.c, st,
-                       lpp::launch_relu_bwd(dt, dy, c->act(w, G.out), dy, Mo * Y.out.c, false, st));
+                       lpp::launch_relu_bwd(dt, dy, c->act(w, G.out), dy, Mo * Y.out.c, false, st, c->signs(w, G.out)));
             }
             if (Y.pw) {
                 if (pl.wgrad[G.a]) {
@@ -1580,7 +1589,8 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
         case G_RELU:
             if (dx0)
                 LAUNCH("relu", 3.0 * eb * Min * Y.out.c, st,
-                       lpp::launch_relu_bwd(dt, dy, x0, dx0, Min * Y.out.c, pl.acc0[G.a] != 0, st));
+                       lpp::launch_relu_bwd(dt, dy, c->act8 ? c->act(w, G.a) : x0, dx0, Min * Y.out.c,
+                                            pl.acc0[G.a] != 0, st, c->signs(w, G.a)));
             break;
         case G_ADD:
             if (dx0)
@@ -2566,13 +2576,13 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* a, void* stream) {
     p.lddx = a->lddx;
     p.gamma = a->gamma;
     p.rstd = a->rstd;
-    p.part = a->dgamma ? a->ws : nullptr;
+    const int parts = lpp::rmsnorm_bwd_parts(a->rows, a->cols);
+    p.part = a->dgamma && parts > 1 ? a->ws : a->dgamma;   // (one part is the sum)
     p.rows = a->rows;
     p.C = a->cols;
     hipError_t e = lpp::launch_rmsnorm_bwd(a->dtype, p, (hipStream_t)stream);
-    if (e == hipSuccess && a->dgamma)
-        e = lpp::launch_part_sums(a->ws, lpp::rmsnorm_bwd_parts(a->rows, a->cols), a->cols, a->dgamma,
-                                  (hipStream_t)stream);
+    if (e == hipSuccess && a->dgamma && parts > 1)
+        e = lpp::launch_part_sums(a->ws, parts, a->cols, a->dgamma, (hipStream_t)stream);
     if (e != hipSuccess) return fail(LPP_EHIP, std::string("rmsnorm_bwd: ") + hipGetErrorString(e));
     return LPP_OK;
 }

@@ -374,56 +374,54 @@ def kernel_snapshot_noalloc(convs, d, dtype, wbuf_elems, x, v, wbuf, stream=None
 # is allocated; tensors used on a stream other than the one they were
 # allocated on must outlive the call's work.
 
-_TORCH = None
-
-
-def _torch():
-    """(module, {dtype: lpp dtype}, float32, uint8), imported on first use."""
-    global _TORCH
-    if _TORCH is None:
-        import torch
-        _TORCH = (torch, {torch.float32: FP32, torch.bfloat16: BF16}, torch.float32, torch.uint8)
-    return _TORCH
-
-
-def _need(ok, what):
-    if not ok:
-        raise LppError(EINVAL, what)
+_TORCH = None     # torch, on first use
+_DTYPES = {}      # torch dtype: lpp dtype
 
 
 def _current_device(t):
-    """The current device, where `t` is a tensor on one."""
-    torch = _torch()[0]
-    _need(isinstance(t, torch.Tensor) and t.is_cuda, "expected a tensor on the current device")
-    return torch.cuda.current_device()
+    """The current device; t, the first argument of a call, is a tensor on one."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _DTYPES.update({torch.float32: FP32, torch.bfloat16: BF16})
+        _TORCH = torch
+    if not isinstance(t, _TORCH.Tensor) or not t.is_cuda:
+        raise LppError(EINVAL, "expected a tensor on the current device")
+    return _TORCH.cuda.current_device()
 
 
 def _matrix(t, what, dev, like=None):
-    """(pointer, row distance, dtype) of a 2-D tensor."""
-    dt = _torch()[1].get(t.dtype)
-    if dt is None or t.dim() != 2 or t.get_device() != dev:
+    """(pointer, row distance, dtype, shape) of a 2-D tensor; like: the shape and dtype
+    that it must have."""
+    dt, s, st = _DTYPES.get(t.dtype), t.shape, t.stride()
+    if dt is None or len(s) != 2 or t.get_device() != dev:
         raise LppError(EINVAL, what + " must be a 2-D float32 or bfloat16 tensor on the current device")
-    rows, cols = t.shape
-    ld = t.stride(0) if rows > 1 else cols
-    if cols > 1 and t.stride(1) != 1 or ld < cols or cols > 1 << 24:
+    rows, cols = s
+    ld = st[0] if rows > 1 else cols
+    if cols > 1 and st[1] != 1 or ld < cols or cols > 1 << 24:
         raise LppError(EINVAL, what + " must have contiguous rows, of at most 2^24 columns, that do not overlap")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+    if like is not None and (s, dt) != like:
         raise LppError(EINVAL, what + " must have the other matrices' shape and type")
-    return t.data_ptr(), ld, dt
+    return t.data_ptr(), ld, dt, s
 
 
 def _floats(t, n, what, dev):
-    if t.dtype != _torch()[2] or not t.is_contiguous() or t.numel() < n or t.get_device() != dev:
+    if t.dtype != _TORCH.float32 or not t.is_contiguous() or t.numel() < n or t.get_device() != dev:
         raise LppError(EINVAL, "%s must be a contiguous float32 tensor of at least %d elements on the current device"
                        % (what, n))
     return t.data_ptr()
 
 
 def _act8(q, rows, cols, dev):
-    if q.dtype != _torch()[3] or not q.is_contiguous() or q.numel() != act8_bytes(rows, cols) or q.get_device() != dev:
+    if q.dtype != _TORCH.uint8 or not q.is_contiguous() or q.numel() != act8_bytes(rows, cols) or q.get_device() != dev:
         raise LppError(EINVAL, "q must be a contiguous uint8 tensor of act8_bytes(rows, cols) elements on the current "
                                "device")
     return q.data_ptr()
+
+
+def _need(ok, what):
+    if not ok:
+        raise LppError(EINVAL, what)
 
 
 def act8_bytes(rows, cols):
@@ -436,8 +434,7 @@ def act8_bytes(rows, cols):
 def kernel_act8_pack(x, q, keep_sign=False, stream=None):
     """q = the 8-bit checkpoint of x (keep_sign: nonzero values stay nonzero)."""
     dev = _current_device(x)
-    p, ld, dt = _matrix(x, "x", dev)
-    rows, cols = x.shape
+    p, ld, dt, (rows, cols) = _matrix(x, "x", dev)
     _check(lib().lpp_kernel_act8_pack(p, dt, rows, cols, ld, int(keep_sign), _act8(q, rows, cols, dev),
                                       _stream_handle(stream)))
 
@@ -445,8 +442,7 @@ def kernel_act8_pack(x, q, keep_sign=False, stream=None):
 def kernel_act8_unpack(q, x, stream=None):
     """x = the values of checkpoint q."""
     dev = _current_device(x)
-    p, ld, dt = _matrix(x, "x", dev)
-    rows, cols = x.shape
+    p, ld, dt, (rows, cols) = _matrix(x, "x", dev)
     _check(lib().lpp_kernel_act8_unpack(_act8(q, rows, cols, dev), rows, cols, p, dt, ld, _stream_handle(stream)))
 
 
@@ -461,35 +457,35 @@ def kernel_act8_wgrad(dy, q, dw, ws=None, stream=None):
     """dw [cout][cin] = dy^T X, dy [rows][cout], q the checkpoint of X [rows][cin];
     ws: act8_wgrad_ws(rows, cout, cin) floats (None where that is 0)."""
     dev = _current_device(dy)
-    p, ld, dt = _matrix(dy, "dy", dev)
-    rows, cout = dy.shape
+    p, ld, dt, (rows, cout) = _matrix(dy, "dy", dev)
     _need(dw.dim() == 2 and dw.shape[0] == cout, "dw must be [cout][cin]")
     cin = dw.shape[1]
-    wp = _floats(ws, 0, "ws", dev) if ws is not None else None
+    wp, wn = (_floats(ws, 0, "ws", dev), ws.numel()) if ws is not None else (None, 0)
     _check(lib().lpp_kernel_act8_wgrad(p, dt, rows, cout, ld, _act8(q, rows, cin, dev), cin,
-                                       _floats(dw, cout * cin, "dw", dev), wp, ws.numel() if ws is not None else 0,
-                                       _stream_handle(stream)))
+                                       _floats(dw, cout * cin, "dw", dev), wp, wn, _stream_handle(stream)))
 
 
 def kernel_rmsnorm(x, gamma, rstd=None, eps=1e-5, res=None, h=None, y=None, q=None, keep_sign=False, stream=None):
     """RMS norm of x (+ res) over the columns into y and / or its checkpoint q;
     h: the sum x + res; rstd [rows]."""
     dev = _current_device(x)
-    a = RmsNormArgs()
-    a.x, a.ldx, a.dtype = _matrix(x, "x", dev)
-    a.rows, a.cols = x.shape
+    xp, ldx, dt, shape = _matrix(x, "x", dev)
+    rows, cols = shape
+    like = (shape, dt)
+    rp = hp = yp = qp = sp = None
+    ldr = ldh = ldy = 0
     if res is not None:
-        a.res, a.ldres, _ = _matrix(res, "res", dev, x)
+        rp, ldr = _matrix(res, "res", dev, like)[:2]
     if h is not None:
-        a.h, a.ldh, _ = _matrix(h, "h", dev, x)
+        hp, ldh = _matrix(h, "h", dev, like)[:2]
     if y is not None:
-        a.y, a.ldy, _ = _matrix(y, "y", dev, x)
+        yp, ldy = _matrix(y, "y", dev, like)[:2]
     if q is not None:
-        a.q = _act8(q, a.rows, a.cols, dev)
-    a.gamma = _floats(gamma, a.cols, "gamma", dev)
+        qp = _act8(q, rows, cols, dev)
     if rstd is not None:
-        a.rstd = _floats(rstd, a.rows, "rstd", dev)
-    a.eps, a.keep_sign = eps, int(keep_sign)
+        sp = _floats(rstd, rows, "rstd", dev)
+    a = RmsNormArgs(xp, rp, hp, yp, qp, ldx, ldr, ldh, ldy, _floats(gamma, cols, "gamma", dev), sp, rows, cols, dt, eps,
+                    int(keep_sign))
     _check(lib().lpp_kernel_rmsnorm(C.byref(a), _stream_handle(stream)))
 
 
@@ -504,20 +500,23 @@ def kernel_rmsnorm_bwd(dy, gamma, rstd, dx=None, dgamma=None, ws=None, h=None, q
     """Gradient of kernel_rmsnorm from its h (x where there was no residual) or from
     h's checkpoint q: dx (+ dres) and dgamma (with ws: rmsnorm_bwd_ws(rows, cols) floats)."""
     dev = _current_device(dy)
-    a = RmsNormBwdArgs()
-    a.dy, a.lddy, a.dtype = _matrix(dy, "dy", dev)
-    a.rows, a.cols = dy.shape
+    yp, ldy, dt, shape = _matrix(dy, "dy", dev)
+    rows, cols = shape
+    like = (shape, dt)
+    hp = qp = rp = xp = gp = wp = None
+    ldh = ldr = ldx = wn = 0
     if h is not None:
-        a.h, a.ldh, _ = _matrix(h, "h", dev, dy)
+        hp, ldh = _matrix(h, "h", dev, like)[:2]
     if q is not None:
-        a.q = _act8(q, a.rows, a.cols, dev)
+        qp = _act8(q, rows, cols, dev)
     if dres is not None:
-        a.dres, a.lddres, _ = _matrix(dres, "dres", dev, dy)
+        rp, ldr = _matrix(dres, "dres", dev, like)[:2]
     if dx is not None:
-        a.dx, a.lddx, _ = _matrix(dx, "dx", dev, dy)
-    a.gamma, a.rstd = _floats(gamma, a.cols, "gamma", dev), _floats(rstd, a.rows, "rstd", dev)
+        xp, ldx = _matrix(dx, "dx", dev, like)[:2]
     if dgamma is not None:
-        a.dgamma = _floats(dgamma, a.cols, "dgamma", dev)
+        gp = _floats(dgamma, cols, "dgamma", dev)
     if ws is not None:
-        a.ws, a.ws_floats = _floats(ws, 0, "ws", dev), ws.numel()
+        wp, wn = _floats(ws, 0, "ws", dev), ws.numel()
+    a = RmsNormBwdArgs(yp, hp, qp, rp, xp, ldy, ldh, ldr, ldx, _floats(gamma, cols, "gamma", dev),
+                       _floats(rstd, rows, "rstd", dev), gp, wp, wn, rows, cols, dt)
     _check(lib().lpp_kernel_rmsnorm_bwd(C.byref(a), _stream_handle(stream)))
