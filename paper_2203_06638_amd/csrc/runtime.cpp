@@ -141,7 +141,7 @@ struct Model {
     // held while the groups between the producer and the last consumer run
     // (shared); those kept as a checkpoint for the backward; and those that decide a
     // ReLU there, whose checkpoint keeps signs
-    std::vector<char> shared, ck, ck_sign;
+    std::vector<char> shared, ck, ck_sign, unwritten;   // unwritten: a folded group's output
     std::vector<int> first_group, last_group;
 };
 
@@ -646,6 +646,7 @@ void plan_act8(Model& M) {
     M.shared.assign(n, 0);
     M.ck.assign(n, 0);
     M.ck_sign.assign(n, 0);
+    M.unwritten.assign(n, 0);
     M.first_group.assign(n, 0);
     M.last_group.assign(n, ng - 1);
     std::vector<int> group_of(n, -1);
@@ -700,8 +701,10 @@ void plan_act8(Model& M) {
         }
     }
     for (const Group& G : M.groups) {
-        // (a folded group's output is never written)
-        if (G.kind == G_BNACT && G.fold) M.ck[G.out] = 0;
+        if (G.kind == G_BNACT && G.fold) {
+            M.unwritten[G.out] = 1;
+            M.ck[G.out] = 0;
+        }
         if (G.kind != G_CONV) continue;
         Layer& Y = M.layers[G.a];
         if (Y.pw || Y.L.k != 1 || Y.L.stride != 1 || Y.L.pad != 0 || Y.L.in0 < 0 || Y.in_bn >= 0 || !M.ck[Y.L.in0])
@@ -1810,7 +1813,7 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
         const long rows_out = (long)N * Y.out.h * Y.out.w;
         if (c->act8 && M.shared[l]) {
             const size_t bytes = align256(dt_size(Y.dt) * (size_t)rows_out * Y.out.c);
-            held.push_back({bytes, M.first_group[l], M.last_group[l], &Y.act});
+            if (!M.unwritten[l]) held.push_back({bytes, M.first_group[l], M.last_group[l], &Y.act});
             held.push_back({bytes, M.first_group[l], M.last_group[l], &Y.dact});
             if (M.ck[l]) Y.q = take((size_t)lpp::act8_bytes(rows_out, Y.out.c));
         } else if (M.stored[l]) {
@@ -2494,6 +2497,8 @@ int lpp_kernel_act8_wgrad(const void* dy, int dtype, long rows, int cout, long l
     if (const char* e = bad_act8(q, rows, cin)) return fail(LPP_EINVAL, e);
     const long need = lpp_act8_wgrad_ws(rows, cout, cin);
     if (need < 0) return fail(LPP_EINVAL, "the gradient must be under 2^31 elements");
+    if (lpp::act8_wgrad_plan(rows, cout, cin).rps > (1 << 30))
+        return fail(LPP_EUNSUPPORTED, "too many rows for so wide a gradient");
     if (rows > 1 && ld > (1 << 24)) return fail(LPP_EUNSUPPORTED, "rows of dy at most 2^24 elements apart");
     if (!dw || (uintptr_t)dw % 4) return fail(LPP_EINVAL, "dw must be a buffer of floats");
     if (need > 0 && (!ws || ((uintptr_t)ws & 15) || ws_floats < need))

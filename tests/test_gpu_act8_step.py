@@ -139,6 +139,48 @@ def test_pre_norm_net_bf16():
         assert PR.relerr(got[2][lo:lo + n], g[lo:lo + n], PR.TAU_BF16) <= PR.TOL_BF16, (kind, lo)
 
 
+def wired():
+    """A sum read by two norms, a conv and a later sum; a norm of a conv's output, of
+    a norm and of a ReLU; a sum of a tensor with itself; a norm that is not the
+    layer after its sum."""
+    m = PM.Model("wired", (3, 10, 10), 10)
+    a = m.conv(-1, 16, 3, bias=True)
+    b = m.conv(m.rmsnorm(a), 16, 3)
+    m.new_unit()
+    s = m.add(b, a)
+    n1, n2 = m.rmsnorm(s), m.rmsnorm(s)
+    c = m.add(m.conv(n1, 16, 1, 1, 0, bias=True), m.conv(m.rmsnorm(n2), 16, 1, 1, 0))
+    m.new_unit()
+    d = m.conv(s, 16, 3)
+    e = m.rmsnorm(c)
+    t = m.add(m.add(e, d), s)
+    u = m.add(t, t)
+    n3 = m.rmsnorm(u)
+    m.new_unit()
+    m.linear(m.gap(m.rmsnorm(m.conv(n3, 24, 3, 2))), 10)
+    return m.assign_blocks([1, 2, 2, 3])
+
+
+@pytest.mark.parametrize("unfused", [False, True])
+@pytest.mark.parametrize("part", [0, 1, 2, 3])
+def test_norms_wired_every_way(part, unfused):
+    m = wired()
+    img, lab, x, tensors = inputs(m, 5, 13)
+    loss, z, g = reference(m, img, lab, x)
+    got = step(m, img, lab, x, part, unfused=unfused)
+    low = step(m, img, lab, x, part, unfused=unfused, act8=True, steps=2)
+    assert PR.relerr(got[1], z, PR.TAU_LOGITS) <= PR.TOL_LOGITS
+    assert np.array_equal(got[1], low[1])
+    info = lpp.describe(m, 5)
+    lo, hi = info.block_lo[part], info.block_hi[part]
+    for kind, at, n in tensors:
+        if at >= lo and at + n <= hi:
+            assert PR.relerr(got[2][at:at + n], g[at:at + n], PR.TAU) <= PR.TOL_GRAD, (kind, at)
+            # (2.3% a checkpoint, six on the longest way: see below)
+            d = low[2][at:at + n] - got[2][at:at + n]
+            assert np.linalg.norm(d) <= 0.06 * np.linalg.norm(got[2][at:at + n]) + 1e-7, (kind, at)
+
+
 @pytest.mark.parametrize("act8", [False, True])
 @pytest.mark.parametrize("dtype", [lpp.FP32, lpp.BF16])
 def test_partial_is_restricted_full(dtype, act8):
