@@ -411,10 +411,12 @@ __global__ __launch_bounds__(kWgThreads, 4) void act8_wgrad_k(const T* __restric
 
 // Splits.  A step of a workgroup costs about 0.4 us and a split's partials O I 8 bytes
 // of traffic at 4 TB/s: rows / S / 32 steps and S partials together are least at
-// S^2 = 6500 rows / (O I) (half or twice that: within 5%).  Never more than two workgroups a compute unit, and one
-// where that leaves a split fewer than 1536 rows.  Measured, one against two: 128 x 512
-// over 131072 rows 41.6 and 44.3 us with the sum, 1024 x 1024 over 100352 rows 356 and
-// 297.
+// S^2 = 6500 rows / (O I) (half or twice that: within 5%).  Never more than two
+// workgroups a compute unit, and one where that leaves a split fewer than 1536 rows
+// (one against two: 128 x 512 over 131072 rows 41.6 and 44.3 us with the sum, 1024 x 1024
+// over 100352 rows 356 and 297).  Up to 400 rows a sum of partials costs more than it
+// saves (64 x 64, 256 rows: 6.7 us in one run, 8.9 in four and a sum for bf16, 7.5 and
+// 10.1 for float32; 640 rows: 9.6 and 8.9, 13.3 and 10.2).
 Act8WgPlan act8_wgrad_plan(long rows, int O, int I) {
     Act8WgPlan p{};
     p.bo = O > 64 ? 128 : 64;
@@ -423,7 +425,7 @@ Act8WgPlan act8_wgrad_plan(long rows, int O, int I) {
     long splits = (long)std::sqrt(6500.0 * rows / ((double)O * I));
     const long two = 512 / tiles;
     splits = std::min(splits, two > 0 && rows / two >= 1536 ? two : 256 / tiles);
-    splits = std::max(1l, std::min(splits, rows / 64));
+    splits = rows <= 400 ? 1 : std::max(1l, std::min(splits, rows / 64));
     p.rps = std::max(32l, ((rows + splits - 1) / splits + 31) / 32 * 32);
     p.splits = (int)std::max(1l, (rows + p.rps - 1) / p.rps);
     p.part_floats = ((long)O * I + 3) / 4 * 4;

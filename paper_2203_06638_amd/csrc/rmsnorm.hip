@@ -58,7 +58,8 @@ __device__ __forceinline__ void ld_gamma(const float* gamma, int ch, int C, floa
 #pragma unroll
     for (int k = 0; k < V; k += 4) {
         const int n = C - (ch + k);
-        chunk_values<float>(ld_chunk(gamma + (n > 0 ? ch + k : 0), n, n < 4), v + k);
+        chunk_values<float>(
+            chunk_mask<float>(ld_chunk(gamma + (n > 0 ? ch + k : 0), n, (n > 0 && n < 4) || C < 4), n), v + k);
     }
 }
 
@@ -355,7 +356,10 @@ hipError_t launch_rmsnorm(int dt, RmsArgs p, hipStream_t st) {
 int rmsnorm_bwd_parts(long rows, int C) {
     const RowShape s = row_shape(DT_F32, C);
     const int rb = std::max(256, s.tpr) / std::max(1, s.tpr);   // rows that a workgroup takes at once
-    return (int)std::max(1l, std::min(kRmsBwdWgs, (rows + rb - 1) / rb));
+    // (few rows: one workgroup; up to four turns of short rows cost less than a sum, a turn
+    // 0.6 us and the sum 2.5; a turn of 2048 channels takes 3 us)
+    const long turns = s.nc > 1 ? 1 : 4;
+    return rows <= turns * rb ? 1 : (int)std::min(kRmsBwdWgs, (rows + rb - 1) / rb);
 }
 
 hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st) {
