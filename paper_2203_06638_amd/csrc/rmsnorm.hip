@@ -318,7 +318,10 @@ static hipError_t rms_dispatch(const P& p, RowShape s, int wgs, hipStream_t st) 
         if constexpr (sizeof(T) == 4) rms_launch<BWD, T, 64, 8>(p, wgs, st);
         else return hipErrorInvalidValue;   // (row_shape: 4 chunks of bf16 a lane)
         break;
-    case 256 * 16 + 2: rms_launch<BWD, T, 256, 2>(p, wgs, st); break;
+    case 256 * 16 + 2:
+        if constexpr (sizeof(T) == 2) rms_launch<BWD, T, 256, 2>(p, wgs, st);
+        else return hipErrorInvalidValue;   // (row_shape: a wave to a row)
+        break;
     case 256 * 16 + 4: rms_launch<BWD, T, 256, 4>(p, wgs, st); break;
     case 1024 * 16 + 2: rms_launch<BWD, T, 1024, 2>(p, wgs, st); break;
     case 1024 * 16 + 4:

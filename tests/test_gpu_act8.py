@@ -167,7 +167,8 @@ def wgrad(dy, q, rows, cin):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_wgrad(dtype, layout):
     shapes = [(0, 8, 8), (1, 1, 1), (1, 40, 24), (31, 64, 64), (33, 65, 63), (257, 16, 128), (512, 129, 130),
-              (1000, 90, 36), (999, 250, 7), (300, 512, 200), (5000, 33, 250), (20000, 128, 64)]
+              (1000, 90, 36), (999, 250, 7), (300, 512, 200), (5000, 33, 250), (20000, 128, 64), (4096, 64, 64),
+              (16384, 128, 512)]
     for k, (rows, cin, cout) in enumerate(shapes):
         x, dy = rand(k, rows, cin).relu(), rand(100 + k, rows, cout, dtype)
         q, xv = checkpoint(x, True)
@@ -225,8 +226,8 @@ def test_wgrad_infinities_and_nan(dtype):
 
 # -- RMS norm ------------------------------------------------------------------
 
-NORM_SHAPES = [(1, 1), (1, 64), (3, 7), (5, 33), (70, 128), (300, 250), (17, 500), (9, 1000), (6, 2000), (5, 4100),
-               (3, 9000), (2, 16384), (9000, 48)]
+NORM_SHAPES = [(1, 1), (1, 64), (3, 7), (5, 33), (70, 128), (300, 250), (17, 500), (9, 1000), (6, 2000), (7, 3000),
+               (5, 4100), (3, 9000), (2, 16384), (9000, 48)]
 
 
 def check_norm(x, gamma, eps, dtype, res, want_y, want_q, layout):
