@@ -66,14 +66,15 @@ __device__ __forceinline__ void act8_val4(uint32_t w, float step, float* v) {
     v[3] = (float)(int8_t)(w >> 24) * step;
 }
 
-// the largest of a value over the L (4 or 8) neighbouring lanes that hold a
-// group's 32 channels, through the lane permutes of the VALU (no LDS)
+// the largest of a value over L (2, 4 or 8) neighbouring lanes, those that hold a
+// group's channels, through the lane permutes of the VALU (no LDS)
 template <int L>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
-    static_assert(L == 4 || L == 8, "lanes of a group");
+    static_assert(L == 2 || L == 4 || L == 8, "lanes of a group");
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));   // lane ^ 1
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));   // lane ^ 2
-    if constexpr (L == 8)
+    if constexpr (L > 2)
+        v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));   // lane ^ 2
+    if constexpr (L > 4)
         v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));   // mirrored in 8 lanes
     return v;
 }

@@ -17,23 +17,29 @@ namespace lpp {
 // sizeof(T) successive channels (a chunk), so that a wave's loads are whole
 // cache lines and the 32 / V lanes of a group are neighbours: the group's
 // maximum takes two or three lane permutes.  Rows are cut into whole groups,
-// so the lanes of a ragged last group idle.  A thread takes kPackU chunks, all
-// loads first.
+// so the lanes of a ragged last group idle; rows of half a group or less take half
+// the lanes.  A thread takes kPackU chunks, all loads first.
 constexpr int kPackU = 4;
 
 struct PackGeom {
     unsigned n;        // chunks: rows x cpr
-    unsigned cpr;      // chunks per row, whole groups
+    unsigned cpr;      // lanes per row
     FastDiv div;       // by cpr
     int C, pitch, G;
     unsigned exact;    // first of the rows whose last chunk must not be read past its values
     long ld;
 };
 
+// lanes that hold a group of rows of C values, padding codes included
 template <typename T>
+static int lanes_of(int C) {
+    return (C <= 16 ? 16 : kAct8Group) * (int)sizeof(T) / 16;
+}
+
+template <typename T, int L>
 __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, PackGeom g, uint8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ exps, int keep_sign) {
-    constexpr int V = 16 / (int)sizeof(T), L = kAct8Group / V;
+    constexpr int V = 16 / (int)sizeof(T);
     const unsigned i0 = blockIdx.x * (256u * kPackU) + threadIdx.x;
     unsigned row[kPackU];
     int ch[kPackU], n[kPackU];
@@ -107,10 +113,9 @@ __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__
 // f(first row, geometry, workgroups) over runs of rows of less than 2^31 chunks
 template <typename T, typename F>
 static hipError_t for_row_runs(long rows, int C, long ld, F f) {
-    constexpr int V = 16 / (int)sizeof(T);
     PackGeom g{};
     g.G = act8_groups(C);
-    g.cpr = (unsigned)g.G * (kAct8Group / V);
+    g.cpr = (unsigned)(g.G * lanes_of<T>(C));
     g.div = fast_div(g.cpr);
     g.C = C;
     g.pitch = act8_pitch(C);
@@ -134,7 +139,9 @@ static hipError_t pack_rows(const T* x, long ld, long rows, int C, bool keep_sig
     return for_row_runs<T>(rows, C, ld, [&](long r0, const PackGeom& g, dim3 grid) {
         uint8_t* c = q + r0 * g.pitch;
         uint8_t* e = exps + r0 * g.G;
-        launch(act8_pack_k<T>, grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
+        constexpr int L = (int)sizeof(T);   // half a group's lanes
+        if (C <= 16) launch((act8_pack_k<T, L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
+        else launch((act8_pack_k<T, 2 * L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
     });
 }
 
@@ -441,7 +448,8 @@ static hipError_t wgrad_parts(const T* dY, long ld, const uint8_t* q, long rows,
     // rows from whose last chunk 8 channels on would lie behind the matrix
     const long over = (O + 7) / 8 * 8 - O, dist = rows > 1 ? ld : over;
     const long tail = over ? std::min(rows, (over + dist - 1) / dist) : 0;
-    const WgGeom g{rows, p.rps, O, I, act8_pitch(I), act8_groups(I), ld, p.part_floats, it, it * ot, p.splits, (int)tail};
+    const WgGeom g{rows, p.rps, O, I, act8_pitch(I), act8_groups(I), ld, p.part_floats, it, it * ot, p.splits,
+                   (int)tail};
     const uint8_t* exps = q + rows * g.pitch;
     const dim3 grid((unsigned)(g.tiles * p.splits)), block(kWgThreads);
     if (p.bo == 128 && p.bi == 128) launch((act8_wgrad_k<T, 128, 128>), grid, block, 0, st, dY, q, exps, part, g);

@@ -28,8 +28,8 @@ __device__ __forceinline__ float dpp_add(float v) {
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* slots, int& turn) {
     v = dpp_add<0xB1>(v);
-    v = dpp_add<0x4E>(v);
-    v = dpp_add<0x141>(v);
+    if constexpr (TPR > 2) v = dpp_add<0x4E>(v);
+    if constexpr (TPR > 4) v = dpp_add<0x141>(v);
     if constexpr (TPR > 8) v = dpp_add<0x140>(v);
     if constexpr (TPR > 16) {
         const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -69,7 +69,8 @@ __device__ __forceinline__ void ld_gamma(const float* gamma, int ch, int C, floa
 // Workgroups walk over the rows and keep gamma in registers.
 template <typename T, int TPR, int NC, bool ST>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_k(RmsArgs p) {
-    constexpr int V = 16 / (int)sizeof(T), L = kAct8Group / V;
+    // lanes of a 32-channel group (rows of 2 or 4 lanes are one group)
+    constexpr int V = 16 / (int)sizeof(T), L = kAct8Group / V < TPR ? kAct8Group / V : TPR;
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;   // threads, rows of a workgroup
     __shared__ float slots[2 * (TB / 64)];
     int turn = 0;
@@ -167,7 +168,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
     __shared__ float slots[2 * (TB / 64)];
-    __shared__ __attribute__((aligned(16))) float sums[RB > 1 ? TB * NC * V : 1];
+    constexpr int W = TB / 64, TW = TPR < 64 ? TPR : 64;   // waves; threads of one whose sums differ by channel
+    __shared__ __attribute__((aligned(16))) float sums[RB > 1 ? W * TW * NC * V : 1];
     int turn = 0;
     const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR;
     float gam[NC][V], dg[NC][V];
@@ -258,14 +260,21 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
     if (!p.part) return;
     float* out = p.part + (long)blockIdx.x * p.pstride;
     if constexpr (RB > 1) {
+        // rows of a wave through lane swaps, waves through LDS
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < V; ++j) sums[((rl * NC + c) * TPR + t) * V + j] = dg[c][j];
+            for (int j = 0; j < V; ++j) {
+#pragma unroll
+                for (int d = TW; d < 64; d *= 2) dg[c][j] += __shfl_xor(dg[c][j], d, 64);
+                if (lane < TW) sums[((wave * NC + c) * TW + lane) * V + j] = dg[c][j];
+            }
         __syncthreads();
         for (int ch = threadIdx.x; ch < p.C; ch += TB) {
             float a = 0.f;
-            for (int w = 0; w < RB; ++w) a += sums[w * (NC * TPR * V) + ch];
+#pragma unroll
+            for (int w = 0; w < W; ++w) a += sums[w * (NC * TW * V) + ch];
             out[ch] = a;
         }
     } else {
@@ -280,12 +289,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
 }
 
 // threads of a row and chunks of a thread: a wave to a row up to 2048 channels (32 a
-// lane in registers), so that rows need no barrier
+// lane in registers), so that rows need no barrier; 16 channels at least, which a
+// checkpoint's padding fills up to
 struct RowShape { int tpr, nc; };
 static RowShape row_shape(int dt, int C) {
     const int V = dt == DT_BF16 ? 8 : 4, chunks = (C + V - 1) / V;
-    for (int tpr : {8, 16, 32, 64})
-        if (chunks <= tpr) return {tpr, 1};
+    for (int tpr : {2, 4, 8, 16, 32, 64})
+        if (chunks <= tpr && tpr * V >= 16) return {tpr, 1};
     for (int nc : {2, 4, 8})
         if (chunks <= 64 * nc && nc * V <= 32) return {64, nc};
     for (int nc : {2, 4})
@@ -308,6 +318,11 @@ static void rms_launch(const P& p, int wgs, hipStream_t st) {
 template <bool BWD, typename T, typename P>
 static hipError_t rms_dispatch(const P& p, RowShape s, int wgs, hipStream_t st) {
     switch (s.tpr * 16 + s.nc) {
+    case 2 * 16 + 1:
+        if constexpr (sizeof(T) == 2) rms_launch<BWD, T, 2, 1>(p, wgs, st);
+        else return hipErrorInvalidValue;   // (8 channels of float32)
+        break;
+    case 4 * 16 + 1: rms_launch<BWD, T, 4, 1>(p, wgs, st); break;
     case 8 * 16 + 1: rms_launch<BWD, T, 8, 1>(p, wgs, st); break;
     case 16 * 16 + 1: rms_launch<BWD, T, 16, 1>(p, wgs, st); break;
     case 32 * 16 + 1: rms_launch<BWD, T, 32, 1>(p, wgs, st); break;

@@ -69,8 +69,8 @@ def untouched(v, buf):
     return bool((buf[mask] == 7).all())
 
 
-SHAPES = [(1, 1), (1, 64), (3, 4), (5, 31), (7, 32), (9, 33), (4, 48), (300, 16), (1000, 90), (257, 250), (33, 1000),
-          (2, 5000), (4097, 64)]
+SHAPES = [(1, 1), (1, 64), (3, 4), (700, 8), (900, 11), (5, 17), (5, 31), (7, 32), (9, 33), (4, 48),
+          (300, 16), (1000, 90), (257, 250), (33, 1000), (2, 5000), (4097, 64)]
 
 
 @pytest.mark.parametrize("keep", [False, True])
@@ -227,7 +227,7 @@ def test_wgrad_infinities_and_nan(dtype):
 # -- RMS norm ------------------------------------------------------------------
 
 NORM_SHAPES = [(1, 1), (1, 64), (3, 7), (5, 33), (70, 128), (300, 250), (17, 500), (9, 1000), (6, 2000), (7, 3000),
-               (5, 4100), (3, 9000), (2, 16384), (9000, 48)]
+               (5, 4100), (3, 9000), (2, 16384), (9000, 48), (9000, 8), (7000, 13), (3000, 20)]
 
 
 def check_norm(x, gamma, eps, dtype, res, want_y, want_q, layout):
