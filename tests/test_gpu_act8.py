@@ -397,6 +397,55 @@ def test_rmsnorm_gradient_against_differences():
         assert abs(num - ana) <= size * (60 * U / e + 10 * e * e), (num, ana)
 
 
+def test_more_than_2_31_elements():
+    """Norm, its gradient and the weight gradient over matrices of 2^31 elements and
+    more: everything but the last rows is zero, so that the last rows are the whole
+    result."""
+    t, last = torch.bfloat16, 150
+    rows, cols = 140000, 16384
+    assert rows * cols > 2 ** 31
+    h, dy = rand(1, last, cols, "bf16"), rand(2, last, cols, "bf16")
+    gamma = rand(3, 1, cols)[0]
+    big = [torch.zeros(rows, cols, dtype=t, device="cuda") for _ in range(3)]
+    big[0][-last:], big[1][-last:] = h.cuda(), dy.cuda()
+    rstd = torch.empty(rows, device="cuda")
+    q = torch.empty(lpp.act8_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    say("norm", rows, cols)
+    lpp.kernel_rmsnorm(big[0], gamma.cuda(), rstd, 1e-5, y=big[2], q=q)
+    yr = R.norm(h.double(), gamma.double(), 1e-5)[2]
+    tol = (cols / 2 + 9) * U + HALF["bf16"]
+    assert ((big[2][-last:].cpu().double() - yr).abs() <= tol * yr.abs()).all()
+    assert not big[2][:-last].any()
+    lpp.kernel_act8_unpack(q, big[2])
+    back = big[2][-last:].cpu().double()
+    assert ((back - yr).abs() <= (0.5 / 63.5 + 1e-3) * yr.abs().amax(1, keepdim=True)).all()
+    say("norm gradient", rows, cols)
+    dg, ws = torch.empty(cols, device="cuda"), torch.empty(lpp.rmsnorm_bwd_ws(rows, cols), device="cuda")
+    lpp.kernel_rmsnorm_bwd(big[1], gamma.cuda(), rstd, big[2], dg, ws, h=big[0])
+    wx, wg, sx, sg = R.norm_bwd(dy.double(), h.double(), rstd[-last:].cpu().double(), gamma.double())
+    tol = (cols + 12) * U * sx
+    assert ((big[2][-last:].cpu().double() - wx).abs() <= tol + HALF["bf16"] * (wx.abs() + tol)).all()
+    assert ((dg.cpu().double() - wg).abs() <= (last + 600) * U * sg + 1e-44).all()
+    assert not big[2][:-last].any()
+    del big, q, rstd
+    torch.cuda.empty_cache()
+    rows, cout, cin = 17000000, 130, 24
+    assert rows * cout > 2 ** 31
+    say("weight gradient", rows, cout, cin)
+    d = rand(4, last, cout, "bf16")
+    x = rand(5, last, cin)
+    dyb = torch.zeros(rows, cout, dtype=t, device="cuda")
+    dyb[-last:] = d.cuda()
+    xb = torch.zeros(rows, cin, device="cuda")
+    xb[-last:] = x.cuda()
+    q = torch.empty(lpp.act8_bytes(rows, cin), dtype=torch.uint8, device="cuda")
+    lpp.kernel_act8_pack(xb, q)
+    got = wgrad(dyb, q, rows, cin)
+    xv = R.values(*R.pack(x.double()), cin)
+    want, size = d.double().t() @ xv, d.double().abs().t() @ xv.abs()
+    assert ((got - want).abs() <= (last + 600) * 2.0 ** -23 * size).all()
+
+
 # -- streams and graphs ------------------------------------------------------------
 
 def chain(t, stream=None):
