@@ -87,7 +87,7 @@ struct Plan {
     std::vector<char> run;        // backward of this layer runs (its output grad exists)
     std::vector<char> wgrad;      // parameter gradients of this layer are written
     std::vector<char> din0, din1; // gradient into input 0 / 1 is computed
-    std::vector<char> acc0, acc1; // ... and accumulated onto an earlier contribution
+    std::vector<char> acc0, acc1; // ... and accumulated onto an earlier contribution (build_groups)
     double flops = 0;             // backward flops (dgrad + wgrad of conv/linear)
 };
 
@@ -329,8 +329,6 @@ int build_model(const lpp_model_desc* desc, int P, Model& M) {
         pl.wgrad.assign(n, 0);
         pl.din0.assign(n, 0);
         pl.din1.assign(n, 0);
-        pl.acc0.assign(n, 0);
-        pl.acc1.assign(n, 0);
         for (int l = 0; l < n; ++l) {
             const Layer& Y = M.layers[l];
             const bool inblk = Y.np > 0 && (i == 0 || Y.L.block == i);
@@ -338,24 +336,11 @@ int build_model(const lpp_model_desc* desc, int P, Model& M) {
             pl.run[l] = inblk || (Y.L.in0 >= 0 && pl.run[Y.L.in0]) ||
                         (two_inputs(Y.L.op) && Y.L.in1 >= 0 && pl.run[Y.L.in1]);
         }
-        std::vector<char> written(n, 0);
         for (int l = n - 1; l >= 0; --l) {
             if (!pl.run[l]) continue;
             const Layer& Y = M.layers[l];
-            const int a = Y.L.in0;
-            if (a >= 0 && pl.run[a]) {
-                pl.din0[l] = 1;
-                pl.acc0[l] = written[a];
-                written[a] = 1;
-            }
-            if (two_inputs(Y.L.op)) {
-                const int b = Y.L.in1;
-                if (b >= 0 && pl.run[b]) {
-                    pl.din1[l] = 1;
-                    pl.acc1[l] = written[b];
-                    written[b] = 1;
-                }
-            }
+            pl.din0[l] = Y.L.in0 >= 0 && pl.run[Y.L.in0];
+            pl.din1[l] = two_inputs(Y.L.op) && Y.L.in1 >= 0 && pl.run[Y.L.in1];
             if (Y.L.op == LPP_CONV || Y.L.op == LPP_LINEAR) {
                 if (pl.wgrad[l]) pl.flops += 2.0 * Y.macs;
                 if (pl.din0[l]) pl.flops += 2.0 * Y.macs;
@@ -409,14 +394,18 @@ void build_groups(Model& M, bool fused) {
                 g.relu = g.out = c;
             } else if (c >= 0 && op(c) == LPP_ADD && !taken[c] && M.layers[c].L.in0 != M.layers[c].L.in1) {
                 const lpp_layer& A = M.layers[c].L;
-                const int other = A.in0 == l ? A.in1 : A.in0;
-                g.add = g.out = c;
-                if (other >= 0 && op(other) == LPP_BN && sole(other) == c && !taken[other])
-                    g.bn2 = other;
-                else
-                    g.res = other;
-                const int r = sole(c);
-                if (r >= 0 && op(r) == LPP_RELU && !taken[r]) g.relu = g.out = r;
+                const int other = A.in0 == l ? A.in1 : A.in0, x = M.layers[l].L.in0;
+                // (one pass writes the gradients of the group's inputs: they are
+                // different tensors)
+                if (other != x) {
+                    g.add = g.out = c;
+                    if (op(other) == LPP_BN && sole(other) == c && !taken[other] && M.layers[other].L.in0 != x)
+                        g.bn2 = other;
+                    else
+                        g.res = other;
+                    const int r = sole(c);
+                    if (r >= 0 && op(r) == LPP_RELU && !taken[r]) g.relu = g.out = r;
+                }
             }
         } else if (op_l == LPP_GAP) {
             const int c = fused ? sole(l) : -1;
@@ -559,6 +548,35 @@ void build_groups(Model& M, bool fused) {
         // the sum that an RMS norm forms; its own readers' gradient is kept there,
         // the whole one goes straight to the add's inputs
         if (g.kind == G_RMS && g.add >= 0) M.stored[g.add] = 1;
+    }
+    // Which contributions to a gradient are added onto an earlier one: in the order in
+    // which the backward pass writes them.  A layer fused into a later one runs
+    // at that one's place, so this is not the order of the layer list.
+    for (Plan& pl : M.plans) {
+        pl.acc0.assign(n, 0);
+        pl.acc1.assign(n, 0);
+        std::vector<char> written(n, 0);
+        auto first = [&](int l) {
+            if (pl.din0[l]) pl.acc0[l] = written[M.layers[l].L.in0], written[M.layers[l].L.in0] = 1;
+        };
+        auto second = [&](int l) {
+            if (pl.din1[l]) pl.acc1[l] = written[M.layers[l].L.in1], written[M.layers[l].L.in1] = 1;
+        };
+        for (int gi = (int)M.groups.size() - 1; gi >= 0; --gi) {
+            const Group& g = M.groups[gi];
+            if (!pl.run[g.out]) continue;
+            if (g.kind == G_RMS && g.add >= 0) {
+                // (the norm's part and the sum's other readers' go on together)
+                if (pl.din0[g.a]) pl.acc0[g.a] = written[g.add];
+            } else {
+                first(g.a);
+                if (two_inputs(op(g.a))) second(g.a);
+            }
+            if (g.bn2 >= 0) first(g.bn2);
+            if (g.add < 0) continue;
+            if (g.kind == G_RMS || M.layers[g.add].L.in0 == g.res) first(g.add);
+            if (g.kind == G_RMS || M.layers[g.add].L.in1 == g.res) second(g.add);
+        }
     }
 }
 
