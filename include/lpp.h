@@ -403,9 +403,9 @@ int lpp_kernel_act8_wgrad(const void* dy, int dtype, long rows, int cout, long l
  * h (wanted or NULL; only with res), y (wanted or NULL) and q (y's 8-bit
  * checkpoint, from the unrounded y; wanted or NULL, keep_sign as above) are
  * written, y or q at least; rstd: float32 [rows] or NULL.  h may be x or res.
- * The gradient, with g = dy * gamma:
- *     dx = rstd * (g - h * rstd^2 * mean over columns of (g * h)) (+ dres),
- *     dgamma = sum over rows of dy * h * rstd,
+ * The gradient, with g = dy * gamma and u = h * rstd:
+ *     dx = rstd * (g - u * mean over columns of (g * u)) (+ dres),
+ *     dgamma = sum over rows of dy * u,
  * from h or, with h NULL, from h's 8-bit checkpoint q.  dx (storage type; it
  * may be dy or dres) or dgamma (float32 [cols], written) may be NULL.  ws: as
  * above, lpp_rmsnorm_bwd_ws(rows, cols) floats, needed for dgamma.

@@ -3,8 +3,8 @@
 //
 //   h = x (+ res, rounded to the storage type), rstd = 1 / sqrt(mean_c h^2 + eps),
 //   y = h * rstd * gamma
-//   g = dy * gamma, dx = rstd * (g - h * rstd^2 * mean_c(g h)) (+ dres),
-//   dgamma = sum over rows of dy * h * rstd
+//   g = dy * gamma, u = h * rstd, dx = rstd * (g - u * mean_c(g u)) (+ dres),
+//   dgamma = sum over rows of dy * u
 //
 // Sums and statistics are float32.  No sums cross workgroups in the forward pass.
 #include <algorithm>
@@ -234,19 +234,23 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rmsnorm_bwd_k(RmsBwdArg
             for (int c = 0; c < NC; ++c) chunk_values<T>(ew[c], e[c]);
         }
         if (kAhead<T, TPR, NC>) load(r0 + step);
+        // (h from here on is u: rstd^2 need not be a float32 number)
         float s = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < V; ++j) s = __builtin_fmaf(dy[c][j] * gam[c][j], h[c][j], s);
-        const float k = row_sum<TPR>(s, slots, turn) / (float)p.C * (rstd * rstd);
+            for (int j = 0; j < V; ++j) {
+                h[c][j] *= rstd;
+                s = __builtin_fmaf(dy[c][j] * gam[c][j], h[c][j], s);
+            }
+        const float k = row_sum<TPR>(s, slots, turn) / (float)p.C;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int ch = (c * TPR + t) * V;
             const int n = ok ? p.C - ch : 0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                dg[c][j] = __builtin_fmaf(dy[c][j], h[c][j] * rstd, dg[c][j]);
+                dg[c][j] = __builtin_fmaf(dy[c][j], h[c][j], dg[c][j]);
                 dy[c][j] = rstd * (dy[c][j] * gam[c][j] - h[c][j] * k);
             }
             if (p.dres) {

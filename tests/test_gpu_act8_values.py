@@ -1,0 +1,35 @@
+"""The stand-alone norm and weight-gradient calls at values their other tests leave out.
+Tolerances as in test_gpu_act8.py."""
+import pytest
+
+from paper_2203_06638_amd import lpp
+from tests import act8ref as R
+from tests.test_gpu_act8 import DT, HALF, U, checkpoint, rand
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_norm_gradient_of_far_rows(dtype, packed):
+    """eps = 0 and rows about 1e-20, 1e-19, 1 and 1e17: 1 / rms and the gradient are
+    float32 numbers, the square of 1 / rms is not.  u = h * rstd takes one
+    rounding, g another, their sum over C terms C + 1, the rest of dx four."""
+    for k, cols in enumerate((70, 250, 2000, 3000, 9000)):
+        scale = torch.tensor([1e-20, 1e-19, 1.0, 1e17, 3e-20]).repeat(3)[:, None]
+        h = (rand(k, 15, cols, spread=0.1) * scale).to(DT[dtype])
+        dy = (rand(k + 20, 15, cols) * 1e-3).to(DT[dtype])
+        gamma = rand(k + 40, 1, cols)[0]
+        q, hv = checkpoint(h) if packed else (None, h.double())
+        rstd = (1 / torch.sqrt((h.double() ** 2).mean(1))).float()
+        assert torch.isfinite(rstd).all()
+        dx, dg = torch.empty_like(dy, device="cuda"), torch.empty(cols, device="cuda")
+        lpp.kernel_rmsnorm_bwd(dy.cuda(), gamma.cuda(), rstd.cuda(), dx, dg,
+                               torch.empty(lpp.rmsnorm_bwd_ws(15, cols), device="cuda"),
+                               h=None if packed else h.cuda(), q=q)
+        wx, wg, sx, sg = R.norm_bwd(dy.double(), hv, rstd.double(), gamma.double())
+        tol = (cols + 12) * U * sx
+        assert ((dx.cpu().double() - wx).abs() <= tol + HALF[dtype] * (wx.abs() + tol)).all(), cols
+        assert ((dg.cpu().double() - wg).abs() <= 30 * U * sg).all(), cols
