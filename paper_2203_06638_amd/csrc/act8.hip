@@ -288,6 +288,8 @@ __global__ __launch_bounds__(kWgThreads, 4) void act8_wgrad_k(const T* __restric
             for (int k = 0; k < QA * 4; ++k) {
                 x[k] = s.a[k / 4][k % 4];
                 if (CAREFUL) x[k] = row ? x[k] : 0u;
+                // (a NaN whose upper half alone would be an infinity)
+                if (CAREFUL && NP > 1 && (x[k] & 0x7fffffffu) > 0x7f800000u) x[k] |= 0x400000u;
             }
             if constexpr (NP == 1) {
                 *(u4*)p = u4{x[0], x[1], x[2], x[3]};

@@ -4,7 +4,7 @@ import pytest
 
 from paper_2203_06638_amd import lpp
 from tests import act8ref as R
-from tests.test_gpu_act8 import DT, HALF, U, checkpoint, rand
+from tests.test_gpu_act8 import DT, HALF, U, checkpoint, rand, wgrad
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +33,21 @@ def test_norm_gradient_of_far_rows(dtype, packed):
         tol = (cols + 12) * U * sx
         assert ((dx.cpu().double() - wx).abs() <= tol + HALF[dtype] * (wx.abs() + tol)).all(), cols
         assert ((dg.cpu().double() - wg).abs() <= 30 * U * sg).all(), cols
+
+
+def test_wgrad_of_a_nan_with_a_low_payload():
+    """A float32 NaN stays one where its upper 16 bits alone would be an
+    infinity: in a row of the steps and in the last row, which ends a ragged
+    matrix."""
+    rows, cin, cout = 100, 70, 66
+    x, dy = rand(1, rows, cin).abs() + 0.1, rand(2, rows, cout)
+    bits = dy.view(torch.int32)
+    bits[17, 5], bits[40, 9], bits[rows - 1, 65] = 0x7f800001, -0x7fff00, 0x7f80ffff
+    assert torch.isnan(dy).sum() == 3
+    q, xv = checkpoint(x)
+    got = wgrad(dy.cuda(), q, rows, cin)
+    bad = torch.zeros(cout, dtype=torch.bool)
+    bad[[5, 9, 65]] = True
+    assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all()
+    want, size = dy.double().t() @ xv, dy.double().abs().t() @ xv.abs()
+    assert ((got - want).abs() <= (rows + 64) * 2.0 ** -23 * size)[~bad].all()
