@@ -79,7 +79,8 @@ enum lpp_mode { LPP_SEQUENTIAL = 0, LPP_ASYNC = 1 };
  * the activation type, and their buffers and their gradients' are shared
  * by layers that are not in use at once.  The forward pass, its loss and its
  * logits are unchanged to the bit; gradients are those of the rounded
- * activations, with the exact ReLU decisions.  Weight gradients of 1x1
+ * activations, with the exact ReLU decisions (also beside an infinity; all
+ * values of its group of channels are then not finite).  Weight gradients of 1x1
  * stride-1 convs and RMS norm gradients read the checkpoints as they are;
  * other layers' inputs are unpacked first.  Inputs of batch norms stay in
  * the activation type.  lpp_get_activation and lpp_get_activation_grad return
@@ -364,10 +365,11 @@ int lpp_kernel_snapshot_noalloc(const lpp_snap_conv* convs, int n_convs, long d,
  * rint(amax * 2^(133-s)) <= 127, within [7, 254],
  *     code = rint(x * 2^(133-s)) (ties to even),  value = code * 2^(s-133).
  * A value is off by at most half a step; a step is between amax/127 and
- * amax/63.5.  Values are exact in float32 and bf16.  With keep_sign a nonzero
- * x never takes code 0 (it takes +-1, up to a whole step off), so that ReLU
- * decisions x > 0 read off the checkpoint are those of x.  A group that holds
- * an infinity or NaN has s = 255 and all its values are NaN.
+ * amax/63.5.  Values are exact in float32 and bf16.  A group that holds an
+ * infinity or NaN has s = 255, its codes are 0 and its values NaN.  With
+ * keep_sign a nonzero x of any other group never takes code 0 (it takes +-1, up
+ * to a whole step off), so that ReLU decisions x > 0 read off the checkpoint
+ * are those of x.
  * Buffer (lpp_act8_bytes(rows, cols) bytes of device memory, 16-byte aligned):
  * int8 codes [rows][pitch], pitch = cols rounded up to 16, the padding codes
  * 0, then the bytes s [rows][(cols + 31) / 32].  lpp_act8_bytes returns -1

@@ -9,7 +9,10 @@
 // keeps every nonzero one a normal number): decoding never rounds.  Rounding
 // to half a step of an amax / 127 .. amax / 63.5 step is the only loss.
 // s = 255 marks a group that holds an infinity or a NaN: all of it decodes to
-// NaN, so a diverged activation is not hidden by its checkpoint.  The largest
+// NaN, so a diverged activation is not hidden by its checkpoint.  Its codes are 0, or
+// with ACT8_DECIDES the values' signs (0 for NaN): ReLU decisions x > 0 are read from
+// the codes, or from the values that they stand for with an infinite step
+// (infinities of x's sign, NaN for 0), since a NaN decides nothing.  The largest
 // float32 magnitudes (from 1.9921875 * 2^127 on) would need s = 255; they take
 // 254 and saturate at code 127.
 //
@@ -39,9 +42,9 @@ __device__ __forceinline__ uint32_t act8_exp(uint32_t amax) {
 }
 // steps per unit of a group with exponent s, 2^(133-s)
 __device__ __forceinline__ float act8_inv(uint32_t s) { return __uint_as_float((260u - s) << 23); }
-// value of one step, 2^(s-133), NaN for 255
-__device__ __forceinline__ float act8_step(uint32_t s) {
-    return __uint_as_float(s == 255u ? 0x7fc00000u : (s - 6u) << 23);
+// value of one step, 2^(s-133), for 255 the float with the bits bad (NaN)
+__device__ __forceinline__ float act8_step(uint32_t s, uint32_t bad = 0x7fc00000u) {
+    return __uint_as_float(s == 255u ? bad : (s - 6u) << 23);
 }
 // four codes, one a byte.  Adding 1.5 * 2^23 rounds to an integer (ties to even)
 // and leaves it in two's complement in the low byte.  keep_sign: a nonzero value
@@ -57,6 +60,13 @@ __device__ __forceinline__ uint32_t act8_code4(const float* x, float inv, bool k
     const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u);
     const uint32_t hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
     return lo | hi;
+}
+// the signs of four values as codes, 0 for NaN
+__device__ __forceinline__ uint32_t act8_sign4(const float* x) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w |= (x[j] > 0.f ? 1u : x[j] < 0.f ? 255u : 0u) << (8 * j);
+    return w;
 }
 // the four values of four codes (signed bytes, converted one by one)
 __device__ __forceinline__ void act8_val4(uint32_t w, float step, float* v) {

@@ -38,7 +38,7 @@ static int lanes_of(int C) {
 
 template <typename T, int L>
 __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, PackGeom g, uint8_t* __restrict__ codes,
-                                                   uint8_t* __restrict__ exps, int keep_sign) {
+                                                   uint8_t* __restrict__ exps, int mode) {
     constexpr int V = 16 / (int)sizeof(T);
     const unsigned i0 = blockIdx.x * (256u * kPackU) + threadIdx.x;
     unsigned row[kPackU];
@@ -63,7 +63,9 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
         uint32_t w[V / 4];
 #pragma unroll
         for (int k = 0; k < V / 4; ++k)
-            w[k] = s == 255u ? 0u : act8_code4(v + 4 * k, act8_inv(s), keep_sign != 0);
+            w[k] = s != 255u              ? act8_code4(v + 4 * k, act8_inv(s), mode != ACT8_NEAREST)
+                   : mode == ACT8_DECIDES ? act8_sign4(v + 4 * k)
+                                          : 0u;
         if (i0 + u * 256u >= g.n) continue;
         if (ch[u] < g.pitch) {
             uint8_t* p = codes + (long)row[u] * g.pitch + ch[u];
@@ -76,7 +78,7 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
 
 template <typename T, bool ST>
 __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__ codes,
-                                                     const uint8_t* __restrict__ exps, PackGeom g,
+                                                     const uint8_t* __restrict__ exps, PackGeom g, uint32_t bad,
                                                      T* __restrict__ x) {
     constexpr int V = 16 / (int)sizeof(T);
     const unsigned i0 = blockIdx.x * (256u * kPackU) + threadIdx.x;
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(256) void act8_unpack_k(const uint8_t* __restrict__
         if (n[u] <= 0) continue;
         float v[V];
 #pragma unroll
-        for (int k = 0; k < V / 4; ++k) act8_val4(w[u][k], act8_step(s[u]), v + 4 * k);
+        for (int k = 0; k < V / 4; ++k) act8_val4(w[u][k], act8_step(s[u], bad), v + 4 * k);
         st_chunk<ST>(x + (long)row[u] * g.ld + ch[u], n[u], v);
     }
 }
@@ -134,38 +136,41 @@ static hipError_t for_row_runs(long rows, int C, long ld, F f) {
 }
 
 template <typename T>
-static hipError_t pack_rows(const T* x, long ld, long rows, int C, bool keep_sign, uint8_t* q, hipStream_t st) {
+static hipError_t pack_rows(const T* x, long ld, long rows, int C, Act8Mode mode, uint8_t* q, hipStream_t st) {
     uint8_t* exps = q + rows * act8_pitch(C);
     return for_row_runs<T>(rows, C, ld, [&](long r0, const PackGeom& g, dim3 grid) {
         uint8_t* c = q + r0 * g.pitch;
         uint8_t* e = exps + r0 * g.G;
         constexpr int L = (int)sizeof(T);   // half a group's lanes
-        if (C <= 16) launch((act8_pack_k<T, L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
-        else launch((act8_pack_k<T, 2 * L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)keep_sign);
+        if (C <= 16) launch((act8_pack_k<T, L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)mode);
+        else launch((act8_pack_k<T, 2 * L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)mode);
     });
 }
 
 template <typename T>
-static hipError_t unpack_rows(const uint8_t* q, long rows, int C, T* x, long ld, hipStream_t st) {
+static hipError_t unpack_rows(const uint8_t* q, long rows, int C, T* x, long ld, bool decides, hipStream_t st) {
     const uint8_t* exps = q + rows * act8_pitch(C);
+    const uint32_t bad = decides ? 0x7f800000u : 0x7fc00000u;   // infinity, NaN
     return for_row_runs<T>(rows, C, ld, [&](long r0, const PackGeom& g, dim3 grid) {
         const uint8_t* c = q + r0 * g.pitch;
         const uint8_t* e = exps + r0 * g.G;
         if (rows * C * (long)sizeof(T) >= kStreamBytes)
-            launch((act8_unpack_k<T, true>), grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
+            launch((act8_unpack_k<T, true>), grid, dim3(256), 0, st, c, e, g, bad, x + r0 * ld);
         else
-            launch((act8_unpack_k<T, false>), grid, dim3(256), 0, st, c, e, g, x + r0 * ld);
+            launch((act8_unpack_k<T, false>), grid, dim3(256), 0, st, c, e, g, bad, x + r0 * ld);
     });
 }
 
-hipError_t launch_act8_pack(int dt, const void* x, long ld, long rows, int C, bool keep_sign, uint8_t* q,
+hipError_t launch_act8_pack(int dt, const void* x, long ld, long rows, int C, Act8Mode mode, uint8_t* q,
                             hipStream_t st) {
-    return dt == DT_BF16 ? pack_rows((const bf16*)x, ld, rows, C, keep_sign, q, st)
-                         : pack_rows((const float*)x, ld, rows, C, keep_sign, q, st);
+    return dt == DT_BF16 ? pack_rows((const bf16*)x, ld, rows, C, mode, q, st)
+                         : pack_rows((const float*)x, ld, rows, C, mode, q, st);
 }
 
-hipError_t launch_act8_unpack(int dt, const uint8_t* q, long rows, int C, void* x, long ld, hipStream_t st) {
-    return dt == DT_BF16 ? unpack_rows(q, rows, C, (bf16*)x, ld, st) : unpack_rows(q, rows, C, (float*)x, ld, st);
+hipError_t launch_act8_unpack(int dt, const uint8_t* q, long rows, int C, void* x, long ld, bool decides,
+                              hipStream_t st) {
+    return dt == DT_BF16 ? unpack_rows(q, rows, C, (bf16*)x, ld, decides, st)
+                         : unpack_rows(q, rows, C, (float*)x, ld, decides, st);
 }
 
 // ---------------------------------------------------------------- weight gradient

@@ -401,9 +401,15 @@ hipError_t launch_average(const RepPtrs& reps, int n_rep, long n, hipStream_t st
 // ---- 8-bit activation checkpoints (act8.h: format and buffer layout) ----
 // x: `rows` rows of C values, ld elements apart, of type dt; q: act8_bytes(rows, C)
 // bytes, 16-byte aligned.
-hipError_t launch_act8_pack(int dt, const void* x, long ld, long rows, int C, bool keep_sign, uint8_t* q,
+// ACT8_NEAREST: the nearest codes; ACT8_KEEP_SIGN: a nonzero value never takes code 0
+// but in a group that is not finite; ACT8_DECIDES: nor there (ReLU decisions).
+enum Act8Mode { ACT8_NEAREST, ACT8_KEEP_SIGN, ACT8_DECIDES };
+hipError_t launch_act8_pack(int dt, const void* x, long ld, long rows, int C, Act8Mode mode, uint8_t* q,
                             hipStream_t st);
-hipError_t launch_act8_unpack(int dt, const uint8_t* q, long rows, int C, void* x, long ld, hipStream_t st);
+// decides: groups that are not finite, packed with ACT8_DECIDES, become infinities of the
+// values' signs (NaN for 0 and NaN) instead of NaN
+hipError_t launch_act8_unpack(int dt, const uint8_t* q, long rows, int C, void* x, long ld, bool decides,
+                              hipStream_t st);
 // dW[O][I] = dY^T X of a checkpoint X [rows][I]: partials [splits][part_floats] over
 // runs of rps rows (bo x bi: the tile of a workgroup); launch_act8_wgrad sums them into
 // dw (ws: splits * part_floats floats, unused with one split)

@@ -1269,8 +1269,8 @@ int run_forward(lpp_ctx* c, Worker& w) {
                 const Layer& O = M.layers[l];
                 const long rows = (long)N * O.out.h * O.out.w;
                 LAUNCH("act8_pack", (eb + 1.0) * rows * O.out.c, st,
-                       lpp::launch_act8_pack(dt, c->act(w, l), O.out.c, rows, O.out.c, M.ck_sign[l] != 0,
-                                             c->ckpt(w, l), st));
+                       lpp::launch_act8_pack(dt, c->act(w, l), O.out.c, rows, O.out.c,
+                                             M.ck_sign[l] ? lpp::ACT8_DECIDES : lpp::ACT8_NEAREST, c->ckpt(w, l), st));
             }
     }
     if (!loss_done) {
@@ -1330,7 +1330,8 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
         const Layer& O = M.layers[l];
         const long rows = (long)N * O.out.h * O.out.w;
         LAUNCH("act8_unpack", (eb + 1.0) * rows * O.out.c, st,
-               lpp::launch_act8_unpack(dt, c->ckpt(w, l), rows, O.out.c, c->act(w, l), O.out.c, st));
+               lpp::launch_act8_unpack(dt, c->ckpt(w, l), rows, O.out.c, c->act(w, l), O.out.c, M.ck_sign[l] != 0,
+                                       st));
         return LPP_OK;
     };
     for (int gi = (int)M.groups.size() - 1; gi >= 0; --gi) {
@@ -2490,7 +2491,8 @@ int lpp_kernel_act8_pack(const void* x, int dtype, long rows, int cols, long ld,
                          void* stream) {
     if (const char* e = bad_matrix(x, dtype, rows, cols, ld)) return fail(LPP_EINVAL, e);
     if (const char* e = bad_act8(q, rows, cols)) return fail(LPP_EINVAL, e);
-    hipError_t e = lpp::launch_act8_pack(dtype, x, ld, rows, cols, keep_sign != 0, (uint8_t*)q, (hipStream_t)stream);
+    hipError_t e = lpp::launch_act8_pack(dtype, x, ld, rows, cols, keep_sign ? lpp::ACT8_KEEP_SIGN : lpp::ACT8_NEAREST,
+                                         (uint8_t*)q, (hipStream_t)stream);
     if (e != hipSuccess) return fail(LPP_EHIP, std::string("act8_pack: ") + hipGetErrorString(e));
     return LPP_OK;
 }
@@ -2498,7 +2500,7 @@ int lpp_kernel_act8_pack(const void* x, int dtype, long rows, int cols, long ld,
 int lpp_kernel_act8_unpack(const void* q, long rows, int cols, void* x, int dtype, long ld, void* stream) {
     if (const char* e = bad_matrix(x, dtype, rows, cols, ld)) return fail(LPP_EINVAL, e);
     if (const char* e = bad_act8(q, rows, cols)) return fail(LPP_EINVAL, e);
-    hipError_t e = lpp::launch_act8_unpack(dtype, (const uint8_t*)q, rows, cols, x, ld, (hipStream_t)stream);
+    hipError_t e = lpp::launch_act8_unpack(dtype, (const uint8_t*)q, rows, cols, x, ld, false, (hipStream_t)stream);
     if (e != hipSuccess) return fail(LPP_EHIP, std::string("act8_unpack: ") + hipGetErrorString(e));
     return LPP_OK;
 }
