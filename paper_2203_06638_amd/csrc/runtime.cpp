@@ -88,6 +88,7 @@ struct Plan {
     std::vector<char> wgrad;      // parameter gradients of this layer are written
     std::vector<char> din0, din1; // gradient into input 0 / 1 is computed
     std::vector<char> acc0, acc1; // ... and accumulated onto an earlier contribution (build_groups)
+    std::vector<char> ck;         // LPP_ACT8: its backward reads this layer's checkpoint
     double flops = 0;             // backward flops (dgrad + wgrad of conv/linear)
 };
 
@@ -653,6 +654,48 @@ bool bnact_apply_reads(const Model& M, const Group& G) {
            2.0 * M.desc.batch * Y.in0.h * Y.in0.w * Y.out.c < 64e6 * M.conv_fill / 512;
 }
 
+// LPP_ACT8: f(layer, how) for the outputs that a group's backward pass reads in the
+// partition of plan pl (-1 and outputs that are held in full among them).
+enum Act8Read {
+    READ_CODES,    // straight from the checkpoint
+    READ_VALUES,   // unpacked
+    READ_SIGNS,    // ReLU decisions from the codes (unpacked where they do not lie as the elements do)
+    READ_MASK      // ReLU decisions of an unpacked output
+};
+template <class F>
+void for_act8_reads(const Model& M, const Plan& pl, const Group& G, F f) {
+    if (!pl.run[G.out]) return;
+    const Layer& Y = M.layers[G.a];
+    switch (G.kind) {
+    case G_CONV:
+        // (with premask the concat's backward has masked its output's gradient)
+        if (G.relu >= 0 && !G.premask) f(G.out, READ_SIGNS);
+        if (pl.wgrad[G.a] && Y.in_bn < 0) f(Y.L.in0, Y.wg_act8 ? READ_CODES : READ_VALUES);
+        if (pl.din0[G.a] && Y.gsum_y >= 0) f(Y.gsum_y, READ_MASK);
+        break;
+    case G_BNACT:
+        if (G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) f(G.out, READ_MASK);
+        break;
+    case G_RELU:
+        // (its output says as well as its input where it clipped, and a conv
+        // that reads it wants it kept anyway)
+        f(G.out, READ_SIGNS);
+        break;
+    case G_CONCAT:
+        if (G.mconv_a >= 0 && pl.din0[G.a]) f(Y.L.in0, READ_MASK);
+        if (G.mconv_a >= 0 && pl.din1[G.a]) f(Y.L.in1, READ_MASK);
+        break;
+    case G_RMS:
+        f(Y.L.in0, READ_CODES);
+        break;
+    case G_LINEAR:
+        if (pl.wgrad[G.a]) f(Y.L.in0, READ_VALUES);
+        break;
+    default:
+        break;
+    }
+}
+
 // LPP_ACT8: which outputs share buffers and which are kept as checkpoints (Model).
 // An output and its gradient are touched by the groups from its producer to
 // its last consumer only, in the forward pass and, reversed, in the backward
@@ -682,47 +725,18 @@ void plan_act8(Model& M) {
             M.last_group[l] = std::max(M.last_group[l], group_of[c]);
         }
     }
-    // outputs that the backward pass reads
-    auto reads = [&](int l, bool sign) {
-        if (l < 0 || !M.shared[l]) return;
-        M.ck[l] = 1;
-        if (sign) M.ck_sign[l] = 1;
-    };
-    for (const Group& G : M.groups) {
-        const Layer& Y = M.layers[G.a];
-        switch (G.kind) {
-        case G_CONV:
-            if (Y.in_bn < 0) reads(Y.L.in0, false);
-            if (G.relu >= 0) reads(G.out, true);
-            if (Y.gsum_y >= 0) reads(Y.gsum_y, true);
-            break;
-        case G_BNACT:
-            if (G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) reads(G.out, true);
-            break;
-        case G_RELU:
-            // (its output says as well as its input where it clipped, and a conv
-            // that reads it wants it kept anyway)
-            reads(G.out, true);
-            break;
-        case G_CONCAT:
-            if (G.mconv_a >= 0) {
-                reads(Y.L.in0, true);
-                reads(Y.L.in1, true);
-            }
-            break;
-        case G_RMS:
-        case G_LINEAR:
-            reads(Y.L.in0, false);
-            break;
-        default:
-            break;
-        }
+    for (const Group& G : M.groups)
+        if (G.kind == G_BNACT && G.fold) M.unwritten[G.out] = 1;
+    for (Plan& pl : M.plans) {
+        pl.ck.assign(n, 0);
+        for (const Group& G : M.groups)
+            for_act8_reads(M, pl, G, [&](int l, Act8Read how) {
+                if (l < 0 || !M.shared[l] || M.unwritten[l]) return;
+                pl.ck[l] = M.ck[l] = 1;
+                if (how == READ_SIGNS || how == READ_MASK) M.ck_sign[l] = 1;
+            });
     }
     for (const Group& G : M.groups) {
-        if (G.kind == G_BNACT && G.fold) {
-            M.unwritten[G.out] = 1;
-            M.ck[G.out] = 0;
-        }
         if (G.kind != G_CONV) continue;
         Layer& Y = M.layers[G.a];
         if (Y.pw || Y.L.k != 1 || Y.L.stride != 1 || Y.L.pad != 0 || Y.L.in0 < 0 || Y.in_bn >= 0 || !M.ck[Y.L.in0])
@@ -1106,9 +1120,12 @@ int bn_stats_standalone(lpp_ctx* c, Worker& w, int b) {
     return LPP_OK;
 }
 
-// Forward pass of worker w at its snapshot; loss and dlogits at the end.
-int run_forward(lpp_ctx* c, Worker& w) {
+// Forward pass of worker w at its snapshot; loss and dlogits at the end.  With
+// LPP_ACT8 it leaves the checkpoints that the partition's backward reads.
+int run_forward(lpp_ctx* c, Worker& w, int partition) {
     Model& M = c->M;
+    const Plan& pl = M.plans[partition];
+    auto wanted = [&](int l) { return c->has_ckpt(l) && pl.ck[l]; };
     const int N = M.desc.batch;
     hipStream_t st = w.stream;
     const int dt = M.dt;
@@ -1210,7 +1227,7 @@ int run_forward(lpp_ctx* c, Worker& w) {
                 a.h = c->act(w, G.add);
             }
             a.y = c->act(w, G.a);
-            a.q = c->has_ckpt(G.a) ? c->ckpt(w, G.a) : nullptr;
+            a.q = wanted(G.a) ? c->ckpt(w, G.a) : nullptr;
             a.keep_sign = a.q && M.ck_sign[G.a];
             a.ldx = a.ldres = a.ldh = a.ldy = C;
             a.gamma = w.v + Y.poff;
@@ -1265,7 +1282,7 @@ int run_forward(lpp_ctx* c, Worker& w) {
         // the outputs that the backward will read, in 8 bits (an RMS norm has
         // written its own)
         for (int l : {G.kind == G_RMS ? G.add : -1, G.kind == G_RMS ? -1 : G.out})
-            if (c->has_ckpt(l)) {
+            if (wanted(l)) {
                 const Layer& O = M.layers[l];
                 const long rows = (long)N * O.out.h * O.out.w;
                 LAUNCH("act8_pack", (eb + 1.0) * rows * O.out.c, st,
@@ -1340,23 +1357,9 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
         Layer& Y = M.layers[G.a];
         if (c->act8) {
             int rc = LPP_OK;
-            auto want = [&](int l) {
-                if (!rc) rc = restore(l);
-            };
-            if (G.kind == G_CONV) {
-                if (G.relu >= 0 && !G.premask && !c->signs(w, G.out)) want(G.out);
-                if (pl.wgrad[G.a] && Y.in_bn < 0 && !Y.wg_act8) want(Y.L.in0);
-                if (pl.din0[G.a] && Y.gsum_y >= 0) want(Y.gsum_y);
-            } else if (G.kind == G_BNACT && G.relu >= 0 && (!bnact_recomputes(G) || bnact_apply_reads(M, G))) {
-                want(G.out);
-            } else if (G.kind == G_RELU && !c->signs(w, G.out)) {
-                want(G.out);
-            } else if (G.kind == G_LINEAR && pl.wgrad[G.a]) {
-                want(Y.L.in0);
-            } else if (G.kind == G_CONCAT && G.mconv_a >= 0) {
-                want(Y.L.in0);
-                want(Y.L.in1);
-            }
+            for_act8_reads(M, pl, G, [&](int l, Act8Read how) {
+                if (!rc && how != READ_CODES && !(how == READ_SIGNS && c->signs(w, l))) rc = restore(l);
+            });
             if (rc) return rc;
         }
         const void* x0 = c->input(w, Y.L.in0);
@@ -1712,7 +1715,7 @@ int enqueue_step(lpp_ctx* c, Worker& w, int worker, int partition, bool traced) 
     LAUNCH("snapshot", c->snap_bytes, st,
            lpp::launch_snapshot(c->M.dt, xq, w.v, c->snap_dev, c->n_snap, c->snap_tiles, w.wbuf, st));
     if (traced) HIPCHK(lpp::launch_timestamp(c->trace_log, w.args, -1, 1, st));
-    int rc = run_forward(c, w);
+    int rc = run_forward(c, w, partition);
     if (rc) return rc;
     rc = run_backward(c, w, partition);
     if (rc) return rc;
