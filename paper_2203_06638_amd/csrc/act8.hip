@@ -36,9 +36,11 @@ static int lanes_of(int C) {
     return (C <= 16 ? 16 : kAct8Group) * (int)sizeof(T) / 16;
 }
 
-template <typename T, int L>
+// DECIDES: ACT8_DECIDES (a branch that costs the other modes 8%: 54675 x 90 float32
+// 7.6 -> 8.2 us)
+template <typename T, int L, bool DECIDES>
 __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, PackGeom g, uint8_t* __restrict__ codes,
-                                                   uint8_t* __restrict__ exps, int mode) {
+                                                   uint8_t* __restrict__ exps, int keep_sign) {
     constexpr int V = 16 / (int)sizeof(T);
     const unsigned i0 = blockIdx.x * (256u * kPackU) + threadIdx.x;
     unsigned row[kPackU];
@@ -63,9 +65,11 @@ __global__ __launch_bounds__(256) void act8_pack_k(const T* __restrict__ x, Pack
         uint32_t w[V / 4];
 #pragma unroll
         for (int k = 0; k < V / 4; ++k)
-            w[k] = s != 255u              ? act8_code4(v + 4 * k, act8_inv(s), mode != ACT8_NEAREST)
-                   : mode == ACT8_DECIDES ? act8_sign4(v + 4 * k)
-                                          : 0u;
+            w[k] = s == 255u ? 0u : act8_code4(v + 4 * k, act8_inv(s), DECIDES || keep_sign != 0);
+        if (DECIDES && s == 255u) {
+#pragma unroll
+            for (int k = 0; k < V / 4; ++k) w[k] = act8_sign4(v + 4 * k);
+        }
         if (i0 + u * 256u >= g.n) continue;
         if (ch[u] < g.pitch) {
             uint8_t* p = codes + (long)row[u] * g.pitch + ch[u];
@@ -142,8 +146,15 @@ static hipError_t pack_rows(const T* x, long ld, long rows, int C, Act8Mode mode
         uint8_t* c = q + r0 * g.pitch;
         uint8_t* e = exps + r0 * g.G;
         constexpr int L = (int)sizeof(T);   // half a group's lanes
-        if (C <= 16) launch((act8_pack_k<T, L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)mode);
-        else launch((act8_pack_k<T, 2 * L>), grid, dim3(256), 0, st, x + r0 * ld, g, c, e, (int)mode);
+        const T* xr = x + r0 * ld;
+        const int keep = mode != ACT8_NEAREST;
+        if (mode == ACT8_DECIDES) {
+            if (C <= 16) launch((act8_pack_k<T, L, true>), grid, dim3(256), 0, st, xr, g, c, e, keep);
+            else launch((act8_pack_k<T, 2 * L, true>), grid, dim3(256), 0, st, xr, g, c, e, keep);
+        } else {
+            if (C <= 16) launch((act8_pack_k<T, L, false>), grid, dim3(256), 0, st, xr, g, c, e, keep);
+            else launch((act8_pack_k<T, 2 * L, false>), grid, dim3(256), 0, st, xr, g, c, e, keep);
+        }
     });
 }
 
