@@ -1228,7 +1228,6 @@ int run_forward(lpp_ctx* c, Worker& w, int partition) {
             }
             a.y = c->act(w, G.a);
             a.q = wanted(G.a) ? c->ckpt(w, G.a) : nullptr;
-            a.keep_sign = a.q && M.ck_sign[G.a];
             a.ldx = a.ldres = a.ldh = a.ldy = C;
             a.gamma = w.v + Y.poff;
             a.rstd = c->aux(w, G.a);

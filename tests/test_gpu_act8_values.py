@@ -4,7 +4,7 @@ import pytest
 
 from paper_2203_06638_amd import lpp
 from tests import act8ref as R
-from tests.test_gpu_act8 import DT, HALF, U, checkpoint, rand, wgrad
+from tests.test_gpu_act8 import DT, HALF, NORM_SHAPES, U, checkpoint, rand, wgrad
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,34 @@ def test_wgrad_of_a_nan_with_a_low_payload():
     assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all()
     want, size = dy.double().t() @ xv, dy.double().abs().t() @ xv.abs()
     assert ((got - want).abs() <= (rows + 64) * 2.0 ** -23 * size)[~bad].all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rmsnorm_keep_sign(dtype):
+    """The norm's checkpoint with keep_sign: codes of y's sign, 0 where y is 0 and in
+    the padding, half a step off where |y| is half a step at least and under a
+    step below."""
+    for k, (rows, cols) in enumerate(NORM_SHAPES):
+        x, res = rand(k, rows, cols, dtype, 2.0), rand(60 + k, rows, cols, dtype, 2.0)
+        x[:, ::3], res[:, ::3] = 0, 0
+        x[::5] *= 1e-3
+        if cols == 1:
+            x[:] = 1.5
+        gamma = rand(90 + k, 1, cols)[0]
+        gamma = torch.where(gamma.abs() < 1e-3, torch.ones(()), gamma)
+        for r in (None, res):
+            q = torch.full((lpp.act8_bytes(rows, cols),), 99, dtype=torch.uint8, device="cuda")
+            lpp.kernel_rmsnorm(x.cuda(), gamma.cuda(), None, 1e-5, res=None if r is None else r.cuda(), q=q,
+                               keep_sign=True)
+            _, _, y = R.norm(x.double(), gamma.double(), 1e-5, None if r is None else r.double(), DT[dtype])
+            codes, s = R.split(q.cpu(), rows, cols)
+            assert (codes[:, cols:] == 0).all()
+            assert torch.equal(torch.sign(codes[:, :cols].double()), torch.sign(y)), (rows, cols)
+            tol = (cols / 2 + 6) * U
+            lo, hi = R.exponents(y * (1 - 2 * tol)), R.exponents(y * (1 + 2 * tol))
+            assert ((s.long() >= lo) & (s.long() <= hi)).all()
+            step = torch.exp2(s.double() - 133).repeat_interleave(32, 1)[:, :cols]
+            err = (R.values(codes, s, cols) - y).abs()
+            far = y.abs() * (1 - 2 * tol) > step / 2
+            assert (err <= step * 0.5 + 3 * tol * y.abs())[far].all()
+            assert (err < step)[~far & (y != 0)].all()
