@@ -1643,10 +1643,18 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
                 if (rc) return rc;
                 break;
             }
-            if (dx0 || pl.din1[G.a])
-                LAUNCH("concat", (1.0 + (dx0 ? 1.0 : 0.0) + (pl.din1[G.a] ? 1.0 : 0.0)) * eb * Min * Y.out.c, st,
+            if (dx0 || pl.din1[G.a]) {
+                // (both slices of one tensor's gradient: one after the other)
+                void* dx1 = pl.din1[G.a] ? c->dact(w, Y.L.in1) : nullptr;
+                const bool apart = dx0 && dx0 == dx1;
+                LAUNCH("concat", (1.0 + (dx0 ? 1.0 : 0.0) + (dx1 && !apart ? 1.0 : 0.0)) * eb * Min * Y.out.c, st,
                        lpp::launch_concat_bwd(dt, dy, Min, Y.in0.c, Y.in1.c, dx0, pl.acc0[G.a] != 0,
-                                              pl.din1[G.a] ? c->dact(w, Y.L.in1) : nullptr, pl.acc1[G.a] != 0, st));
+                                              apart ? nullptr : dx1, pl.acc1[G.a] != 0, st));
+                if (apart)
+                    LAUNCH("concat", 2.0 * eb * Min * Y.out.c, st,
+                           lpp::launch_concat_bwd(dt, dy, Min, Y.in0.c, Y.in1.c, nullptr, false, dx1,
+                                                  pl.acc1[G.a] != 0, st));
+            }
             break;
         case G_MAXPOOL:
             if (dx0)

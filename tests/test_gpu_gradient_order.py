@@ -62,3 +62,29 @@ def test_gradient_against_float64(name, dtype, unfused, act8):
     for kind, lo, n in tensors:
         a, b = got[2][lo:lo + n], g[lo:lo + n]
         assert np.linalg.norm(a - b) <= bar * (np.linalg.norm(b) + 0.01 * np.linalg.norm(g)), (kind, lo)
+
+
+@pytest.mark.parametrize("unfused", [False, True])
+@pytest.mark.parametrize("dtype", [lpp.FP32, lpp.BF16])
+def test_concat_of_a_tensor_with_itself(dtype, unfused):
+    """A 1x1 conv over concat(x, x) is one over x with the sum of its halves: the
+    reference net; the gradients of the halves are that of their sum."""
+    def make(twice):
+        m = PM.Model("twice", (8, 8, 8), 8)
+        x = m.conv(-1, 16, 3, bias=True)
+        t = m.conv(m.concat(x, x) if twice else x, 16, 1, 1, 0)
+        m.linear(m.gap(m.conv(t, 16, 3, 2)), 8)
+        return m.assign_blocks([1])
+    m, one = make(True), make(False)
+    img, lab, x, tensors = inputs(m, 8, 23, True)
+    lo, n = tensors[2][1:]
+    assert tensors[2][0] == "conv_w" and n == 16 * 32
+    w = x[lo:lo + n].reshape(16, 2, 16)
+    loss, z, g = reference(one, img, lab, np.concatenate([x[:lo], w.sum(1).ravel(), x[lo + n:]]))
+    half = g[lo:lo + n // 2].reshape(16, 1, 16)
+    g = np.concatenate([g[:lo], np.broadcast_to(half, (16, 2, 16)).ravel(), g[lo + n // 2:]])
+    got = step(m, img, lab, x, 0, dtype, steps=2, unfused=unfused)
+    bar = 0.1 if dtype == lpp.BF16 else 0.01     # (as above)
+    for kind, at, k in tensors:
+        a, b = got[2][at:at + k], g[at:at + k]
+        assert np.linalg.norm(a - b) <= bar * (np.linalg.norm(b) + 0.01 * np.linalg.norm(g)), (kind, at)
