@@ -364,8 +364,10 @@ int lpp_kernel_snapshot_noalloc(const lpp_snap_conv* convs, int n_convs, long d,
  * magnitude and s the biased exponent of the smallest power of two for which
  * rint(amax * 2^(133-s)) <= 127, within [7, 254],
  *     code = rint(x * 2^(133-s)) (ties to even),  value = code * 2^(s-133).
- * A value is off by at most half a step; a step is between amax/127 and
- * amax/63.5.  Values are exact in float32 and bf16.  A group that holds an
+ * A value is off by at most half a step; a step is more than amax/127.5 and at
+ * most amax/63.75, but 2^-126 at least (for amax under 63.75 * 2^-126), and
+ * magnitudes from 127.5 * 2^121 on saturate, up to a step off.  Values are exact
+ * in float32 and bf16.  A group that holds an
  * infinity or NaN has s = 255, its codes are 0 and its values NaN.  With
  * keep_sign a nonzero x of any other group never takes code 0 (it takes +-1, up
  * to a whole step off), so that ReLU decisions x > 0 read off the checkpoint
@@ -411,7 +413,9 @@ int lpp_kernel_act8_wgrad(const void* dy, int dtype, long rows, int cout, long l
  * from h or, with h NULL, from h's 8-bit checkpoint q.  dx (storage type; it
  * may be dy or dres) or dgamma (float32 [cols], written) may be NULL.  ws: as
  * above, lpp_rmsnorm_bwd_ws(rows, cols) floats, needed for dgamma.
- * Statistics and sums are float32, in a fixed order.  dtype: enum lpp_dtype of
+ * Statistics and sums are float32, in a fixed order: a row whose squares add up to
+ * more than float32 holds has rstd = 0, and y = 0 where h is finite; with eps = 0
+ * one whose squares vanish has an infinite rstd.  dtype: enum lpp_dtype of
  * every matrix; gamma float32 [cols]; at most 16384 columns
  * (LPP_EUNSUPPORTED).  Streams, capture and errors as above.
  */

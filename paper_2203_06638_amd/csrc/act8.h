@@ -6,15 +6,15 @@
 // for which rint(amax * 2^(133-s)) <= 127, kept within [7, 254]; a value is
 // stored as code = rint(x * 2^(133-s)) and stands for code * 2^(s-133).  Codes
 // have 7 magnitude bits, so that value is exact in bfloat16 and float32 (s >= 7
-// keeps every nonzero one a normal number): decoding never rounds.  Rounding
-// to half a step of an amax / 127 .. amax / 63.5 step is the only loss.
+// keeps every nonzero one a normal number): decoding never rounds.  Rounding to half
+// a step, of a step in (amax / 127.5, amax / 63.75] or 2^-126, is the only loss.
 // s = 255 marks a group that holds an infinity or a NaN: all of it decodes to
 // NaN, so a diverged activation is not hidden by its checkpoint.  Its codes are 0, or
 // with ACT8_DECIDES the values' signs (0 for NaN): ReLU decisions x > 0 are read from
 // the codes, or from the values that they stand for with an infinite step
 // (infinities of x's sign, NaN for 0), since a NaN decides nothing.  The largest
 // float32 magnitudes (from 1.9921875 * 2^127 on) would need s = 255; they take
-// 254 and saturate at code 127.
+// 254 and saturate at code 127, up to a step off.
 //
 // Buffer: codes [rows][pitch], pitch = C rounded up to 16 (padding codes 0), then
 // the exponents [rows][ceil(C / 32)], both bytes.

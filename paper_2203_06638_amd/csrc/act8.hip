@@ -435,14 +435,16 @@ __global__ __launch_bounds__(kWgThreads, 4) void act8_wgrad_k(const T* __restric
         }
 }
 
-// Splits.  A step of a workgroup costs about 0.4 us and a split's partials O I 8 bytes
-// of traffic at 4 TB/s: rows / S / 32 steps and S partials together are least at
-// S^2 = 6500 rows / (O I) (half or twice that: within 5%).  Never more than two
-// workgroups a compute unit, and one where that leaves a split fewer than 1536 rows
-// (one against two: 128 x 512 over 131072 rows 41.6 and 44.3 us with the sum, 1024 x 1024
-// over 100352 rows 356 and 297).  Up to 400 rows a sum of partials costs more than it
-// saves (64 x 64, 256 rows: 6.7 us in one run, 8.9 in four and a sum for bf16, 7.5 and
-// 10.1 for float32; 640 rows: 9.6 and 8.9, 13.3 and 10.2).
+// Splits.  A step of a workgroup costs about 0.4 us (bf16 with two workgroups a compute
+// unit; float32 0.75, or 1.2 with one: the rule takes both types alike) and a split's
+// partials O I 8 bytes of traffic at 4 TB/s: rows / S / 32 steps and S partials
+// together are least at S^2 = 6500 rows / (O I) (half or twice that: within 5%).  Never
+// more than two workgroups a compute unit, and one where that leaves a split fewer than
+// 1536 rows (one against two: 128 x 512 over 131072 rows 41.6 and 44.3 us with the sum,
+// 1024 x 1024 over 100352 rows 356 and 297).  Up to 400 rows a sum of partials costs more
+// than it saves (64 x 64, 256 rows: 6.7 us in one run, 8.9 in four and a sum for bf16, 7.5
+// and 10.1 for float32; 640 rows: 9.6 and 8.9, 13.3 and 10.2; 333 x 100 x 36 float32 10.6
+// in one, 6.4 + 3.8 in several and a sum, whose launch it saves).
 Act8WgPlan act8_wgrad_plan(long rows, int O, int I) {
     Act8WgPlan p{};
     p.bo = O > 64 ? 128 : 64;

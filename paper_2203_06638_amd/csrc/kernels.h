@@ -427,7 +427,9 @@ hipError_t launch_act8_wgrad(int dt, const void* dY, long ld, const uint8_t* q, 
 // Tensors of type dt with their row distances in elements; null pointers: not there /
 // not wanted.  h is written only with res.  q: y's checkpoint.  The fields after the
 // blank line are set by the launcher.
-constexpr int kRmsMaxC = 16384;   // a row stays in the registers of 1024 threads
+// (a row stays in the registers of 1024 threads; the gradient, which keeps gamma and
+// dgamma as well, spills 144 (bf16) or 264 (float32) bytes a lane above 8192 channels)
+constexpr int kRmsMaxC = 16384;
 struct RmsArgs {
     const void *x, *res;
     void *h, *y;

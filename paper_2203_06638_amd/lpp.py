@@ -372,7 +372,9 @@ def kernel_snapshot_noalloc(convs, d, dtype, wbuf_elems, x, v, wbuf, stream=None
 # act8_bytes(rows, cols) bytes; gamma, rstd, gradients of parameters and
 # workspaces are contiguous float32 tensors.  Buffers are checked and nothing
 # is allocated; tensors used on a stream other than the one they were
-# allocated on must outlive the call's work.
+# allocated on must outlive the call's work.  stream=None is the default (NULL)
+# stream, as in every call here, not torch's current one: inside
+# torch.cuda.stream(s), and to be captured, calls need stream=s.
 
 _TORCH = None     # torch, on first use
 _DTYPES = {}      # torch dtype: lpp dtype

@@ -82,3 +82,21 @@ def test_rmsnorm_keep_sign(dtype):
             far = y.abs() * (1 - 2 * tol) > step / 2
             assert (err <= step * 0.5 + 3 * tol * y.abs())[far].all()
             assert (err < step)[~far & (y != 0)].all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rmsnorm_beyond_float32_squares(dtype):
+    """A row whose squares add up to more than float32 holds: rstd 0 and y 0; with
+    eps = 0 one whose squares vanish: rstd infinite.  Other rows are as ever."""
+    for cols in (40, 3000):
+        x = rand(3, 4, cols, dtype, 0.1)
+        x[1] = torch.finfo(DT[dtype]).min
+        x[2] = 1e-30
+        xd = x.cuda()
+        y, rstd = torch.empty_like(xd), torch.empty(4, device="cuda")
+        lpp.kernel_rmsnorm(xd, torch.ones(cols, device="cuda"), rstd, 0.0, y=y)
+        assert rstd[1] == 0 and rstd[2] == float("inf") and (y[1] == 0).all()
+        _, rr, yr = R.norm(x.double(), torch.ones(cols, dtype=torch.float64), 0.0)
+        tol = (cols / 2 + 9) * U + HALF[dtype]
+        for r in (0, 3):
+            assert ((y[r].cpu().double() - yr[r]).abs() <= tol * yr[r].abs()).all()
