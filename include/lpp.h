@@ -367,11 +367,10 @@ int lpp_kernel_snapshot_noalloc(const lpp_snap_conv* convs, int n_convs, long d,
  * A value is off by at most half a step; a step is more than amax/127.5 and at
  * most amax/63.75, but 2^-126 at least (for amax under 63.75 * 2^-126), and
  * magnitudes from 127.5 * 2^121 on saturate, up to a step off.  Values are exact
- * in float32 and bf16.  A group that holds an
- * infinity or NaN has s = 255, its codes are 0 and its values NaN.  With
- * keep_sign a nonzero x of any other group never takes code 0 (it takes +-1, up
- * to a whole step off), so that ReLU decisions x > 0 read off the checkpoint
- * are those of x.
+ * in float32 and bf16.  A group that holds an infinity or NaN has s = 255, its
+ * codes are 0 and its values NaN.  With keep_sign a nonzero x of any other group
+ * never takes code 0 (it takes +-1, up to a whole step off), so that ReLU
+ * decisions x > 0 read off the checkpoint are those of x.
  * Buffer (lpp_act8_bytes(rows, cols) bytes of device memory, 16-byte aligned):
  * int8 codes [rows][pitch], pitch = cols rounded up to 16, the padding codes
  * 0, then the bytes s [rows][(cols + 31) / 32].  lpp_act8_bytes returns -1
