@@ -454,6 +454,140 @@ typedef struct {
 long lpp_rmsnorm_bwd_ws(long rows, int cols);
 int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* args, void* stream);
 
+/*
+ * Group norm of a channels-last activation with an activation function behind it.
+ * The matrix has images * pixels rows (pixels of an image, image after image) of
+ * `channels` columns, rows ld >= channels elements apart.  A group is channels /
+ * groups successive channels of one image (groups divides channels; 1 group: all
+ * channels, groups == channels: one each):
+ *     mean, var (biased) over the group's pixels and channels,
+ *     rstd = 1 / sqrt(var + eps),  u = (x - mean) * rstd,
+ *     z = u * gamma + beta,  y = act(z),
+ * act: enum lpp_act.  A ReLU lets z > 0 through (a NaN becomes 0, as in LPP_RELU); SiLU is
+ * z / (1 + e^-z).  y may be x.  mean and rstd (float32 [images][groups]) may be NULL.
+ * The gradient, with dz = dy * act'(z), z from x, mean and rstd as above:
+ *     dbeta = sum of dz, dgamma = sum of dz * u over images and pixels,
+ *     dx = rstd * (dz * gamma - (s1 + u * s2)) (+ dres),
+ *     s1 = mean over the group of dz * gamma, s2 = of dz * gamma * u.
+ * dx (storage type; it may be dy, dres or x), dgamma and dbeta (float32 [channels],
+ * written) may be NULL, one at least is wanted.  dres may be NULL.
+ * Statistics and sums are float32, merged in a fixed order.  A group whose squared
+ * deviations add up to more than float32 holds has rstd = 0; one that holds an infinity or
+ * NaN has a NaN mean.  images == 0 is valid (dgamma and dbeta become 0); pixels >= 1.
+ * ws: lpp_groupnorm_ws / lpp_groupnorm_bwd_ws floats of device memory (16-byte aligned, may
+ * be NULL where that is 0), scratch of this call until it has run: calls that may
+ * overlap need their own.  -1 for sizes that the calls refuse, LPP_EUNSUPPORTED for more
+ * than 2^31 workgroups (more than 2^24 channels or 2^40 elements: LPP_EINVAL).  dtype, streams,
+ * capture and errors as above.
+ */
+enum lpp_act { LPP_ACT_NONE = 0, LPP_ACT_RELU = 1, LPP_ACT_SILU = 2 };
+typedef struct {
+    const void* x;
+    void* y;
+    long ldx, ldy;               /* elements between rows                       */
+    const float* gamma;          /* float32 [channels]                          */
+    const float* beta;
+    float* mean;
+    float* rstd;
+    float* ws;
+    long ws_floats;
+    long images, pixels;
+    int channels, groups;
+    int dtype;
+    int act;
+    float eps;
+} lpp_groupnorm_args;
+long lpp_groupnorm_ws(long images, long pixels, int channels, int groups);
+int lpp_kernel_groupnorm(const lpp_groupnorm_args* args, void* stream);
+
+typedef struct {
+    const void* dy;
+    const void* x;
+    const void* dres;
+    void* dx;
+    long lddy, ldx, lddres, lddx;
+    const float* gamma;
+    const float* beta;
+    const float* mean;
+    const float* rstd;
+    float* dgamma;
+    float* dbeta;
+    float* ws;
+    long ws_floats;
+    long images, pixels;
+    int channels, groups;
+    int dtype;
+    int act;
+} lpp_groupnorm_bwd_args;
+long lpp_groupnorm_bwd_ws(long images, long pixels, int channels, int groups);
+int lpp_kernel_groupnorm_bwd(const lpp_groupnorm_bwd_args* args, void* stream);
+
+/*
+ * What is kept of a teacher's answers: of every row of logits z [rows][classes] (rows
+ * ldz >= classes elements apart) the k largest values (float32 [rows][k], in descending
+ * order), their classes (int32 [rows][k]; equal values: the lowest class first, 0 and -0
+ * are equal; a NaN is above everything) and, if rest is not NULL (float32 [rows]),
+ *     rest = log of the sum of exp(z / temperature) over all other classes
+ * (-inf where none has a value above -inf).  1 <= k <= min(classes, 128)
+ * (LPP_EUNSUPPORTED for more than 128); temperature > 0 and finite.  ws:
+ * lpp_top_logits_ws(rows, classes, k) floats, as above.  rows == 0 is valid.
+ */
+typedef struct {
+    const void* z;
+    long ldz;
+    long rows;
+    int classes, k;
+    int dtype;                   /* of z                                        */
+    float temperature;
+    float* values;
+    int* index;
+    float* rest;
+    float* ws;
+    long ws_floats;
+} lpp_top_logits_args;
+long lpp_top_logits_ws(long rows, int classes, int k);
+int lpp_kernel_top_logits(const lpp_top_logits_args* args, void* stream);
+
+/*
+ * Distillation from a teacher's top logits, forward and backward in one call.  The
+ * teacher's answer to a row is its list -- values and index, [rows][k], an index outside
+ * [0, classes) marks an entry that is not used -- and rest, [rows] or NULL.  With T =
+ * temperature, p = softmax over {values / T} of the list and rest, which stands for all
+ * classes that are not listed (rest NULL: the list stands for all, p of other classes is
+ * 0); q = softmax(z / T) at the listed classes, and their others' sum for rest:
+ *     soft = sum of p log(p / q)  (the terms with p = 0 are 0),
+ *     hard = -log softmax(z)[label],
+ *     loss = weight * ((1 - alpha) * hard + alpha * T^2 * soft)      (float32 [rows]),
+ *     dz = scale * d loss / dz             (type and shape of z; may be z, or NULL).
+ * p_j = q_j p_rest / q_rest is the gradient's share of a class that is not listed.  A row whose
+ * label is outside [0, classes) (all rows with labels NULL) has no hard term, one whose
+ * list is empty (no entry used, or all of them and rest -inf) no soft term; one of weight 0
+ * has loss 0 and gradient 0, whatever it holds.  weight: float32 [rows], NULL for 1.  A class that
+ * is listed twice counts with both entries.  Logits of -inf (masked classes) take no
+ * part; a row with an infinity or NaN otherwise is NaN.
+ * 1 <= k <= 128; classes >= 1; 0 <= alpha <= 1; temperature > 0; scale finite.  ws:
+ * lpp_distill_ws(rows, classes) floats, as above.  rows == 0 is valid.
+ */
+typedef struct {
+    const void* z;
+    void* dz;
+    long ldz, lddz;
+    long rows;
+    int classes, k;
+    int dtype;
+    const float* values;
+    const int* index;
+    const float* rest;
+    const int* labels;
+    const float* weight;
+    float* loss;
+    float alpha, temperature, scale;
+    float* ws;
+    long ws_floats;
+} lpp_distill_args;
+long lpp_distill_ws(long rows, int classes);
+int lpp_kernel_distill(const lpp_distill_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

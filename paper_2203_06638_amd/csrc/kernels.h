@@ -36,6 +36,12 @@ struct StepArgs {
     const int* labels;
     float lr;
     long trace_slot;   // this step's row of the timestamp log, or -1
+    // a distillation step's teacher (lpp_teacher)
+    const float* values;
+    const int* index;
+    const float* rest;
+    int k;
+    float alpha, temperature;
 };
 hipError_t launch_set_step_args(StepArgs* dst, const float* images, const int* labels, float lr, long trace_slot,
                                 hipStream_t st);
@@ -469,5 +475,94 @@ struct RmsBwdArgs {
 };
 int rmsnorm_bwd_parts(long rows, int C);
 hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st);
+
+// ---- top logits and distillation (distill.hip) ----
+// As lpp_kernel_top_logits and lpp_kernel_distill; the fields after the blank line are set
+// by the launcher.  step: the teacher and the labels are read from there on the device.
+constexpr int kDistillMaxK = 128;
+struct TopArgs {
+    const void* z;
+    long ldz, rows;
+    int C, k;
+    float temp;
+    float* values;
+    int* index;
+    float* rest;
+    float* ws;
+
+    long exact;
+    int pieces, piece;
+};
+struct DistillArgs {
+    const void* z;
+    void* dz;
+    long ldz, lddz, rows;
+    int C, k;
+    const float* values;
+    const int* index;
+    const float* rest;
+    const int* labels;
+    const float* weight;
+    float* loss;
+    float alpha, temp, scale;
+    float* ws;
+    const StepArgs* step;
+
+    long exact;
+    int pieces, piece, grid_pieces, lds_k;
+};
+// floats of ws, and the workgroups of a launch
+long top_logits_ws(long rows, int C, int k);
+long top_logits_wgs(long rows, int C, int k);
+long distill_ws(long rows, int C);
+hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st);
+hipError_t launch_distill(int dt, DistillArgs p, hipStream_t st);
+
+// ---- group norm with an activation function (groupnorm.hip) ----
+// Tensors as for the RMS norm, rows image after image; the shape and the fields after the
+// blank line are set by the launcher.
+enum ActFn { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2 };
+struct GnShape {
+    long images, pixels;
+    int C, G, cg;       // channels, groups, channels of a group
+    int lw;             // log2 of the lanes that take a row's chunks
+    int slabs, splits;  // of the channels; of an image's rows, rps rows each
+    long rps;
+    int parts;          // (group, slab) pairs of a split: group + slab
+    int cp;             // C rounded up to 4
+    long rows_ws;       // images * splits
+    long sums;          // gradient: where the channels' sums begin in ws (floats)
+};
+struct GnArgs {
+    const void* x;
+    void* y;
+    long ldx, ldy;
+    const float *gamma, *beta;
+    float *mean, *rstd;   // [images][G], may be null
+    float* ws;
+    int act;
+    float eps;
+
+    GnShape s;
+    long exact;
+};
+struct GnBwdArgs {
+    const void *dy, *x, *dres;
+    void* dx;
+    long lddy, ldx, lddres, lddx;
+    const float *gamma, *beta, *mean, *rstd;
+    float *dgamma, *dbeta, *ws;
+    int act;
+
+    GnShape s;
+    long exact;
+    int extra;
+};
+// floats of ws, and the workgroups of a launch
+long groupnorm_ws(long images, long pixels, int C, int G);
+long groupnorm_bwd_ws(long images, long pixels, int C, int G);
+long groupnorm_wgs(long images, long pixels, int C, int G);
+hipError_t launch_groupnorm(int dt, GnArgs p, long images, long pixels, int C, int G, hipStream_t st);
+hipError_t launch_groupnorm_bwd(int dt, GnBwdArgs p, long images, long pixels, int C, int G, hipStream_t st);
 
 }  // namespace lpp

@@ -12,45 +12,9 @@
 #include "act8.h"
 #include "kernels.h"
 #include "launch.h"
+#include "rowred.h"
 
 namespace lpp {
-
-// v + its value on a lane that DPP control CTRL names
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float v) {
-    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true));
-}
-
-// sum over the TPR threads of a row; all of them get it.  TPR <= 64: lanes of one
-// wave, through VALU lane permutes (quad, half-row and row mirrors, then swaps of 16-
-// and 32-lane halves).  Above: the wave sums meet in LDS (two slots in turn, so that one
-// barrier a sum is enough).
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* slots, int& turn) {
-    v = dpp_add<0xB1>(v);
-    if constexpr (TPR > 2) v = dpp_add<0x4E>(v);
-    if constexpr (TPR > 4) v = dpp_add<0x141>(v);
-    if constexpr (TPR > 8) v = dpp_add<0x140>(v);
-    if constexpr (TPR > 16) {
-        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    }
-    if constexpr (TPR > 32) {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    }
-    if constexpr (TPR > 64) {
-        constexpr int W = TPR / 64;
-        float* s = slots + turn * W;
-        turn ^= 1;
-        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.f;
-#pragma unroll
-        for (int w = 0; w < W; ++w) v += s[w];
-    }
-    return v;
-}
 
 // a thread's gammas: V from channel ch on, 0 past the row
 template <int V>

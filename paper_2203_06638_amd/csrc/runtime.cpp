@@ -2469,7 +2469,7 @@ int lpp_kernel_average(float* const* replicas, int n_rep, long n, void* stream) 
 }  // extern "C"
 
 // ------------------------------------------------------------------------
-// Stand-alone operators on caller buffers: 8-bit checkpoints, RMS norm
+// Stand-alone operators on caller buffers: 8-bit checkpoints, norms, top logits, distillation
 
 namespace {
 int elem_size(int dtype) { return dtype == LPP_BF16 ? 2 : 4; }
@@ -2619,6 +2619,190 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* a, void* stream) {
     if (e == hipSuccess && a->dgamma && parts > 1)
         e = lpp::launch_part_sums(a->ws, parts, a->cols, a->dgamma, (hipStream_t)stream);
     if (e != hipSuccess) return fail(LPP_EHIP, std::string("rmsnorm_bwd: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+static const char* bad_groups(long images, long pixels, int channels, int groups) {
+    if (images < 0 || pixels < 1 || channels < 1 || channels > (1 << 24)) return "images must be at least 0, pixels and channels at least 1";
+    if (groups < 1 || channels % groups) return "groups must divide channels";
+    if (pixels > (1L << 40) / channels || images > (1L << 40) / (pixels * channels)) return "the matrix must be under 2^40 elements";
+    return nullptr;
+}
+
+long lpp_groupnorm_ws(long images, long pixels, int channels, int groups) {
+    if (bad_groups(images, pixels, channels, groups)) return -1;
+    return lpp::groupnorm_ws(images, pixels, channels, groups);
+}
+
+int lpp_kernel_groupnorm(const lpp_groupnorm_args* a, void* stream) {
+    if (!a) return fail(LPP_EINVAL, "args is NULL");
+    if (const char* e = bad_groups(a->images, a->pixels, a->channels, a->groups)) return fail(LPP_EINVAL, e);
+    if (a->act < LPP_ACT_NONE || a->act > LPP_ACT_SILU) return fail(LPP_EINVAL, "unknown activation function");
+    if (!(a->eps >= 0.f) || !std::isfinite(a->eps)) return fail(LPP_EINVAL, "eps must be >= 0 and finite");
+    const long rows = a->images * a->pixels;
+    if (const char* e = bad_matrix(a->x, a->dtype, rows, a->channels, a->ldx)) return fail(LPP_EINVAL, e);
+    if (const char* e = bad_matrix(a->y, a->dtype, rows, a->channels, a->ldy)) return fail(LPP_EINVAL, e);
+    if (!a->gamma || !a->beta || ((uintptr_t)a->gamma | (uintptr_t)a->beta | (uintptr_t)a->mean | (uintptr_t)a->rstd) % 4)
+        return fail(LPP_EINVAL, "gamma, beta, mean and rstd must be buffers of floats");
+    const long need = lpp::groupnorm_ws(a->images, a->pixels, a->channels, a->groups);
+    if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
+        return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_groupnorm_ws floats");
+    if (lpp::groupnorm_wgs(a->images, a->pixels, a->channels, a->groups) >= (1L << 31) - 1)
+        return fail(LPP_EUNSUPPORTED, "too many images for one launch");
+    lpp::GnArgs p{};
+    p.x = a->x;
+    p.y = a->y;
+    p.ldx = a->ldx;
+    p.ldy = a->ldy;
+    p.gamma = a->gamma;
+    p.beta = a->beta;
+    p.mean = a->mean;
+    p.rstd = a->rstd;
+    p.ws = a->ws;
+    p.act = a->act;
+    p.eps = a->eps;
+    hipError_t e = lpp::launch_groupnorm(a->dtype, p, a->images, a->pixels, a->channels, a->groups, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("groupnorm: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+long lpp_groupnorm_bwd_ws(long images, long pixels, int channels, int groups) {
+    if (bad_groups(images, pixels, channels, groups)) return -1;
+    return lpp::groupnorm_bwd_ws(images, pixels, channels, groups);
+}
+
+int lpp_kernel_groupnorm_bwd(const lpp_groupnorm_bwd_args* a, void* stream) {
+    if (!a) return fail(LPP_EINVAL, "args is NULL");
+    if (const char* e = bad_groups(a->images, a->pixels, a->channels, a->groups)) return fail(LPP_EINVAL, e);
+    if (a->act < LPP_ACT_NONE || a->act > LPP_ACT_SILU) return fail(LPP_EINVAL, "unknown activation function");
+    if (!a->dx && !a->dgamma && !a->dbeta && a->images > 0) return fail(LPP_EINVAL, "none of dx, dgamma and dbeta is wanted");
+    const long rows = a->images * a->pixels;
+    struct { const void* p; long ld; bool want; } m[] = {
+        {a->dy, a->lddy, true}, {a->x, a->ldx, true}, {a->dres, a->lddres, a->dres != nullptr},
+        {a->dx, a->lddx, a->dx != nullptr}};
+    for (auto& t : m)
+        if (t.want)
+            if (const char* e = bad_matrix(t.p, a->dtype, rows, a->channels, t.ld)) return fail(LPP_EINVAL, e);
+    if (!a->gamma || !a->beta || (rows > 0 && (!a->mean || !a->rstd)) ||
+        ((uintptr_t)a->gamma | (uintptr_t)a->beta | (uintptr_t)a->mean | (uintptr_t)a->rstd | (uintptr_t)a->dgamma |
+         (uintptr_t)a->dbeta) % 4)
+        return fail(LPP_EINVAL, "gamma, beta, mean, rstd, dgamma and dbeta must be buffers of floats");
+    const long need = lpp::groupnorm_bwd_ws(a->images, a->pixels, a->channels, a->groups);
+    if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
+        return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_groupnorm_bwd_ws floats");
+    if (lpp::groupnorm_wgs(a->images, a->pixels, a->channels, a->groups) >= (1L << 30))
+        return fail(LPP_EUNSUPPORTED, "too many images for one launch");
+    lpp::GnBwdArgs p{};
+    p.dy = a->dy;
+    p.x = a->x;
+    p.dres = a->dres;
+    p.dx = a->dx;
+    p.lddy = a->lddy;
+    p.ldx = a->ldx;
+    p.lddres = a->lddres;
+    p.lddx = a->lddx;
+    p.gamma = a->gamma;
+    p.beta = a->beta;
+    p.mean = a->mean;
+    p.rstd = a->rstd;
+    p.dgamma = a->dgamma;
+    p.dbeta = a->dbeta;
+    p.ws = a->ws;
+    p.act = a->act;
+    hipError_t e = lpp::launch_groupnorm_bwd(a->dtype, p, a->images, a->pixels, a->channels, a->groups,
+                                             (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("groupnorm_bwd: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+static const char* bad_logits(long rows, int classes, int k) {
+    if (rows < 0 || classes < 1 || k < 1) return "rows must be at least 0, classes and k at least 1";
+    if (classes > (1 << 24) || rows > (1L << 40) / classes) return "at most 2^24 classes, and the matrix under 2^40 elements";
+    return nullptr;
+}
+
+long lpp_top_logits_ws(long rows, int classes, int k) {
+    if (bad_logits(rows, classes, k) || k > std::min(classes, lpp::kDistillMaxK)) return -1;
+    return lpp::top_logits_ws(rows, classes, k);
+}
+
+int lpp_kernel_top_logits(const lpp_top_logits_args* a, void* stream) {
+    if (!a) return fail(LPP_EINVAL, "args is NULL");
+    if (const char* e = bad_logits(a->rows, a->classes, a->k)) return fail(LPP_EINVAL, e);
+    if (a->k > a->classes) return fail(LPP_EINVAL, "k is more than the classes");
+    if (a->k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
+    if (const char* e = bad_matrix(a->z, a->dtype, a->rows, a->classes, a->ldz)) return fail(LPP_EINVAL, e);
+    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature))
+        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if ((a->rows > 0 && (!a->values || !a->index)) ||
+        ((uintptr_t)a->values | (uintptr_t)a->index | (uintptr_t)a->rest) % 4)
+        return fail(LPP_EINVAL, "values, index and rest must be buffers of floats and ints");
+    const long need = lpp::top_logits_ws(a->rows, a->classes, a->k);
+    if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
+        return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_top_logits_ws floats");
+    if (lpp::top_logits_wgs(a->rows, a->classes, a->k) >= (1L << 31) - 1)
+        return fail(LPP_EUNSUPPORTED, "too many rows for one launch");
+    lpp::TopArgs p{};
+    p.z = a->z;
+    p.ldz = a->ldz;
+    p.rows = a->rows;
+    p.C = a->classes;
+    p.k = a->k;
+    p.temp = a->temperature;
+    p.values = a->values;
+    p.index = a->index;
+    p.rest = a->rest;
+    p.ws = a->ws;
+    hipError_t e = lpp::launch_top_logits(a->dtype, p, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("top_logits: ") + hipGetErrorString(e));
+    return LPP_OK;
+}
+
+long lpp_distill_ws(long rows, int classes) {
+    if (bad_logits(rows, classes, 1)) return -1;
+    return lpp::distill_ws(rows, classes);
+}
+
+int lpp_kernel_distill(const lpp_distill_args* a, void* stream) {
+    if (!a) return fail(LPP_EINVAL, "args is NULL");
+    if (const char* e = bad_logits(a->rows, a->classes, a->k)) return fail(LPP_EINVAL, e);
+    if (a->k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
+    if (const char* e = bad_matrix(a->z, a->dtype, a->rows, a->classes, a->ldz)) return fail(LPP_EINVAL, e);
+    if (a->dz)
+        if (const char* e = bad_matrix(a->dz, a->dtype, a->rows, a->classes, a->lddz)) return fail(LPP_EINVAL, e);
+    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature))
+        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (!(a->alpha >= 0.f && a->alpha <= 1.f)) return fail(LPP_EINVAL, "alpha must be in [0, 1]");
+    if (!std::isfinite(a->scale)) return fail(LPP_EINVAL, "scale must be finite");
+    if ((a->rows > 0 && (!a->values || !a->index || !a->loss)) ||
+        ((uintptr_t)a->values | (uintptr_t)a->index | (uintptr_t)a->rest | (uintptr_t)a->labels |
+         (uintptr_t)a->weight | (uintptr_t)a->loss) % 4)
+        return fail(LPP_EINVAL, "values, index, rest, labels, weight and loss must be buffers of floats and ints");
+    const long need = lpp::distill_ws(a->rows, a->classes);
+    if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
+        return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_distill_ws floats");
+    if (lpp::top_logits_wgs(a->rows, a->classes, 1) >= (1L << 31) - 1)
+        return fail(LPP_EUNSUPPORTED, "too many rows for one launch");
+    lpp::DistillArgs p{};
+    p.z = a->z;
+    p.dz = a->dz;
+    p.ldz = a->ldz;
+    p.lddz = a->lddz;
+    p.rows = a->rows;
+    p.C = a->classes;
+    p.k = a->k;
+    p.values = a->values;
+    p.index = a->index;
+    p.rest = a->rest;
+    p.labels = a->labels;
+    p.weight = a->weight;
+    p.loss = a->loss;
+    p.alpha = a->alpha;
+    p.temp = a->temperature;
+    p.scale = a->scale;
+    p.ws = a->ws;
+    hipError_t e = lpp::launch_distill(a->dtype, p, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(LPP_EHIP, std::string("distill: ") + hipGetErrorString(e));
     return LPP_OK;
 }
 

@@ -21,6 +21,7 @@ CONV, BN, RELU, ADD, MAXPOOL, GAP, LINEAR, CONCAT, RMSNORM = range(9)
 FP32, BF16 = 0, 1
 SEQUENTIAL, ASYNC = 0, 1
 ACT8 = 0x100
+ACT_NONE, ACT_RELU, ACT_SILU = range(3)
 OK, EINVAL, ENOMEM, EHIP, ESTATE, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 STATUS = {0: "LPP_OK", -1: "LPP_EINVAL", -2: "LPP_ENOMEM", -3: "LPP_EHIP", -4: "LPP_ESTATE", -5: "LPP_EUNSUPPORTED"}
 
@@ -77,6 +78,36 @@ class RmsNormBwdArgs(C.Structure):
                 ("lddy", C.c_long), ("ldh", C.c_long), ("lddres", C.c_long), ("lddx", C.c_long),
                 ("gamma", C.c_void_p), ("rstd", C.c_void_p), ("dgamma", C.c_void_p), ("ws", C.c_void_p),
                 ("ws_floats", C.c_long), ("rows", C.c_long), ("cols", C.c_int), ("dtype", C.c_int)]
+
+
+class GroupNormArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("ldx", C.c_long), ("ldy", C.c_long), ("gamma", C.c_void_p),
+                ("beta", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p), ("ws", C.c_void_p),
+                ("ws_floats", C.c_long), ("images", C.c_long), ("pixels", C.c_long), ("channels", C.c_int),
+                ("groups", C.c_int), ("dtype", C.c_int), ("act", C.c_int), ("eps", C.c_float)]
+
+
+class GroupNormBwdArgs(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("x", C.c_void_p), ("dres", C.c_void_p), ("dx", C.c_void_p), ("lddy", C.c_long),
+                ("ldx", C.c_long), ("lddres", C.c_long), ("lddx", C.c_long), ("gamma", C.c_void_p),
+                ("beta", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p), ("dgamma", C.c_void_p),
+                ("dbeta", C.c_void_p), ("ws", C.c_void_p), ("ws_floats", C.c_long), ("images", C.c_long),
+                ("pixels", C.c_long), ("channels", C.c_int), ("groups", C.c_int), ("dtype", C.c_int),
+                ("act", C.c_int)]
+
+
+class TopLogitsArgs(C.Structure):
+    _fields_ = [("z", C.c_void_p), ("ldz", C.c_long), ("rows", C.c_long), ("classes", C.c_int), ("k", C.c_int),
+                ("dtype", C.c_int), ("temperature", C.c_float), ("values", C.c_void_p), ("index", C.c_void_p),
+                ("rest", C.c_void_p), ("ws", C.c_void_p), ("ws_floats", C.c_long)]
+
+
+class DistillArgs(C.Structure):
+    _fields_ = [("z", C.c_void_p), ("dz", C.c_void_p), ("ldz", C.c_long), ("lddz", C.c_long), ("rows", C.c_long),
+                ("classes", C.c_int), ("k", C.c_int), ("dtype", C.c_int), ("values", C.c_void_p),
+                ("index", C.c_void_p), ("rest", C.c_void_p), ("labels", C.c_void_p), ("weight", C.c_void_p),
+                ("loss", C.c_void_p), ("alpha", C.c_float), ("temperature", C.c_float), ("scale", C.c_float),
+                ("ws", C.c_void_p), ("ws_floats", C.c_long)]
 
 
 class ModelInfo(C.Structure):
@@ -139,6 +170,14 @@ def lib():
             "lpp_kernel_rmsnorm": ([C.POINTER(RmsNormArgs), C.c_void_p], C.c_int),
             "lpp_rmsnorm_bwd_ws": ([C.c_long, C.c_int], C.c_long),
             "lpp_kernel_rmsnorm_bwd": ([C.POINTER(RmsNormBwdArgs), C.c_void_p], C.c_int),
+            "lpp_groupnorm_ws": ([C.c_long, C.c_long, C.c_int, C.c_int], C.c_long),
+            "lpp_kernel_groupnorm": ([C.POINTER(GroupNormArgs), C.c_void_p], C.c_int),
+            "lpp_groupnorm_bwd_ws": ([C.c_long, C.c_long, C.c_int, C.c_int], C.c_long),
+            "lpp_kernel_groupnorm_bwd": ([C.POINTER(GroupNormBwdArgs), C.c_void_p], C.c_int),
+            "lpp_top_logits_ws": ([C.c_long, C.c_int, C.c_int], C.c_long),
+            "lpp_kernel_top_logits": ([C.POINTER(TopLogitsArgs), C.c_void_p], C.c_int),
+            "lpp_distill_ws": ([C.c_long, C.c_int], C.c_long),
+            "lpp_kernel_distill": ([C.POINTER(DistillArgs), C.c_void_p], C.c_int),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -366,7 +405,7 @@ def kernel_snapshot_noalloc(convs, d, dtype, wbuf_elems, x, v, wbuf, stream=None
                                              wbuf.data_ptr(), _stream_handle(stream)))
 
 
-# -- 8-bit activation checkpoints and RMS norm on device tensors (include/lpp.h) --
+# -- 8-bit activation checkpoints, norms, top logits and distillation on device tensors (include/lpp.h) --
 # Matrices are 2-D float32 or bfloat16 tensors on the current device whose rows are
 # contiguous (any row distance); checkpoints are 1-D contiguous uint8 tensors of
 # act8_bytes(rows, cols) bytes; gamma, rstd, gradients of parameters and
@@ -522,3 +561,141 @@ def kernel_rmsnorm_bwd(dy, gamma, rstd, dx=None, dgamma=None, ws=None, h=None, q
     a = RmsNormBwdArgs(yp, hp, qp, rp, xp, ldy, ldh, ldr, ldx, _floats(gamma, cols, "gamma", dev),
                        _floats(rstd, rows, "rstd", dev), gp, wp, wn, rows, cols, dt)
     _check(lib().lpp_kernel_rmsnorm_bwd(C.byref(a), _stream_handle(stream)))
+
+
+def _groups(f, images, pixels, channels, groups):
+    n = f(images, pixels, channels, groups) if max(channels, groups) <= 1 << 24 else -1
+    _need(n >= 0, "images must be at least 0, pixels and channels at least 1, groups must divide channels, and the "
+                  "matrix be under 2^40 elements")
+    return n
+
+
+def groupnorm_ws(images, pixels, channels, groups):
+    """Floats of the workspace of kernel_groupnorm."""
+    return _groups(lib().lpp_groupnorm_ws, images, pixels, channels, groups)
+
+
+def groupnorm_bwd_ws(images, pixels, channels, groups):
+    """Floats of the workspace of kernel_groupnorm_bwd."""
+    return _groups(lib().lpp_groupnorm_bwd_ws, images, pixels, channels, groups)
+
+
+def _pixels(rows, images, channels, groups):
+    """Pixels of an image."""
+    _need(images >= 0 and (rows % images == 0 and rows >= images if images else rows == 0),
+          "the rows must be images * pixels")
+    _need(1 <= groups <= channels and channels % groups == 0, "groups must divide the channels")
+    return rows // images if images else 1
+
+
+def kernel_groupnorm(x, images, groups, gamma, beta, y, mean=None, rstd=None, ws=None, eps=1e-5, act=ACT_NONE,
+                     stream=None):
+    """y = act(group norm of x): x [images * pixels][channels]; mean, rstd [images][groups];
+    ws: groupnorm_ws(images, pixels, channels, groups) floats (None where that is 0)."""
+    dev = _current_device(x)
+    xp, ldx, dt, shape = _matrix(x, "x", dev)
+    rows, ch = shape
+    pixels = _pixels(rows, images, ch, groups)
+    yp, ldy = _matrix(y, "y", dev, (shape, dt))[:2]
+    mp = _floats(mean, images * groups, "mean", dev) if mean is not None else None
+    rp = _floats(rstd, images * groups, "rstd", dev) if rstd is not None else None
+    wp, wn = (_floats(ws, 0, "ws", dev), ws.numel()) if ws is not None else (None, 0)
+    a = GroupNormArgs(xp, yp, ldx, ldy, _floats(gamma, ch, "gamma", dev), _floats(beta, ch, "beta", dev), mp, rp, wp, wn,
+                      images, pixels, ch, groups, dt, act, eps)
+    _check(lib().lpp_kernel_groupnorm(C.byref(a), _stream_handle(stream)))
+
+
+def kernel_groupnorm_bwd(dy, x, images, groups, gamma, beta, mean, rstd, dx=None, dgamma=None, dbeta=None, ws=None,
+                         dres=None, act=ACT_NONE, stream=None):
+    """Gradient of kernel_groupnorm from its x, mean and rstd: dx (+ dres), dgamma and dbeta;
+    ws: groupnorm_bwd_ws(images, pixels, channels, groups) floats (None where that is 0)."""
+    dev = _current_device(dy)
+    yp, ldy, dt, shape = _matrix(dy, "dy", dev)
+    rows, ch = shape
+    pixels = _pixels(rows, images, ch, groups)
+    like = (shape, dt)
+    xp, ldx = _matrix(x, "x", dev, like)[:2]
+    ep = dp = gp = bp = wp = None
+    lde = ldd = wn = 0
+    if dres is not None:
+        ep, lde = _matrix(dres, "dres", dev, like)[:2]
+    if dx is not None:
+        dp, ldd = _matrix(dx, "dx", dev, like)[:2]
+    if dgamma is not None:
+        gp = _floats(dgamma, ch, "dgamma", dev)
+    if dbeta is not None:
+        bp = _floats(dbeta, ch, "dbeta", dev)
+    if ws is not None:
+        wp, wn = _floats(ws, 0, "ws", dev), ws.numel()
+    a = GroupNormBwdArgs(yp, xp, ep, dp, ldy, ldx, lde, ldd, _floats(gamma, ch, "gamma", dev),
+                         _floats(beta, ch, "beta", dev), _floats(mean, images * groups, "mean", dev),
+                         _floats(rstd, images * groups, "rstd", dev), gp, bp, wp, wn, images, pixels, ch, groups, dt, act)
+    _check(lib().lpp_kernel_groupnorm_bwd(C.byref(a), _stream_handle(stream)))
+
+
+def _ints(t, n, what, dev):
+    if t.dtype != _TORCH.int32 or not t.is_contiguous() or t.numel() < n or t.get_device() != dev:
+        raise LppError(EINVAL, "%s must be a contiguous int32 tensor of at least %d elements on the current device"
+                       % (what, n))
+    return t.data_ptr()
+
+
+def _list(values, index, rows, dev):
+    """(pointers, k) of a teacher's list."""
+    _need(values.dim() == 2 and values.shape[0] == rows and index.shape == values.shape and values.shape[1] <= 1 << 24,
+          "values and index must be [rows][k]")
+    return _floats(values, 0, "values", dev), _ints(index, 0, "index", dev), values.shape[1]
+
+
+def top_logits_ws(rows, classes, k):
+    """Floats of the workspace of kernel_top_logits."""
+    n = lib().lpp_top_logits_ws(rows, classes, k) if max(classes, k) <= 1 << 24 else -1
+    _need(n >= 0, "rows must be at least 0, k in [1, min(classes, 128)], at most 2^24 classes, and the matrix under "
+                  "2^40 elements")
+    return n
+
+
+def kernel_top_logits(z, values, index, rest=None, temperature=1.0, ws=None, stream=None):
+    """The k largest logits of each row of z [rows][classes] into values and index
+    [rows][k], and the log of the sum of exp(z / temperature) over the others into rest [rows];
+    ws: top_logits_ws(rows, classes, k) floats (None where that is 0)."""
+    dev = _current_device(z)
+    p, ld, dt, (rows, classes) = _matrix(z, "z", dev)
+    vp, ip, k = _list(values, index, rows, dev)
+    rp = _floats(rest, rows, "rest", dev) if rest is not None else None
+    wp, wn = (_floats(ws, 0, "ws", dev), ws.numel()) if ws is not None else (None, 0)
+    a = TopLogitsArgs(p, ld, rows, classes, k, dt, temperature, vp, ip, rp, wp, wn)
+    _check(lib().lpp_kernel_top_logits(C.byref(a), _stream_handle(stream)))
+
+
+def distill_ws(rows, classes):
+    """Floats of the workspace of kernel_distill."""
+    n = lib().lpp_distill_ws(rows, classes) if classes <= 1 << 24 else -1
+    _need(n >= 0, "rows must be at least 0, classes in [1, 2^24], and the matrix under 2^40 elements")
+    return n
+
+
+def kernel_distill(z, values, index, loss, dz=None, rest=None, labels=None, weight=None, alpha=1.0, temperature=1.0,
+                   scale=1.0, ws=None, stream=None):
+    """The loss [rows] of logits z [rows][classes] against a teacher's list values, index [rows][k]
+    and rest [rows] (share alpha) and labels [rows], and dz = scale times its gradient;
+    ws: distill_ws(rows, classes) floats (None where that is 0)."""
+    dev = _current_device(z)
+    p, ld, dt, shape = _matrix(z, "z", dev)
+    rows, classes = shape
+    vp, ip, k = _list(values, index, rows, dev)
+    dp = ep = lp = hp = wp = None
+    ldd = wn = 0
+    if dz is not None:
+        dp, ldd = _matrix(dz, "dz", dev, (shape, dt))[:2]
+    if rest is not None:
+        ep = _floats(rest, rows, "rest", dev)
+    if labels is not None:
+        lp = _ints(labels, rows, "labels", dev)
+    if weight is not None:
+        hp = _floats(weight, rows, "weight", dev)
+    if ws is not None:
+        wp, wn = _floats(ws, 0, "ws", dev), ws.numel()
+    a = DistillArgs(p, dp, ld, ldd, rows, classes, k, dt, vp, ip, ep, lp, hp, _floats(loss, rows, "loss", dev), alpha,
+                    temperature, scale, wp, wn)
+    _check(lib().lpp_kernel_distill(C.byref(a), _stream_handle(stream)))
