@@ -14,7 +14,6 @@
 // Sums are float32 in a fixed order.  exp(x) is taken as 2^(x log2 e) of x <= 0, whose
 // relative error grows with |x| while its share of a sum falls as e^x.
 #include <algorithm>
-#include <type_traits>
 
 #include "act8.h"
 #include "kernels.h"
@@ -29,9 +28,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A thread's chunks of a row: NC of them, chunk c at value (c * TPR + t) * V of the piece
-// [c0, c1) of classes.  Values behind the end are -inf.
+// [c0, c1) of classes.
 template <typename T, int TPR, int NC>
-struct RowValues {
+struct RowChunks {
     static constexpr int V = 16 / (int)sizeof(T);
     u4 w[NC];
     __device__ __forceinline__ void load(const T* row, int c0, int c1, int t, bool exact) {
@@ -41,35 +40,58 @@ struct RowValues {
             w[c] = ld_chunk(row + (n > 0 ? ch : c0), n, exact);
         }
     }
+    // Converted values are not to be kept from one pass over the chunks to the next: twice the
+    // registers, and half the workgroups.
+    __device__ __forceinline__ void again() {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(w[c]));
+    }
+    // the values of chunk c, -inf behind the end
     __device__ __forceinline__ void get(int c, int c0, int c1, int t, float* v) const {
         const int n = c1 - (c0 + (c * TPR + t) * V);
         chunk_values<T>(w[c], v);
+        if (n >= V) return;
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = j < n ? v[j] : -INFINITY;
     }
 };
+// the larger of two, NaN if one is
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+enum RowMode { WHOLE, PIECE_SUMS, PIECE_GRAD };
 
 // ---- distillation ------------------------------------------------------------
 
 // LDS of a row: the list (classes, teacher's values and then probabilities, student's
-// logits; the label behind it), and a bit for each class of the piece that is listed
-__host__ __device__ inline int distill_lds(int k, int values) { return 3 * (k + 1) + (values + 31) / 32; }
-
+// logits, whether a class is listed before; the label behind it), four results, and a bit for
+// each class of the piece that is listed
+__host__ __device__ inline int distill_lds(int k, int values) { return 4 * (k + 1) + 4 + (values + 31) / 32; }
 constexpr int kListPitch = kDistillMaxK + 4;   // floats of a row's list in the workspace
 
-enum DistillMode { WHOLE, PIECE_SUMS, PIECE_GRAD };
+// Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
+// other, are covered by other rows.
+constexpr int distill_waves(int values, bool both) {
+    return both ? (values <= 16 ? 5 : values <= 40 ? 4 : 2) : values <= 32 ? 6 : 4;
+}
 
 // WHOLE: a row to TPR threads, in their registers, so that z is read once.  PIECE_SUMS: a
-// workgroup takes a piece of a row and leaves its largest value and its three sums;
-// PIECE_GRAD: the loss, and the gradient of its piece, from all pieces' sums.
-template <typename T, int TPR, int NC, int MODE, bool ST>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void distill_k(DistillArgs p) {
+// workgroup takes a piece of a row and leaves its largest value and its sums; PIECE_GRAD: the
+// loss, and the gradient of its piece, from all pieces' sums.
+// The listed classes and the label are taken out of the row (set to -inf) and have their
+// parts of the sums, and their gradients, from the list, which the row's first wave
+// works on: its teacher's side while the row is on its way, its student's side between
+// the sums and the gradient.  BOTH: exp(z) and exp(z / T) are both wanted; they stay in
+// registers from the sums to the gradient.
+template <typename T, int TPR, int NC, int MODE, bool BOTH, bool ST>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int)sizeof(T), BOTH)) void distill_k(DistillArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
-    __shared__ float slots[2 * (TB / 64)];
+    constexpr int LW = TPR < 64 ? TPR : 64;      // lanes that work on the list
+    __shared__ float slots[4 * (TB / 64)];
     extern __shared__ float lds[];
-    int turn = 0;
+    int turn = 0, none = 0;
     const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR;
+    const bool lead = t < LW;
     long r = MODE == WHOLE ? (long)blockIdx.x * RB + rl : blockIdx.x / p.grid_pieces;
     const bool ok = r < p.rows;
     if (!ok) r = p.rows - 1;
@@ -84,186 +106,212 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void distill_k(DistillArgs p
     const int* labels = step ? step->labels : p.labels;
     const float w = p.weight ? p.weight[r] : 1.f;
     const bool use1 = labels && alpha < 1.f, useT = alpha > 0.f, tail = rests && useT;
-    const float iT = 1.f / temp, e1 = kLog2e, eT = kLog2e * iT;
+    // (BOTH not set: one temperature serves both, the other's terms have no weight or T = 1)
+    const float iT = 1.f / temp, e1 = kLog2e, eT = !BOTH && !useT ? kLog2e : kLog2e * iT;
     const T* z = (const T*)p.z + r * p.ldz;
-
-    RowValues<T, TPR, NC> x;
-    x.load(z, c0, c1, t, r >= p.exact);
 
     // the list; entry k is the label
     float* at = lds + rl * distill_lds(p.lds_k, TPR * NC * V);
     int* cls = (int*)at;
-    float *pr = at + (k + 1), *zc = at + 2 * (k + 1);
-    uint32_t* mask = (uint32_t*)(at + 3 * (k + 1));
-    for (int e = t; e <= k; e += TPR) {
-        int c = e < k ? (useT ? index[r * k + e] : -1) : (use1 ? labels[r] : -1);
-        if ((unsigned)c >= (unsigned)p.C) c = -1;
-        cls[e] = c;
-        pr[e] = e < k && c >= 0 ? values[r * k + e] * iT : -INFINITY;
-        // (dz may be z: the pieces' workgroups keep z at the listed classes for each other)
-        float* kept = p.ws + 4 * p.rows * p.pieces + r * kListPitch;
-        if (MODE == PIECE_GRAD) zc[e] = c >= 0 ? kept[e] : 0.f;
-        else zc[e] = c >= 0 ? ld1(z, c) : 0.f;
-        if (MODE == PIECE_SUMS && c >= c0 && c < c1) kept[e] = zc[e];
-    }
-    if (MODE != PIECE_GRAD && tail) {
-        for (int e = t; e < (TPR * NC * V + 31) / 32; e += TPR) mask[e] = 0u;
-        row_sync<TPR>();
-        for (int e = t; e < k; e += TPR) {
-            const int c = cls[e] - c0;
-            if (cls[e] >= 0 && c >= 0 && c < c1 - c0) atomicOr(&mask[c >> 5], 1u << (c & 31));
+    float *pr = at + (k + 1), *zc = at + 2 * (k + 1), *out = at + 4 * (k + 1);
+    int* again = (int*)(at + 3 * (k + 1));
+    uint32_t* mask = (uint32_t*)(out + 4);
+    float rest = -INFINITY;
+    if (lead) {
+        for (int e = t; e <= k; e += LW) {
+            int c = e < k ? (useT ? index[r * k + e] : -1) : (use1 ? labels[r] : -1);
+            if ((unsigned)c >= (unsigned)p.C) c = -1;
+            cls[e] = c;
+            pr[e] = e < k && c >= 0 ? values[r * k + e] * iT : -INFINITY;
         }
+        if (tail) rest = rests[r];
     }
+    RowChunks<T, TPR, NC> x;
+    if (MODE != PIECE_GRAD || p.dz) x.load(z, c0, c1, t, r >= p.exact);
+    for (int e = t; e < (TPR * NC * V + 31) / 32; e += TPR) mask[e] = 0u;
+    row_sync<TPR>();
+    float tm = rest, ts = 0.f;
+    if (lead) {
+        bool bad = rest != rest;      // (a maximum drops a NaN)
+        for (int e = t; e <= k; e += LW) {
+            const int c = cls[e];
+            // (dz may be z: the pieces' workgroups keep z at the listed classes for each other)
+            float* kept = p.ws + 4 * p.rows * p.pieces + r * kListPitch;
+            float v = 0.f;
+            if (c >= 0) v = MODE == PIECE_GRAD ? kept[e] : ld1(z, c);
+            zc[e] = v;
+            if (MODE == PIECE_SUMS && c >= c0 && c < c1) kept[e] = v;
+            if (c >= c0 && c < c1) atomicOr(&mask[(c - c0) >> 5], 1u << ((c - c0) & 31));
+            if (MODE == PIECE_SUMS) continue;
+            int seen = 0;
+#pragma unroll 4
+            for (int o = 0; o < e; ++o) seen |= cls[o] == c;
+            again[e] = seen;
+            tm = fmaxf(tm, pr[e]);
+            bad |= pr[e] != pr[e];
+        }
+        // the teacher's probabilities
+        tm = row_max<LW>(tm, slots, none);
+        for (int e = t; e < k; e += LW) ts += cls[e] >= 0 && tm > -INFINITY ? pow2((pr[e] - tm) * kLog2e) : 0.f;
+        ts = row_sum<LW>(bad ? NAN : ts, slots, none) + (rest > -INFINITY ? pow2((rest - tm) * kLog2e) : 0.f);
+    }
+    // (a list without an entry, or of -inf alone, says nothing)
+    const bool some = useT && !(tm == -INFINITY && ts == ts);
     row_sync<TPR>();
 
-    // largest value, and the sums of exp(z - m), exp((z - m) / T) and the latter's over
-    // the classes that are not listed
-    float m, s1 = 0.f, sT = 0.f, so = 0.f;
+    // the row, then its exponentials: a of z / T (of z where only that is wanted), b of z
+    float a[NC][V], b[BOTH ? NC : 1][V];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        x.get(c, c0, c1, t, a[c]);
+        const int i = (c * TPR + t) * V;
+        const uint32_t gone = mask[i >> 5] >> (i & 31) & ((1u << V) - 1u);
+        if (gone)
+#pragma unroll
+            for (int j = 0; j < V; ++j) a[c][j] = (gone >> j) & 1u ? -INFINITY : a[c][j];
+    }
+    // largest value, and the sums of exp(z - m) and exp((z - m) / T) over the classes that are
+    // not listed
+    float m = -INFINITY, s1 = 0.f, so = 0.f;
+    const f4* all = (const f4*)p.ws + r * p.pieces;
     if (MODE == PIECE_GRAD) {
-        const f4* all = (const f4*)p.ws + r * p.pieces;
-        m = -INFINITY;
         for (int e = t; e < p.pieces; e += TPR) m = fmaxf(m, all[e][0]);
-        m = row_max<TPR>(m, slots, turn);
-        for (int e = t; e < p.pieces; e += TPR) {
-            const f4 s = all[e];
-            s1 += s[1] * pow2((s[0] - m) * e1);
-            sT += s[2] * pow2((s[0] - m) * eT);
-            so += s[3] * pow2((s[0] - m) * eT);
-        }
     } else {
-        m = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            float v[V];
-            x.get(c, c0, c1, t, v);
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < V; ++j) m = fmaxf(m, v[j]);
-        }
-        m = row_max<TPR>(m, slots, turn);
-        // (a piece of nothing but -inf: sums of 0)
-        const float base = MODE == PIECE_SUMS && m == -INFINITY ? 0.f : m;
+            for (int j = 0; j < V; ++j) m = fmaxf(m, a[c][j]);
+    }
+    if (MODE != PIECE_SUMS && lead)
+        for (int e = t; e <= k; e += LW) m = fmaxf(m, cls[e] >= 0 ? zc[e] : -INFINITY);
+    m = row_max<TPR>(m, slots, turn);
+    // (a piece of nothing but -inf: sums of 0)
+    const float base = MODE == PIECE_SUMS && m == -INFINITY ? 0.f : m;
+    if (MODE != PIECE_GRAD || p.dz) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            float v[V];
-            x.get(c, c0, c1, t, v);
-            const int i = (c * TPR + t) * V;
-            const uint32_t listed = tail ? mask[i >> 5] >> (i & 31) : 0u;
-            const int n = c1 - c0 - i;
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = v[j] - base;
-                if (use1) s1 += j < n ? pow2(d * e1) : 0.f;
-                const float e = j < n ? pow2(d * eT) : 0.f;
-                sT += e;
-                so += (listed >> j) & 1u ? 0.f : e;
+                const float d = a[c][j] - base;
+                if constexpr (BOTH) {
+                    b[c][j] = pow2(d * e1);
+                    if (MODE != PIECE_GRAD) s1 += b[c][j];
+                }
+                a[c][j] = pow2(d * eT);
+                if (MODE != PIECE_GRAD) so += a[c][j];
             }
-        }
     }
-    s1 = row_sum<TPR>(s1, slots, turn);
-    sT = row_sum<TPR>(sT, slots, turn);
-    so = row_sum<TPR>(so, slots, turn);
+    if (MODE == PIECE_GRAD)
+        for (int e = t; e < p.pieces; e += TPR) {
+            const f4 s = all[e];
+            if (BOTH) s1 += s[1] * pow2((s[0] - m) * e1);
+            so += s[2] * pow2((s[0] - m) * eT);
+        }
+    if (BOTH) row_sum2<TPR>(s1, so, slots, turn);
+    else so = row_sum<TPR>(so, slots, turn);
     if (MODE == PIECE_SUMS) {
-        if (t == 0) ((f4*)p.ws)[r * p.pieces + piece] = f4{m, s1, sT, so};
+        if (t == 0) ((f4*)p.ws)[r * p.pieces + piece] = f4{m, s1, so, 0.f};
         return;
     }
 
-    // the teacher's probabilities
-    const float rest = tail ? rests[r] : -INFINITY;
-    float tm = rest;
-    for (int e = t; e < k; e += TPR) tm = fmaxf(tm, pr[e]);
-    tm = row_max<TPR>(tm, slots, turn);
-    float ts = 0.f;
-    bool bad = rest != rest;      // (row_max drops a NaN)
-    for (int e = t; e < k; e += TPR) {
-        bad |= pr[e] != pr[e];
-        ts += cls[e] >= 0 && tm > -INFINITY ? pow2((pr[e] - tm) * kLog2e) : 0.f;
-    }
-    ts = row_sum<TPR>(bad ? NAN : ts, slots, turn) + (rest > -INFINITY ? pow2((rest - tm) * kLog2e) : 0.f);
-    // (a list without an entry, or of -inf alone, says nothing)
-    const bool some = useT && !(tm == -INFINITY && ts == ts);
-    const float lt = logf(ts), lq = logf(sT);
-    for (int e = t; e < k; e += TPR) {
-        const float d = pr[e] - tm;
-        // (log p where the row sums need it: pr holds p from here on, zc of an entry stays)
-        pr[e] = cls[e] >= 0 && some ? pow2(d * kLog2e) / ts : 0.f;
-    }
-    row_sync<TPR>();
-
-    float soft = 0.f, sp = 0.f, sq = 0.f;
-    for (int e = t; e < k; e += TPR) {
-        const int c = cls[e];
-        if (c < 0 || !some) continue;
-        bool first = true;
-        for (int o = 0; o < e; ++o) first &= cls[o] != c;
-        const float pe = pr[e], u = (zc[e] - m) * iT - lq, q = pow2(u * kLog2e);
-        const float d = (values[r * k + e] * iT - tm) - lt - u;
-        sp += pe;
-        if (first) sq += q;
-        if (tail) {
-            // both sides' probabilities add up to 1: p log(p / q) - p + q in place of
-            // p log(p / q) keeps the sum exact where p is near q
-            if (pe > 0.f) soft += !first ? pe * d - pe : d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + q;
-            else if (pe != pe) soft = pe;
-            else if (first) soft += q;
-        } else if (pe != 0.f) {
-            soft += pe * d;
-        }
-    }
-    soft = row_sum<TPR>(soft, slots, turn);
-    float others = 1.f / sT;      // what gT times exp((z - m) / T) of a class that is not listed has
-    if (tail) {
-        sp = row_sum<TPR>(sp, slots, turn);
-        sq = row_sum<TPR>(sq, slots, turn);
-        const float q = so / sT, pe = some ? (rest > -INFINITY ? pow2((rest - tm) * kLog2e) / ts : 0.f) : 0.f;
-        if (some) {
-            const float d = (rest - tm) - lt - logf(q);
-            if (pe > 0.f) soft += d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + q;
-            else soft += q;
-        }
-        // q - p of the rest is p - q of the list, which is the smaller and so the more
-        // exact of the two where the rest is large
-        others = so != 0.f ? (pe > 0.5f ? sp - sq : q - pe) / so : 0.f;
-    }
+    // the student's side of the list
     const int y = cls[k];
     const float a1 = use1 ? 1.f - alpha : 0.f, aT = some ? alpha * temp : 0.f;
-    if (t == 0 && ok && piece == 0) {
-        float l = 0.f;
-        if (y >= 0 && use1) l += a1 * (logf(s1) - (zc[k] - m));
-        if (some) l += aT * temp * soft;
-        p.loss[r] = w != 0.f ? w * l : 0.f;
-    }
-    if (!p.dz) return;
     const float g1 = y >= 0 && use1 ? p.scale * w * a1 : 0.f, gT = p.scale * w * aT;
     const bool live = w != 0.f && (g1 != 0.f || gT != 0.f);   // (a row without a loss has no gradient, whatever it holds)
-    const float k1 = g1 != 0.f ? g1 / s1 : 0.f, kT = gT != 0.f ? gT * others : 0.f;
+    float sT = 0.f, kT = 0.f;
+    if (lead) {
+        // what the listed classes add: once each, the label's to the first sum (and to the
+        // other classes' of the second, if it is not listed)
+        float l1 = 0.f, lT = 0.f, ly = 0.f;
+        for (int e = t; e <= k; e += LW) {
+            if (cls[e] < 0 || again[e]) continue;
+            const float d = zc[e] - m, q = pow2(d * eT);
+            if (BOTH) l1 += pow2(d * e1);
+            if (e < k) lT += q;
+            else ly = q;
+        }
+        row_sum2<LW>(lT, ly, slots, none);
+        if (BOTH) s1 += row_sum<LW>(l1, slots, none);
+        so += ly;
+        sT = so + lT;
+        if (!BOTH) s1 = sT;
+        const float lt = logf(ts), lq = logf(sT);
+        float soft = 0.f, sp = 0.f;
+        for (int e = t; e < k; e += LW) {
+            if (cls[e] < 0 || !some) {
+                pr[e] = 0.f;
+                continue;
+            }
+            const float v = pr[e] - tm, pe = pow2(v * kLog2e) / ts, u = (zc[e] - m) * iT - lq, d = v - lt - u;
+            pr[e] = pe;
+            sp += pe;
+            if (tail) {
+                // both sides' probabilities add up to 1: p log(p / q) - p + q in place of
+                // p log(p / q) keeps the sum exact where p is near q
+                if (pe > 0.f)
+                    soft += again[e] ? pe * d - pe : d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + pow2(u * kLog2e);
+                else if (pe != pe) soft = pe;
+                else if (!again[e]) soft += pow2(u * kLog2e);
+            } else if (pe != 0.f) {
+                soft += pe * d;
+            }
+        }
+        row_sum2<LW>(soft, sp, slots, none);
+        float others = 1.f / sT;      // what gT times exp((z - m) / T) of a class that is not listed has
+        if (tail) {
+            const float q = so / sT, pe = some && rest > -INFINITY ? pow2((rest - tm) * kLog2e) / ts : 0.f;
+            if (some) {
+                const float d = (rest - tm) - lt - logf(q);
+                if (pe > 0.f) soft += d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + q;
+                else soft += q;
+            }
+            // q - p of the rest is p - q of the list, which is the smaller and so the more
+            // exact of the two where the rest is large
+            others = so != 0.f ? (pe > 0.5f ? sp - lT / sT : q - pe) / so : 0.f;
+        }
+        kT = gT != 0.f ? gT * others : 0.f;
+        if (t == 0) {
+            if (ok && piece == 0) {
+                float l = 0.f;
+                if (y >= 0 && use1) l += a1 * (logf(s1) - (zc[k] - m));
+                if (some) l += aT * temp * soft;
+                p.loss[r] = w != 0.f ? w * l : 0.f;
+            }
+            out[0] = g1 != 0.f ? g1 / s1 : 0.f;
+            out[1] = kT;
+            out[2] = live ? 1.f : 0.f;
+        }
+    }
+    if (!p.dz) return;
+    row_sync<TPR>();
     T* dz = (T*)p.dz + r * p.lddz;
+    const float k1 = out[0];
+    kT = out[1];
+    const bool wanted = out[2] != 0.f;
     // (dz may be z: what the list needs of z was read above, before a barrier)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        float v[V];
-        x.get(c, c0, c1, t, v);
         const int ch = c0 + (c * TPR + t) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float d = v[j] - m;
-            float g = 0.f;
-            if (use1) g = k1 * pow2(d * e1);
-            if (useT) g = __builtin_fmaf(kT, pow2(d * eT), g);
-            v[j] = live ? g : 0.f;
+            const float g = BOTH ? __builtin_fmaf(kT, a[c][j], k1 * b[c][j]) : (kT + k1) * a[c][j];
+            a[c][j] = wanted ? g : 0.f;
         }
-        if (ok) st_chunk<ST>(dz + ch, c1 - ch, v);
+        if (ok) st_chunk<ST>(dz + ch, c1 - ch, a[c]);
     }
     row_sync<TPR>();
-    for (int e = t; e <= k; e += TPR) {
+    if (!lead || !ok || !live) return;
+    for (int e = t; e <= k; e += LW) {
         const int c = cls[e];
-        if (c < c0 || c >= c1 || !ok || !live) continue;
+        if (c < c0 || c >= c1) continue;
         float pe = 0.f;
         bool listed = false;
-        for (int o = 0; o < k; ++o)
-            if (cls[o] == c) {
-                pe += pr[o];
-                listed = true;
-            }
+#pragma unroll 4
+        for (int o = 0; o < k; ++o) {
+            pe += cls[o] == c ? pr[o] : 0.f;
+            listed |= cls[o] == c;
+        }
         const float d = zc[e] - m, q = pow2(d * eT);
         float g = g1 != 0.f ? g1 * (pow2(d * e1) / s1 - (c == y ? 1.f : 0.f)) : 0.f;
         if (gT != 0.f) g += listed || !tail ? gT * (q / sT - pe) : kT * q;
@@ -310,54 +358,84 @@ __device__ __forceinline__ u64 row_max64(u64 v, u64* slots) {
 template <int TPR>
 constexpr int kCandidates = TPR <= 16 ? 128 : TPR <= 64 ? 256 : 1024;
 
-// The k largest of the keys that TPR threads hold; each(f) calls f(key) for those of a
-// thread.  emit(i, key) takes the i-th; returns the k-th, 0 where there are fewer keys.
-//
-// The k-th largest of the threads' own maxima is a bound that at least k keys reach, and
-// few more: T threads with random values leave about T ln(T / (T - k)).  Those go to LDS,
-// where each is placed by counting the larger ones.  Values laid out against the
-// threads can leave too many; then the k largest are taken one by one.
+// LDS of a row
+template <int TPR>
+struct TopSpace {
+    u64 cand[kCandidates<TPR>];
+    u64 border;
+    int count;
+    __device__ __forceinline__ void add(u64 key) {
+        const int i = atomicAdd(&count, 1);
+        if (i < kCandidates<TPR>) cand[i] = key;
+    }
+};
+// The k largest of the m candidates, each placed by counting the larger ones: emit(i, key)
+// takes the i-th.  Returns the k-th, 0 where there are fewer; next: the (k + 1)-th or 0.
+template <int TPR, class Emit>
+__device__ __forceinline__ u64 rank_candidates(int k, int t, int m, TopSpace<TPR>& s, u64& next, Emit emit) {
+    if (t == 0) s.border = 0;
+    row_sync<TPR>();
+    u64 mine = 0;
+    for (int i = t; i < m; i += TPR) {
+        const u64 key = s.cand[i];
+        int larger = 0;
+#pragma unroll 4
+        for (int o = 0; o < m; ++o) larger += s.cand[o] > key;
+        if (larger < k) emit(larger, key);
+        if (larger == k - 1) s.border = key;
+        if (larger == k) mine = key;
+    }
+    row_sync<TPR>();
+    const u64 border = s.border;
+    row_sync<TPR>();
+    if (mine) s.border = mine;
+    else if (t == 0 && m <= k) s.border = 0;
+    row_sync<TPR>();
+    next = s.border;
+    return border;
+}
+
+// The same of the keys that TPR threads hold, whatever they are; each(f) calls f(key) for
+// those of a thread.  The k-th largest of the threads' own maxima is a bound that at least
+// k keys reach, k exactly where all values are equal.  Keys laid out against the threads can
+// leave too many; then the k largest are taken one by one.
 template <int TPR, class Each, class Emit>
-__device__ __forceinline__ u64 top_keys(int k, int t, u64* cand, int* count, u64* border, u64* slots, Each each,
-                                        Emit emit) {
-    constexpr int N = kCandidates<TPR>;
+__device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slots, u64& next, Each each, Emit emit) {
+    constexpr int H = TPR < 256 ? TPR : 256;     // threads whose maxima are compared
     u64 best = 0;
     each([&](u64 key) { best = key > best ? key : best; });
-    if (t == 0) *count = 0, *border = 0;
-    u64 bound = 0;
-    if (k < TPR) {
-        cand[t] = best;
-        row_sync<TPR>();
-        int larger = 0;
-        for (int o = 0; o < TPR; ++o) larger += cand[o] > best;
-        if (larger == k - 1 && best) *border = best;     // (keys differ: one thread, or none)
-        row_sync<TPR>();
-        bound = *border;
+    u64 lead = best;
+    for (int d = H; d < TPR; d *= 2) {           // (TPR / H neighbours' maxima as one)
+        const u64 o = shfl_xor64(lead, d / H);
+        lead = o > lead ? o : lead;
     }
+    row_sync<TPR>();
+    if (t == 0) s.count = 0, s.border = 0;
+    if (t % (TPR / H) == 0) s.cand[t / (TPR / H)] = lead;
+    row_sync<TPR>();
+    if (t < H) {
+        const u64 mine = s.cand[t];
+        int larger = 0;
+        for (int o = 0; o < H; ++o) larger += s.cand[o] > mine;
+        if (larger == k - 1 && mine) s.border = mine;     // (keys differ: one thread, or none)
+    }
+    row_sync<TPR>();
+    const u64 bound = s.border;
     row_sync<TPR>();
     if (best >= bound)
         each([&](u64 key) {
-            if (key < bound || !key) return;
-            const int i = atomicAdd(count, 1);
-            if (i < N) cand[i] = key;
+            if (key >= bound && key) s.add(key);
         });
-    if (t == 0) *border = 0;
     row_sync<TPR>();
-    const int m = *count;
-    if (m <= N) {
-        for (int i = t; i < m; i += TPR) {
-            const u64 key = cand[i];
-            int larger = 0;
-            for (int o = 0; o < m; ++o) larger += cand[o] > key;
-            if (larger < k) emit(larger, key);
-            if (larger == k - 1) *border = key;
-        }
-        row_sync<TPR>();
-        return *border;
-    }
+    const int m = s.count;
+    if (m <= kCandidates<TPR>) return rank_candidates<TPR>(k, t, m, s, next, emit);
     u64 last = 0;
-    for (int i = 0; i < k; ++i) {
+    for (int i = 0; i <= k; ++i) {
         const u64 top = row_max64<TPR>(best, slots);
+        if (i == k) {
+            next = top;
+            break;
+        }
         if (best == top) {
             if (top) emit(i, top);
             best = 0;
@@ -374,39 +452,98 @@ __device__ __forceinline__ u64 top_keys(int k, int t, u64* cand, int* count, u64
 // base m where that is finite
 __device__ __forceinline__ float rest_base(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
 
+// Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
+// other, are covered by other rows.
+constexpr int top_waves(int values) { return values <= 40 ? 6 : 4; }
+
+// Rows of a few candidates are finished by their first wave: the others are gone by then.
+constexpr int kFew = 256;
+
 // WHOLE: a row to TPR threads.  PIECE_SUMS: a workgroup takes a piece of a row and leaves
 // the piece's k largest keys, the largest of the others and their sum.
-template <typename T, int TPR, int NC, int MODE>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void top_logits_k(TopArgs p) {
+//
+// The row is cut into G groups of neighbouring threads' values.  The k-th largest of the
+// groups' maxima is a bound that at least k values reach, and few more: about
+// G ln(G / (G - k)) of random ones.  Those go to LDS, and the values under the bound are
+// summed, relative to it; then the first wave places the candidates.  Where too many reach
+// the bound (equal values, or values laid out against the threads) top_keys takes over, and
+// where the values under it add up to less than 1, so that the bound may lie far above them,
+// they are summed again relative to their largest.
+template <typename T, int TPR, int NC, int MODE, int G>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves(NC * 16 / (int)sizeof(T))) void top_logits_k(TopArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
-    __shared__ u64 cands[RB][kCandidates<TPR>], borders[RB], slots[TB / 64];
-    __shared__ int counts[RB];
+    constexpr int LW = TPR < 64 ? TPR : 64;
+    __shared__ TopSpace<TPR> spaces[RB];
+    __shared__ u64 slots[TB / 64];
+    __shared__ __attribute__((aligned(16))) float maxima[RB][G];
     __shared__ float fslots[2 * (TB / 64)];
-    int turn = 0;
+    int turn = 0, none = 0;
     const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR;
+    TopSpace<TPR>& space = spaces[rl];
     long r = MODE == WHOLE ? (long)blockIdx.x * RB + rl : blockIdx.x / p.pieces;
     const bool ok = r < p.rows;
     if (!ok) r = p.rows - 1;
     const int piece = MODE == WHOLE ? 0 : (int)(blockIdx.x - r * p.pieces);
     const int c0 = piece * p.piece, c1 = min(p.C, c0 + p.piece);
-    RowValues<T, TPR, NC> x;
+    RowChunks<T, TPR, NC> x;
     x.load((const T*)p.z + r * p.ldz, c0, c1, t, r >= p.exact);
-    auto each = [&](auto f) {
+    float top[NC], best = -INFINITY;      // of the chunks, of the thread; NaN is the largest
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            float v[V];
-            x.get(c, c0, c1, t, v);
+    for (int c = 0; c < NC; ++c) {
+        float v[V];
+        x.get(c, c0, c1, t, v);
+        top[c] = v[0];
+#pragma unroll
+        for (int j = 1; j < V; ++j) top[c] = max_nan(top[c], v[j]);
+        best = max_nan(best, top[c]);
+    }
+    best = best != best ? INFINITY : best;
+#pragma unroll
+    for (int d = 1; d < TPR / G; d *= 2) best = fmaxf(best, __shfl_xor(best, d));
+    if (t % (TPR / G) == 0) maxima[rl][t / (TPR / G)] = best;
+    if (t == 0) space.count = 0;
+    row_sync<TPR>();
+    float bound;
+    {
+        // (up to 64 groups every wave finds it by itself)
+        const float mine = maxima[rl][t % G];
+        int larger = 0;
+#pragma unroll 4
+        for (int o = 0; o < G; o += 4) {
+            const f4 v = *(const f4*)&maxima[rl][o];
+            larger += (v[0] > mine) + (v[1] > mine) + (v[2] > mine) + (v[3] > mine);
+        }
+        bound = larger < p.k ? -mine : -INFINITY;
+        if constexpr (G <= 64) bound = -row_max<(G < LW ? G : LW)>(bound, fslots, none);
+        else bound = -row_max<TPR>(bound, fslots, turn);
+    }
+    const float eT = kLog2e / p.temp;
+    const float base0 = rest_base(bound);
+    float s = 0.f;
+    x.again();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        float v[V];
+        x.get(c, c0, c1, t, v);
+        if (!(top[c] < bound)) {
             const int ch = c0 + (c * TPR + t) * V;
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (ch + j < c1) f(rank_key(v[j], ch + j));
+            for (int j = 0; j < V; ++j) {
+                if (v[j] < bound) continue;
+                if (ch + j < c1) space.add(rank_key(v[j], ch + j));
+                v[j] = -INFINITY;
+            }
         }
-    };
+        if (p.rest)
+#pragma unroll
+            for (int j = 0; j < V; ++j) s += pow2((v[j] - base0) * eT);
+    }
+    s = row_sum<TPR>(s, fslots, turn);     // (its barrier is the candidates' too)
+    row_sync<LW>();
+    const int n = space.count;
     u64* keys = MODE == WHOLE ? nullptr : (u64*)p.ws + (r * p.pieces + piece) * p.k;
-    if (MODE == PIECE_SUMS)
-        for (int i = c1 - c0 + t; i < p.k; i += TPR) keys[i] = 0;
-    const u64 border = top_keys<TPR>(p.k, t, cands[rl], &counts[rl], &borders[rl], slots, each, [&](int i, u64 key) {
+    auto emit = [&](int i, u64 key) {
         if (!ok) return;
         if (MODE == WHOLE) {
             p.values[r * p.k + i] = key_value(key);
@@ -414,122 +551,238 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void top_logits_k(TopArgs p)
         } else {
             keys[i] = key;
         }
-    });
+    };
+    auto give = [&](float m, float base, float sum) {     // (the others' largest value, their sum relative to base)
+        if (t || !ok) return;
+        if (MODE == WHOLE) p.rest[r] = base / p.temp + logf(sum);
+        else ((f4*)((u64*)p.ws + (p.rows * p.pieces * p.k + 1) / 2 * 2))[r * p.pieces + piece] = f4{m, base, sum, 0.f};
+    };
+    if (n <= kFew && ((s >= 1.f && s < INFINITY && fabsf(bound) < INFINITY) || !p.rest)) {
+        if (t >= LW) return;
+        if (MODE == PIECE_SUMS)
+            for (int i = n + t; i < p.k; i += LW) keys[i] = 0;
+        // the candidates that are not among the k are others too: relative to the largest
+        // of them, at least the bound
+        float lead = -INFINITY;
+        int place[kFew / LW];
+#pragma unroll
+        for (int q = 0; q < kFew / LW; ++q) {
+            const int i = q * LW + t;
+            place[q] = 0;
+            if (q * LW >= n) continue;
+            const u64 key = space.cand[min(i, n - 1)];
+            int larger = 0;
+#pragma unroll 4
+            for (int o = 0; o < n; ++o) larger += space.cand[o] > key;
+            place[q] = larger;
+            if (i >= n) continue;
+            if (larger < p.k) emit(larger, key);
+            else lead = fmaxf(lead, key_value(key));
+        }
+        if (!p.rest) return;
+        lead = row_max<LW>(lead, fslots, none);
+        const float base = lead > bound ? rest_base(lead) : base0;
+        float more = 0.f;
+#pragma unroll
+        for (int q = 0; q < kFew / LW; ++q) {
+            const int i = q * LW + t;
+            if (i < n && place[q] >= p.k) more += pow2((key_value(space.cand[i]) - base) * eT);
+        }
+        more = row_sum<LW>(more, fslots, none);
+        give(fmaxf(lead, bound), base, s * pow2((base0 - base) * eT) + more);
+        return;
+    }
+    // (rows that come here are few: they are read again, for registers that the others have)
+    const T* z = (const T*)p.z + r * p.ldz;
+    auto each = [&](auto f) {
+#pragma unroll 1
+        for (int c = 0; c < NC; ++c) {
+            const int ch = c0 + (c * TPR + t) * V;
+            if (ch >= c1) break;
+            float v[V];
+            chunk_values<T>(ld_chunk(z + ch, c1 - ch, r >= p.exact), v);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (ch + j < c1) f(rank_key(v[j], ch + j));
+        }
+    };
+    if (MODE == PIECE_SUMS)
+        for (int i = c1 - c0 + t; i < p.k; i += TPR) keys[i] = 0;
+    u64 next;
+    const u64 border = n <= kCandidates<TPR> ? rank_candidates<TPR>(p.k, t, n, space, next, emit)
+                                             : top_keys<TPR>(p.k, t, space, slots, next, each, emit);
     if (!p.rest) return;
-    const float eT = kLog2e / p.temp;
-    float m = -INFINITY, s = 0.f;
-    each([&](u64 key) {
-        if (key < border) m = fmaxf(m, key_value(key));
-    });
+    float m = -INFINITY;
+    s = 0.f;
+    each([&](u64 key) { m = key < border ? fmaxf(m, key_value(key)) : m; });
     m = row_max<TPR>(m, fslots, turn);
     const float base = rest_base(m);
-    each([&](u64 key) {
-        if (key < border) s += pow2((key_value(key) - base) * eT);
-    });
-    s = row_sum<TPR>(s, fslots, turn);
-    if (t || !ok) return;
-    if (MODE == WHOLE) p.rest[r] = base / p.temp + logf(s);
-    else ((float2*)((u64*)p.ws + p.rows * p.pieces * p.k))[r * p.pieces + piece] = float2{m, s};
+    each([&](u64 key) { s += key < border ? pow2((key_value(key) - base) * eT) : 0.f; });
+    give(m, base, row_sum<TPR>(s, fslots, turn));
 }
 
-// A row's answer from its pieces'.
-__global__ __launch_bounds__(256) void top_merge_k(TopArgs p) {
-    __shared__ u64 cand[kCandidates<256>], border_s, slots[4];
-    __shared__ int count;
-    __shared__ float fslots[8];
+// A row's answer from its pieces' lists, which are in descending order.  With j = 2 k / P
+// (P pieces) at least k keys reach the ceil(k / j)-th largest of the pieces' j-th keys.
+constexpr int kMergeThreads = 1024, kMergeKeys = 4;
+__global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
+    constexpr int TPR = kMergeThreads;
+    __shared__ TopSpace<TPR> space;
+    __shared__ u64 slots[TPR / 64];
+    __shared__ float fslots[2 * TPR / 64];
     int turn = 0;
     const int t = threadIdx.x;
     const long r = blockIdx.x;
     const u64* keys = (const u64*)p.ws + r * p.pieces * p.k;
-    const long n = (long)p.pieces * p.k;
+    const f4* part = (const f4*)((const u64*)p.ws + (p.rows * p.pieces * p.k + 1) / 2 * 2) + r * p.pieces;
+    const int n = p.pieces * p.k;
+    const int jth = min(p.k, (2 * p.k + p.pieces - 1) / p.pieces), nth = (p.k + jth - 1) / jth;
+    u64 v[kMergeKeys];
+#pragma unroll
+    for (int u = 0; u < kMergeKeys; ++u) v[u] = u * TPR + t < n ? keys[u * TPR + t] : 0;
+    f4 mine = t < p.pieces ? part[t] : f4{-INFINITY, 0.f, 0.f, 0.f};
+    u64 bound = 0;
+    const bool few = p.pieces <= 64;
+    if (few && t < p.pieces) {
+        bound = keys[(long)t * p.k + jth - 1];
+        space.cand[t] = bound;
+    }
+    if (t == 0) space.count = 0, space.border = 0;
+    __syncthreads();
+    if (few && t < p.pieces) {
+        int larger = 0;
+        for (int o = 0; o < p.pieces; ++o) larger += space.cand[o] > bound;
+        if (larger == nth - 1) space.border = bound;     // (equal ones are 0: no bound)
+    }
+    __syncthreads();
+    bound = space.border;
+    __syncthreads();
     auto each = [&](auto f) {
-        for (long i = t; i < n; i += 256)
+#pragma unroll
+        for (int u = 0; u < kMergeKeys; ++u)
+            if (v[u]) f(v[u]);
+        for (int i = kMergeKeys * TPR + t; i < n; i += TPR)
             if (keys[i]) f(keys[i]);
     };
-    const u64 border = top_keys<256>(p.k, t, cand, &count, &border_s, slots, each, [&](int i, u64 key) {
+    each([&](u64 key) {
+        if (key >= bound) space.add(key);
+    });
+    __syncthreads();
+    auto emit = [&](int i, u64 key) {
         p.values[r * p.k + i] = key_value(key);
         p.index[r * p.k + i] = (int)~(uint32_t)key;
-    });
+    };
+    u64 next;
+    const int m0 = space.count;
+    const u64 border = m0 <= kCandidates<TPR> ? rank_candidates<TPR>(p.k, t, m0, space, next, emit)
+                                              : top_keys<TPR>(p.k, t, space, slots, next, each, emit);
     if (!p.rest) return;
-    const float2* part = (const float2*)((const u64*)p.ws + p.rows * p.pieces * p.k) + r * p.pieces;
     const float eT = kLog2e / p.temp;
-    float m = -INFINITY, s = 0.f;
-    each([&](u64 key) {
-        if (key < border) m = fmaxf(m, key_value(key));
-    });
-    for (int i = t; i < p.pieces; i += 256) m = fmaxf(m, part[i].x);
-    m = row_max<256>(m, fslots, turn);
+    float m = mine[0], s = 0.f;
+    each([&](u64 key) { m = key < border ? fmaxf(m, key_value(key)) : m; });
+    for (int i = t + TPR; i < p.pieces; i += TPR) m = fmaxf(m, part[i][0]);
+    m = row_max<TPR>(m, fslots, turn);
     const float base = rest_base(m);
-    each([&](u64 key) {
-        if (key < border) s += pow2((key_value(key) - base) * eT);
-    });
-    for (int i = t; i < p.pieces; i += 256) s += part[i].y * pow2((rest_base(part[i].x) - base) * eT);
-    s = row_sum<256>(s, fslots, turn);
+    each([&](u64 key) { s += key < border ? pow2((key_value(key) - base) * eT) : 0.f; });
+    for (int i = t; i < p.pieces; i += TPR) {
+        if (i >= TPR) mine = part[i];
+        s += mine[2] != 0.f ? mine[2] * pow2((mine[1] - base) * eT) : 0.f;
+    }
+    s = row_sum<TPR>(s, fslots, turn);
     if (t == 0) p.rest[r] = base / p.temp + logf(s);
 }
 
 // ---- plans -------------------------------------------------------------------
 
-// Threads of a row and chunks of a thread; rows of more than kWholeChunks chunks are cut
-// into pieces of at most kPieceChunks.
+// Threads of a row and chunks of a thread.  Rows that the registers of 512 threads do not
+// hold are cut into pieces.
 struct RowPlan {
     int tpr, nc;
     int pieces, piece;    // piece: classes
 };
-constexpr int kPieceChunks = 256 * 8;
-RowPlan row_plan(int V, int C, int k) {
-    const int chunks = (C + V - 1) / V;
+// values that a thread keeps at most, and chunks of the longest row that is not cut
+constexpr int kThreadValues = 64;
+RowPlan row_plan(int V, long rows, int C, int k) {
+    const int chunks = (C + V - 1) / V, most = kThreadValues / V;
     if (chunks <= 16 && k < 16) return {16, 1, 1, C};
     if (k <= 32)
         for (int nc : {1, 2, 4})
             if (chunks <= 64 * nc) return {64, nc, 1, C};
-    for (int nc : {2, 4, 8})
+    for (int nc : {1, 2, 4})
         if (chunks <= 256 * nc) return {256, nc, 1, C};
-    const int pieces = (chunks + kPieceChunks - 1) / kPieceChunks;
+    for (int nc : {3, 4, 5, 6, 8, 12, 16})
+        if (nc <= most && chunks <= 512 * nc) return {512, nc, 1, C};
+    // 256 workgroups with two chunks a thread at least, or as few as hold the row
+    const long want = std::min<long>((256 + rows - 1) / std::max(rows, 1L), chunks / 512);
+    const int pieces = (int)std::max<long>(want, (chunks + 256 * 8 - 1) / (256 * 8));
     const int per = (chunks + pieces - 1) / pieces;
-    return {256, 8, (chunks + per - 1) / per, per * V};
+    return {256, per <= 512 ? 2 : per <= 1024 ? 4 : 8, (chunks + per - 1) / per, per * V};
 }
 
 long exact_row(int dt, long rows, int C, long ld) {
     return rows - (dt == DT_BF16 ? tail_rows<bf16>(rows, C, ld) : tail_rows<float>(rows, C, ld));
 }
 
-template <typename T, int TPR, int NC, int MODE, typename P>
-void row_launch(const P& p, long wgs, hipStream_t st) {
+template <typename T, int TPR, int NC, int MODE>
+void row_launch(const TopArgs& p, long wgs, hipStream_t st) {
+    const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
+    if constexpr (TPR <= 64) launch((top_logits_k<T, TPR, NC, MODE, TPR>), grid, block, 0, st, p);
+    else if (p.k <= 32) launch((top_logits_k<T, TPR, NC, MODE, 64>), grid, block, 0, st, p);
+    else launch((top_logits_k<T, TPR, NC, MODE, 256>), grid, block, 0, st, p);
+}
+template <typename T, int TPR, int NC, int MODE>
+void row_launch(const DistillArgs& p, long wgs, hipStream_t st) {
     const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
     constexpr int V = 16 / (int)sizeof(T), RB = TPR > 256 ? 1 : 256 / TPR;
-    if constexpr (std::is_same<P, DistillArgs>::value) {
-        const unsigned lds = sizeof(float) * RB * distill_lds(p.lds_k, TPR * NC * V);
-        if (p.dz && p.rows * p.C * (long)sizeof(T) >= kStreamBytes)
-            launch((distill_k<T, TPR, NC, MODE, true>), grid, block, lds, st, p);
-        else
-            launch((distill_k<T, TPR, NC, MODE, false>), grid, block, lds, st, p);
-    } else {
-        launch((top_logits_k<T, TPR, NC, MODE>), grid, block, 0, st, p);
-    }
+    const unsigned lds = sizeof(float) * RB * distill_lds(p.lds_k, TPR * NC * V);
+    const bool both = p.step || (p.labels && p.alpha > 0.f && p.alpha < 1.f && p.temp != 1.f);
+    const bool stream = MODE != PIECE_SUMS && p.dz && p.rows * p.C * (long)sizeof(T) >= kStreamBytes;
+    if (both && stream) launch((distill_k<T, TPR, NC, MODE, true, MODE != PIECE_SUMS>), grid, block, lds, st, p);
+    else if (both) launch((distill_k<T, TPR, NC, MODE, true, false>), grid, block, lds, st, p);
+    else if (stream) launch((distill_k<T, TPR, NC, MODE, false, MODE != PIECE_SUMS>), grid, block, lds, st, p);
+    else launch((distill_k<T, TPR, NC, MODE, false, false>), grid, block, lds, st, p);
 }
 
 template <typename T, typename P>
 hipError_t whole_rows(const P& p, RowPlan s, hipStream_t st) {
-    const long wgs = (p.rows + (s.tpr < 256 ? 256 / s.tpr : 1) - 1) / (s.tpr < 256 ? 256 / s.tpr : 1);
-    switch (s.tpr * 16 + s.nc) {
-    case 16 * 16 + 1: row_launch<T, 16, 1, WHOLE>(p, wgs, st); break;
-    case 64 * 16 + 1: row_launch<T, 64, 1, WHOLE>(p, wgs, st); break;
-    case 64 * 16 + 2: row_launch<T, 64, 2, WHOLE>(p, wgs, st); break;
-    case 64 * 16 + 4: row_launch<T, 64, 4, WHOLE>(p, wgs, st); break;
-    case 256 * 16 + 2: row_launch<T, 256, 2, WHOLE>(p, wgs, st); break;
-    case 256 * 16 + 4: row_launch<T, 256, 4, WHOLE>(p, wgs, st); break;
-    case 256 * 16 + 8: row_launch<T, 256, 8, WHOLE>(p, wgs, st); break;
+    const int rb = s.tpr < 256 ? 256 / s.tpr : 1;
+    const long wgs = (p.rows + rb - 1) / rb;
+    switch (s.tpr * 32 + s.nc) {
+    case 16 * 32 + 1: row_launch<T, 16, 1, WHOLE>(p, wgs, st); break;
+    case 64 * 32 + 1: row_launch<T, 64, 1, WHOLE>(p, wgs, st); break;
+    case 64 * 32 + 2: row_launch<T, 64, 2, WHOLE>(p, wgs, st); break;
+    case 64 * 32 + 4: row_launch<T, 64, 4, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 1: row_launch<T, 256, 1, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 2: row_launch<T, 256, 2, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 4: row_launch<T, 256, 4, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 3: row_launch<T, 512, 3, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 4: row_launch<T, 512, 4, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 5: row_launch<T, 512, 5, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 6: row_launch<T, 512, 6, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 8: row_launch<T, 512, 8, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 12:
+        if constexpr (sizeof(T) == 4) row_launch<T, 512, 12, WHOLE>(p, wgs, st);
+        else return hipErrorInvalidValue;   // (row_plan: 64 values a thread)
+        break;
+    case 512 * 32 + 16:
+        if constexpr (sizeof(T) == 4) row_launch<T, 512, 16, WHOLE>(p, wgs, st);
+        else return hipErrorInvalidValue;
+        break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
+}
+template <typename T, int MODE, typename P>
+void piece_rows(const P& p, int nc, long wgs, hipStream_t st) {
+    if (nc == 2) row_launch<T, 256, 2, MODE>(p, wgs, st);
+    else if (nc == 4) row_launch<T, 256, 4, MODE>(p, wgs, st);
+    else row_launch<T, 256, 8, MODE>(p, wgs, st);
 }
 
 template <typename T>
 hipError_t top_rows(TopArgs p, RowPlan s, hipStream_t st) {
     if (s.pieces == 1) return whole_rows<T>(p, s, st);
-    row_launch<T, 256, 8, PIECE_SUMS>(p, p.rows * p.pieces, st);
-    launch(top_merge_k, dim3((unsigned)p.rows), dim3(256), 0, st, p);
+    piece_rows<T, PIECE_SUMS>(p, s.nc, p.rows * p.pieces, st);
+    launch(top_merge_k, dim3((unsigned)p.rows), dim3(kMergeThreads), 0, st, p);
     return hipGetLastError();
 }
 
@@ -537,29 +790,30 @@ template <typename T>
 hipError_t distill_rows(DistillArgs p, RowPlan s, hipStream_t st) {
     if (s.pieces == 1) return whole_rows<T>(p, s, st);
     p.grid_pieces = s.pieces;
-    row_launch<T, 256, 8, PIECE_SUMS>(p, p.rows * s.pieces, st);
+    piece_rows<T, PIECE_SUMS>(p, s.nc, p.rows * s.pieces, st);
     p.grid_pieces = p.dz ? s.pieces : 1;
-    row_launch<T, 256, 8, PIECE_GRAD>(p, p.rows * p.grid_pieces, st);
+    piece_rows<T, PIECE_GRAD>(p, s.nc, p.rows * p.grid_pieces, st);
     return hipGetLastError();
 }
 
 }  // namespace
 
-long top_logits_wgs(long rows, int C, int k) {
-    return rows * std::max(row_plan(4, C, k).pieces, row_plan(8, C, k).pieces);
+static long most_pieces(long rows, int C, int k) {
+    return std::max(row_plan(4, rows, C, k).pieces, row_plan(8, rows, C, k).pieces);
 }
+long top_logits_wgs(long rows, int C, int k) { return rows * most_pieces(rows, C, k); }
 long top_logits_ws(long rows, int C, int k) {
-    const long pieces = std::max(row_plan(4, C, k).pieces, row_plan(8, C, k).pieces);
-    return pieces > 1 ? rows * pieces * (2L * k + 2) : 0;
+    const long pieces = most_pieces(rows, C, k);
+    return pieces > 1 ? (rows * pieces * (2L * k) + 3) / 4 * 4 + rows * pieces * 4 : 0;
 }
 long distill_ws(long rows, int C) {
-    const long pieces = std::max(row_plan(4, C, 1).pieces, row_plan(8, C, 1).pieces);
+    const long pieces = most_pieces(rows, C, 1);
     return pieces > 1 ? rows * (4 * pieces + kListPitch) : 0;
 }
 
 hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.C, p.k);
+    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, p.k);
     p.exact = exact_row(dt, p.rows, p.C, p.ldz);
     p.pieces = s.pieces;
     p.piece = s.piece;
@@ -568,7 +822,7 @@ hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st) {
 
 hipError_t launch_distill(int dt, DistillArgs p, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.C, 1);
+    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, 1);
     p.exact = exact_row(dt, p.rows, p.C, p.ldz);
     p.pieces = s.pieces;
     p.piece = s.piece;

@@ -41,6 +41,30 @@ __device__ __forceinline__ float row_sum(float v, float* slots, int& turn) {
     return v;
 }
 
+// two sums at once: one barrier for both (slots: 4 * TPR / 64 of them)
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float* slots, int& turn) {
+    int none = 0;
+    a = row_sum<(TPR < 64 ? TPR : 64)>(a, slots, none);
+    b = row_sum<(TPR < 64 ? TPR : 64)>(b, slots, none);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        float* s = slots + turn * 2 * W;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) {
+            s[2 * (threadIdx.x >> 6)] = a;
+            s[2 * (threadIdx.x >> 6) + 1] = b;
+        }
+        __syncthreads();
+        a = b = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            a += s[2 * w];
+            b += s[2 * w + 1];
+        }
+    }
+}
+
 // LDS of a row between its TPR threads.  Up to 64 they are lanes of one wave, whose LDS
 // accesses are in order: only the compiler has to keep them so.  Rows of a workgroup may take
 // different branches then.
