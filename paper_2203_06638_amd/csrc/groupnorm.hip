@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "act8.h"
+#include "groupnorm.h"
 #include "kernels.h"
 #include "launch.h"
 
@@ -37,23 +38,6 @@ __device__ __forceinline__ void merge(Moments& a, float n, float mean, float m2)
     a.m2 += m2 + a.n * f * d * d;
     a.mean += d * f;
     a.n = sum;
-}
-
-template <int ACT>
-__device__ __forceinline__ float act_value(float z) {
-    if (ACT == ACT_RELU) return z > 0.f ? z : 0.f;
-    if (ACT == ACT_SILU) return z / (1.f + expf(-z));
-    return z;
-}
-// dy * act'(z)
-template <int ACT>
-__device__ __forceinline__ float act_grad(float dy, float z) {
-    if (ACT == ACT_RELU) return z > 0.f ? dy : 0.f;
-    if (ACT == ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-z));
-        return dy * (s * (1.f + z * (1.f - s)));
-    }
-    return dy;
 }
 
 // A workgroup's part of an activation: a split of an image's rows, a slab of its
@@ -82,17 +66,34 @@ struct Place {
         np = (c1 - 1) / s.cg - g0 + 1;   // groups that the slab meets
     }
 };
-// lanes (a power of two, one wave at most) that a workgroup has for each of n items
-__device__ __forceinline__ int item_lanes(int n) {
-    int l = 6;
-    while (l > 0 && (n << l) > TB) --l;
-    return l;
-}
 // slabs that group g lies in
 template <int V>
 __device__ __forceinline__ int first_slab(const GnShape& s, int g) { return g * s.cg / (V << s.lw); }
 template <int V>
 __device__ __forceinline__ int last_slab(const GnShape& s, int g) { return ((g + 1) * s.cg - 1) / (V << s.lw); }
+
+// f(split, slab, part) for every 2^ll-th of a group's parts, l the first: slabs sa .. sa + ns - 1 of
+// every split.  Four loads are under way at once.
+template <class F>
+__device__ __forceinline__ void each_part(const GnShape& s, const float2* ws, long image, int g, int sa, int ns, int l,
+                                          int ll, F f) {
+    const float2* in = ws + image * s.splits * s.parts + g + sa;
+    const int total = ns * s.splits;
+    for (int e0 = l; e0 < total; e0 += 4 << ll) {
+        float2 m[4];
+        int split[4], slab[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int e = min(e0 + (u << ll), total - 1);
+            split[u] = ns == 1 ? e : e / ns;
+            slab[u] = e - split[u] * ns;
+            m[u] = in[(long)split[u] * s.parts + slab[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (e0 + (u << ll) < total) f(split[u], sa + slab[u], m[u]);
+    }
+}
 
 // ---- forward -----------------------------------------------------------------
 
@@ -107,8 +108,8 @@ __global__ __launch_bounds__(TB) void gn_stats_k(GnArgs p) {
     const Place<V> at(p.s, blockIdx.x);
     const T* x = (const T*)p.x + at.ch;
     float k[V], s[V], ss[V];
-    const long first = min(at.r0 + at.rl, at.r1 - 1);
-    chunk_values<T>(ld_chunk(x + first * p.ldx, at.n, first >= p.exact), k);
+    const long lead = min(at.r0 + at.rl, at.r1 - 1);
+    chunk_values<T>(ld_chunk(x + lead * p.ldx, at.n, lead >= p.exact), k);
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = ss[j] = 0.f;
     auto add = [&](u4 w) {
@@ -141,29 +142,48 @@ __global__ __launch_bounds__(TB) void gn_stats_k(GnArgs p) {
         const float m2 = ss[j] == INFINITY ? ss[j] : ss[j] - e * (e * cnt);
         ss[j] = m2 < 0.f ? 0.f : m2;
     }
-    const int t = threadIdx.x, wave = t >> 6;
-    for (int d = 1 << p.s.lw; d < 64; d <<= 1) {
+    // the wave's rows: each merge halves the channels that a lane goes on with (as fold)
+    const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+    int d = 1 << p.s.lw, first = 0, n = V;
+#pragma unroll
+    for (int h = V / 2; h >= 1; h /= 2) {
+        if (d >= 64) continue;
+        const bool up = (lane & d) != 0;
         const float oc = __shfl_xor(cnt, d);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            Moments a{cnt, s[j], ss[j]};
-            merge(a, oc, __shfl_xor(s[j], d), __shfl_xor(ss[j], d));
-            s[j] = a.mean;
-            ss[j] = a.m2;
+        for (int j = 0; j < h; ++j) {
+            Moments m{cnt, up ? s[j + h] : s[j], up ? ss[j + h] : ss[j]};
+            const float mean = __shfl_xor(up ? s[j] : s[j + h], d), m2 = __shfl_xor(up ? ss[j] : ss[j + h], d);
+            merge(m, oc, mean, m2);
+            s[j] = m.mean;
+            ss[j] = m.m2;
         }
         cnt += oc;
+        first += up ? h : 0;
+        n = h;
+        d <<= 1;
     }
-    if ((t & 63) < 1 << p.s.lw) {
-        const int c = (t & ((1 << p.s.lw) - 1)) * V;
+    const int apart = d;       // lanes from here on repeat the channels of the lower ones
+    for (; d < 64; d <<= 1) {
+        Moments m{cnt, s[0], ss[0]};
+        const float oc = __shfl_xor(cnt, d), mean = __shfl_xor(s[0], d), m2 = __shfl_xor(ss[0], d);
+        merge(m, oc, mean, m2);
+        s[0] = m.mean;
+        ss[0] = m.m2;
+        cnt = m.n;
+    }
+    if (lane < apart) {
+        const int c = (t & ((1 << p.s.lw) - 1)) * V + first;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            sm[0][wave][c + j] = s[j];
-            sm[1][wave][c + j] = ss[j];
-        }
-        if ((t & 63) == 0) scnt[wave] = cnt;
+        for (int j = 0; j < V; ++j)
+            if (j < n) {
+                sm[0][wave][c + j] = s[j];
+                sm[1][wave][c + j] = ss[j];
+            }
+        if (lane == 0) scnt[wave] = cnt;
     }
     __syncthreads();
-    const int ll = item_lanes(at.np), l = t & ((1 << ll) - 1);
+    const int ll = item_lanes(TB, at.np), l = t & ((1 << ll) - 1);
     float2* out = (float2*)p.ws + (at.image * p.s.splits + at.split) * p.s.parts;
     for (int q = t >> ll; q < at.np; q += TB >> ll) {
         const int g = at.g0 + q;
@@ -188,17 +208,15 @@ __global__ __launch_bounds__(TB) void gn_apply_k(GnArgs p) {
     __shared__ float smean[64 * V], srstd[64 * V];
     const Place<V> at(p.s, blockIdx.x);
     const int t = threadIdx.x;
-    const int ll = item_lanes(at.np), l = t & ((1 << ll) - 1);
+    const int ll = item_lanes(TB, at.np), l = t & ((1 << ll) - 1);
     for (int q = t >> ll; q < at.np; q += TB >> ll) {
         const int g = at.g0 + q, sa = first_slab<V>(p.s, g), ns = last_slab<V>(p.s, g) - sa + 1;
         Moments a{0.f, 0.f, 0.f};
-        for (int e = l; e < ns * p.s.splits; e += 1 << ll) {
-            const int split = e / ns, slab = sa + e - split * ns;
+        each_part(p.s, (const float2*)p.ws, at.image, g, sa, ns, l, ll, [&](int split, int slab, float2 m) {
             const int lo = max(g * p.s.cg, slab * (V << p.s.lw)), hi = min((g + 1) * p.s.cg, (slab + 1) * (V << p.s.lw));
             const long rows = min((split + 1) * p.s.rps, p.s.pixels) - split * p.s.rps;
-            const float2 m = ((const float2*)p.ws)[(at.image * p.s.splits + split) * p.s.parts + g + slab];
             merge(a, (float)rows * (float)(hi - lo), m.x, m.y);
-        }
+        });
         for (int d = 1; d < 1 << ll; d <<= 1) {
             const float n = __shfl_xor(a.n, d), mean = __shfl_xor(a.mean, d), m2 = __shfl_xor(a.m2, d);
             merge(a, n, mean, m2);
@@ -302,19 +320,17 @@ __global__ __launch_bounds__(TB) void gn_bwd_sums_k(GnBwdArgs p) {
     }
     for (; r < at.r1; r += at.RL) add(ld_chunk(x + r * p.ldx, at.n, r >= p.exact), ld_chunk(dy + r * p.lddy, at.n, r >= p.exact));
     const int t = threadIdx.x, wave = t >> 6;
-    for (int d = 1 << p.s.lw; d < 64; d <<= 1)
+    int first, n;
+    fold<V>(a, p.s.lw, first, n);
+    fold<V>(b, p.s.lw, first, n);
+    {
+        const int c = (t & ((1 << p.s.lw) - 1)) * V + first;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            a[j] += __shfl_xor(a[j], d);
-            b[j] += __shfl_xor(b[j], d);
-        }
-    if ((t & 63) < 1 << p.s.lw) {
-        const int c = (t & ((1 << p.s.lw) - 1)) * V;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            sm[0][wave][c + j] = a[j];
-            sm[1][wave][c + j] = b[j];
-        }
+        for (int j = 0; j < V; ++j)
+            if (j < n) {
+                sm[0][wave][c + j] = a[j];
+                sm[1][wave][c + j] = b[j];
+            }
     }
     __syncthreads();
     const long row = at.image * p.s.splits + at.split;
@@ -333,7 +349,7 @@ __global__ __launch_bounds__(TB) void gn_bwd_sums_k(GnBwdArgs p) {
         sm[1][0][c] = sb * g;
     }
     __syncthreads();
-    const int ll = item_lanes(at.np), l = t & ((1 << ll) - 1);
+    const int ll = item_lanes(TB, at.np), l = t & ((1 << ll) - 1);
     float2* part = (float2*)p.ws + row * p.s.parts;
     for (int q = t >> ll; q < at.np; q += TB >> ll) {
         const int g = at.g0 + q;
@@ -351,28 +367,35 @@ __global__ __launch_bounds__(TB) void gn_bwd_sums_k(GnBwdArgs p) {
     }
 }
 
-// dgamma and dbeta: 64 columns of the channels' sums a workgroup, 16 threads to a
-// column, over all images and splits
+// dgamma and dbeta: kColumns columns of the channels' sums a workgroup, 32 threads to four
+// columns, over all images and splits
+constexpr int kColumns = TB / 32 * 4;
 __device__ void gn_columns(const GnBwdArgs& p, int block, float* sm) {
-    const int t = threadIdx.x, q = t & 15, l = t >> 4, col = block * 64 + q * 4;
+    const int t = threadIdx.x, q = t % (kColumns / 4), l = t / (kColumns / 4), col = block * kColumns + q * 4;
     const float* in = p.ws + p.s.sums + col;
     f4 a = f4{0.f, 0.f, 0.f, 0.f};
     if (col < 2 * p.s.cp) {
 #pragma unroll 4
-        for (long r = l; r < p.s.rows_ws; r += 16) a += *(const f4*)(in + r * 2 * p.s.cp);
+        for (long r = l; r < p.s.rows_ws; r += 32) a += *(const f4*)(in + r * 2 * p.s.cp);
     }
-    *(f4*)(sm + l * 64 + q * 4) = a;
+    *(f4*)(sm + l * kColumns + q * 4) = a;
     __syncthreads();
-    const int c = block * 64 + t;
-    if (t < 64 && c < 2 * p.s.cp) {
+    const int c = block * kColumns + t;
+    if (t < kColumns && c < 2 * p.s.cp) {
         float v = sm[t];
-        for (int k = 1; k < 16; ++k) v += sm[k * 64 + t];
+#pragma unroll
+        for (int k = 1; k < 32; ++k) v += sm[k * kColumns + t];
         if (c < p.s.C) {
             if (p.dbeta) p.dbeta[c] = v;
         } else if (c >= p.s.cp && c < p.s.cp + p.s.C) {
             if (p.dgamma) p.dgamma[c - p.s.cp] = v;
         }
     }
+}
+
+__global__ __launch_bounds__(TB) void gn_columns_k(GnBwdArgs p) {
+    __shared__ __attribute__((aligned(16))) float sm[1024];
+    gn_columns(p, blockIdx.x, sm);
 }
 
 // dx; the first `extra` workgroups sum dgamma and dbeta beside it.
@@ -387,17 +410,15 @@ __global__ __launch_bounds__(TB) void gn_bwd_apply_k(GnBwdArgs p) {
     const Place<V> at(p.s, blockIdx.x - p.extra);
     float *s1 = sm, *s2 = sm + 64 * V;
     const int t = threadIdx.x;
-    const int ll = item_lanes(at.np), l = t & ((1 << ll) - 1);
+    const int ll = item_lanes(TB, at.np), l = t & ((1 << ll) - 1);
     const float size = (float)p.s.pixels * (float)p.s.cg;
     for (int q = t >> ll; q < at.np; q += TB >> ll) {
         const int g = at.g0 + q, sa = first_slab<V>(p.s, g), ns = last_slab<V>(p.s, g) - sa + 1;
         float a = 0.f, b = 0.f;
-        for (int e = l; e < ns * p.s.splits; e += 1 << ll) {
-            const int split = e / ns, slab = sa + e - split * ns;
-            const float2 m = ((const float2*)p.ws)[(at.image * p.s.splits + split) * p.s.parts + g + slab];
+        each_part(p.s, (const float2*)p.ws, at.image, g, sa, ns, l, ll, [&](int, int, float2 m) {
             a += m.x;
             b += m.y;
-        }
+        });
         for (int d = 1; d < 1 << ll; d <<= 1) {
             a += __shfl_xor(a, d);
             b += __shfl_xor(b, d);
@@ -481,10 +502,6 @@ GnShape gn_shape(int V, long images, long pixels, int C, int G) {
     return s;
 }
 
-long exact_row(int dt, long rows, int C, long ld) {
-    return rows - (dt == DT_BF16 ? tail_rows<bf16>(rows, C, ld) : tail_rows<float>(rows, C, ld));
-}
-
 template <typename T, int ACT>
 void gn_launch(const GnArgs& p, unsigned wgs, hipStream_t st) {
     launch((gn_stats_k<T>), dim3(wgs), dim3(TB), 0, st, p);
@@ -497,7 +514,7 @@ template <typename T, int ACT>
 void gn_bwd_launch(GnBwdArgs p, unsigned wgs, hipStream_t st) {
     if (wgs) launch((gn_bwd_sums_k<T, ACT>), dim3(wgs), dim3(TB), 0, st, p);
     // (workgroups with the same rows go to the same XCD in both kernels)
-    const unsigned columns = (unsigned)((2 * p.s.cp + 63) / 64);
+    const unsigned columns = (unsigned)((2 * p.s.cp + kColumns - 1) / kColumns);
     p.extra = p.dgamma || p.dbeta ? (int)(columns + 7) / 8 * 8 : 0;
     const unsigned grid = p.extra + (p.dx ? wgs : 0);
     if (grid == 0) return;
@@ -536,8 +553,13 @@ long groupnorm_bwd_ws(long images, long pixels, int C, int G) {
 
 hipError_t launch_groupnorm(int dt, GnArgs p, long images, long pixels, int C, int G, hipStream_t st) {
     if (images <= 0) return hipSuccess;
-    p.s = gn_shape(dt == DT_BF16 ? 8 : 4, images, pixels, C, G);
     p.exact = exact_row(dt, images * pixels, C, p.ldx);
+    const GnWhole whole = groupnorm_whole(dt == DT_BF16 ? 8 : 4, images, pixels, C, G, std::max(p.ldx, p.ldy), false);
+    if (whole.threads) {
+        if (whole.slots > 2 || C % 8) p.exact = exact_row_any(dt, images * pixels, p.ldx);
+        return launch_groupnorm_whole(dt, p, whole, st);
+    }
+    p.s = gn_shape(dt == DT_BF16 ? 8 : 4, images, pixels, C, G);
     const unsigned wgs = (unsigned)(images * p.s.slabs * p.s.splits);
     if (dt == DT_BF16) {
         if (p.act == ACT_RELU) gn_launch<bf16, ACT_RELU>(p, wgs, st);
@@ -554,6 +576,21 @@ hipError_t launch_groupnorm(int dt, GnArgs p, long images, long pixels, int C, i
 hipError_t launch_groupnorm_bwd(int dt, GnBwdArgs p, long images, long pixels, int C, int G, hipStream_t st) {
     p.s = gn_shape(dt == DT_BF16 ? 8 : 4, images, pixels, C, G);
     p.exact = exact_row(dt, images * pixels, C, std::min({p.lddy, p.ldx, p.dres ? p.lddres : p.ldx}));
+    const GnWhole whole = groupnorm_whole(dt == DT_BF16 ? 8 : 4, images, pixels, C, G,
+                                          std::max({p.lddy, p.ldx, p.dres ? p.lddres : 0, p.dx ? p.lddx : 0}), true);
+    if (images > 0 && whole.threads) {
+        if (whole.slots > 2 || C % 8)
+            p.exact = exact_row_any(dt, images * pixels, std::min({p.lddy, p.ldx, p.dres ? p.lddres : p.ldx}));
+        p.s.rows_ws = images;
+        p.s.sums = 0;
+        if (images == 1) p.ws = nullptr;
+        hipError_t e = launch_groupnorm_whole_bwd(dt, p, whole, st);
+        if (e == hipSuccess && p.ws && (p.dgamma || p.dbeta)) {
+            launch(gn_columns_k, dim3((unsigned)((2 * p.s.cp + kColumns - 1) / kColumns)), dim3(TB), 0, st, p);
+            e = hipGetLastError();
+        }
+        return e;
+    }
     const unsigned wgs = (unsigned)(images * p.s.slabs * p.s.splits);
     if (dt == DT_BF16) {
         if (p.act == ACT_RELU) gn_bwd_launch<bf16, ACT_RELU>(p, wgs, st);

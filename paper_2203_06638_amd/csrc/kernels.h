@@ -533,6 +533,16 @@ struct GnShape {
     long rows_ws;       // images * splits
     long sums;          // gradient: where the channels' sums begin in ws (floats)
 };
+// Maps that the registers of a workgroup hold (groupnorm_whole.hip); threads 0: not this one
+struct GnWhole {
+    long images, pixels;
+    int G, cg, gps, slabs;   // groups, channels of one, groups of a workgroup's slab
+    int slots;               // a chunk's parts with statistics of their own
+    int lw, threads, nc;
+    unsigned wgs, per_xcd;
+};
+constexpr long kWholeLd = 1 << 18;   // row distance up to which offsets within 1024 rows fit 32 bits
+GnWhole groupnorm_whole(int V, long images, long pixels, int C, int G, long ld, bool bwd);
 struct GnArgs {
     const void* x;
     void* y;
@@ -558,6 +568,9 @@ struct GnBwdArgs {
     long exact;
     int extra;
 };
+hipError_t launch_groupnorm_whole(int dt, const GnArgs& p, const GnWhole& s, hipStream_t st);
+// (p.ws null: the image's sums are dgamma and dbeta; else [image][2][p.s.cp])
+hipError_t launch_groupnorm_whole_bwd(int dt, const GnBwdArgs& p, const GnWhole& s, hipStream_t st);
 // floats of ws, and the workgroups of a launch
 long groupnorm_ws(long images, long pixels, int C, int G);
 long groupnorm_bwd_ws(long images, long pixels, int C, int G);
