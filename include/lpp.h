@@ -31,7 +31,8 @@
  *   - Flat parameter vectors are float32 in the model's canonical order: the
  *     layers' parameter tensors in layer order, each flattened in its natural
  *     layout: conv W[cout][cin][k][k] then bias[cout]; batch-norm gamma[c]
- *     then beta[c]; RMS norm gamma[c]; linear W[out][in] then bias[out].
+ *     then beta[c]; RMS norm gamma[c]; group norm gamma[c] then beta[c]; linear
+ *     W[out][in] then bias[out].
  *   - worker w in [0, K*P) belongs to replica q = w / P; its default block is
  *     w % P + 1 (the paper's rank(u^q), Sec. 3 "Block Selection Rule").  Any
  *     worker may run any partition; the selection rule is caller policy.
@@ -63,8 +64,10 @@ enum lpp_op {
     LPP_GAP = 5,     /* mean over H x W                                       */
     LPP_LINEAR = 6,  /* y = x W^T + b on the flattened input; params W, b     */
     LPP_CONCAT = 7,  /* channels of in0 followed by channels of in1 (same H, W) */
-    LPP_RMSNORM = 8  /* root-mean-square norm over the channels of every pixel;
+    LPP_RMSNORM = 8, /* root-mean-square norm over the channels of every pixel;
                         param gamma (see lpp_kernel_rmsnorm)                  */
+    LPP_GROUPNORM = 9 /* group norm of each image, k groups of channels; gamma,
+                        beta (see lpp_kernel_groupnorm)                       */
 };
 
 enum lpp_dtype { LPP_FP32 = 0, LPP_BF16 = 1 };
@@ -82,7 +85,7 @@ enum lpp_mode { LPP_SEQUENTIAL = 0, LPP_ASYNC = 1 };
  * activations, with the exact ReLU decisions (also beside an infinity; all
  * values of its group of channels are then not finite).  Weight gradients of 1x1
  * stride-1 convs and RMS norm gradients read the checkpoints as they are;
- * other layers' inputs are unpacked first.  Inputs of batch norms stay in
+ * other layers' inputs are unpacked first.  Inputs of batch and group norms stay in
  * the activation type.  lpp_get_activation and lpp_get_activation_grad return
  * LPP_ESTATE. */
 enum { LPP_ACT8 = 0x100 };
@@ -91,7 +94,7 @@ typedef struct {
     int op;          /* enum lpp_op                                              */
     int in0, in1;    /* producer layer indices (< this layer); -1 = image batch  */
     int cin, cout;   /* conv/linear channels; norms: cout = channels             */
-    int k, stride, pad; /* conv and maxpool geometry                             */
+    int k, stride, pad; /* conv and maxpool geometry; group norm: k = its groups */
     int bias;        /* conv/linear: 1 if the layer has a bias vector            */
     int block;       /* 1..P for a layer that owns parameters, else ignored      */
 } lpp_layer;
@@ -107,7 +110,7 @@ typedef struct {
                                 master parameters                              */
     float momentum;          /* heavy-ball momentum, 0 = plain SGD             */
     float weight_decay;      /* coupled L2 (g + wd*x), block-restricted        */
-    float bn_eps;            /* of batch norms and RMS norms                   */
+    float bn_eps;            /* of batch, RMS and group norms                  */
 } lpp_model_desc;
 
 typedef struct {
@@ -186,6 +189,36 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
  * host threads at once; different workers may.
  */
 int lpp_step(lpp_ctx* ctx, int worker, const lpp_batch* batch, int partition, float lr);
+
+/*
+ * The same iteration with a teacher: the loss of image n is that of
+ * lpp_kernel_distill for its logits, (1 - alpha) * cross-entropy of its label +
+ * alpha * temperature^2 * distillation loss of the teacher's list, and lpp_get_loss
+ * returns its mean over the batch.  The teacher's buffers (device) hold a list for
+ * every image of the batch, as lpp_top_logits or lpp_kernel_top_logits leaves
+ * it, and must stay valid as long as the batch's.  1 <= k <= 128 (LPP_EUNSUPPORTED for
+ * more), 0 <= alpha <= 1, temperature > 0 and finite.
+ */
+typedef struct {
+    const float* values;     /* float32 [batch][k]                                 */
+    const int* index;        /* int32 [batch][k]                                   */
+    const float* rest;       /* float32 [batch], or NULL                           */
+    int k;
+    float alpha;             /* share of the distillation loss                     */
+    float temperature;
+} lpp_teacher;
+int lpp_step_distill(lpp_ctx* ctx, int worker, const lpp_batch* batch, const lpp_teacher* teacher, int partition,
+                     float lr);
+
+/*
+ * The k largest logits, their classes and the rest (NULL: not wanted) of every image of the
+ * worker's last step, as lpp_kernel_top_logits, into device buffers: a teacher's answers to
+ * that batch.  (A step with lr = 0 leaves a teacher's parameters as they are.)  Enqueued on
+ * the worker's stream; sequential mode waits for it, in async mode a student's step on
+ * another stream needs lpp_sync or an event in between.  LPP_ESTATE before the worker's first
+ * step.
+ */
+int lpp_top_logits(lpp_ctx* ctx, int worker, int k, float temperature, float* values, int* index, float* rest);
 
 /*
  * One averaging round over the listed replicas (Alg. 1, averaging loop with

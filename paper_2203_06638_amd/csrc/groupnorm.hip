@@ -10,7 +10,8 @@
 //   dx = rstd * (dz * gamma - (s1 + u * s2)) (+ dres),
 //   s1 = mean over the group of dz * gamma, s2 = of dz * gamma * u
 //
-// Statistics and sums are float32: means and sums of squared deviations of parts are
+// z is the same expression in both directions, so that a ReLU's gradient decides as the
+// forward pass did.  Statistics and sums are float32: means and sums of squared deviations of parts are
 // merged (never sums of squares of the values), everything in a fixed order.
 #include <algorithm>
 
@@ -232,14 +233,15 @@ __global__ __launch_bounds__(TB) void gn_apply_k(GnArgs p) {
         }
     }
     __syncthreads();
-    float mu[V], sc[V], sh[V];
+    float mu[V], rs[V], ga[V], be[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c = min(at.ch + j, p.s.C - 1), q = c / p.s.cg - at.g0;
         const bool has = j < at.n;
         mu[j] = has ? smean[q] : 0.f;
-        sc[j] = has ? srstd[q] * p.gamma[c] : 0.f;
-        sh[j] = has ? p.beta[c] : 0.f;
+        rs[j] = has ? srstd[q] : 0.f;
+        ga[j] = p.gamma[c];
+        be[j] = p.beta[c];
     }
     const T* x = (const T*)p.x + at.ch;
     T* y = (T*)p.y + at.ch;
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(TB) void gn_apply_k(GnArgs p) {
         float v[V];
         chunk_values<T>(w, v);
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = act_value<ACT>(__builtin_fmaf(v[j] - mu[j], sc[j], sh[j]));
+        for (int j = 0; j < V; ++j) v[j] = act_value<ACT>(__builtin_fmaf((v[j] - mu[j]) * rs[j], ga[j], be[j]));
         st_chunk<ST>(y + r * p.ldy, at.n, v);
     };
     const long whole = min(at.r1, p.exact);

@@ -175,12 +175,12 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
     const Slab<V, TB> at(s);
     u4 w[NC] = {};
     load_slab<const T, V, TB, NC>((const T*)p.x, p.ldx, at, s.pixels, p.exact, w);
-    float sc[V], sh[V];
+    float ga[V], be[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c = min(at.ch + j, s.G * s.cg - 1);
-        sc[j] = p.gamma[c];
-        sh[j] = p.beta[c];
+        ga[j] = p.gamma[c];
+        be[j] = p.beta[c];
     }
     int q[V];
     if (S == V) slab_groups<V>(at.w, s.cg, at.np, q);
@@ -226,21 +226,20 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
         for (int j = 0; j < S; ++j) v[0][j] = j < at.n ? v[0][j] : 0.f, v[1][j] = j < at.n ? v[1][j] : 0.f;
     group_sums<V, TB, S, 2>(v, s, at.w, at.np, q, lds + whole_lds(TB, S, s.lw, 1));
     keep_packed<NC>(w);
+    float rs[S];
 #pragma unroll
     for (int j = 0; j < S; ++j) {
         const float e = v[0][j] / size;
         const float var = v[1][j] == INFINITY ? v[1][j] : v[1][j] / size - e * e;
-        const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + p.eps);
+        rs[j] = 1.f / sqrtf((var < 0.f ? 0.f : var) + p.eps);
         mu[j] += e;
         // (the thread with the group's first channel; a slab's last chunk may end before its slots do)
         const int c = at.w * V + j * Q, own = S == V ? q[j] : c / s.cg;
         if (at.n > j * Q && at.rl == 0 && c == own * s.cg) {
             const long g = at.image * s.G + at.g0 + own;
             if (p.mean) p.mean[g] = mu[j];
-            if (p.rstd) p.rstd[g] = rstd;
+            if (p.rstd) p.rstd[g] = rs[j];
         }
-#pragma unroll
-        for (int i = 0; i < Q; ++i) sc[j * Q + i] *= rstd;
     }
     auto put = [&](auto act) {
 #pragma unroll
@@ -251,7 +250,7 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
             chunk_values<T>(w[c], f);
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                f[j] = act_value<decltype(act)::value>(__builtin_fmaf(f[j] - mu[j / Q], sc[j], sh[j]));
+                f[j] = act_value<decltype(act)::value>(__builtin_fmaf((f[j] - mu[j / Q]) * rs[j / Q], ga[j], be[j]));
             st_chunk<ST>(row_of((T*)p.y, p.ldy, at, s.pixels, c), c * at.RL + at.rl < s.pixels ? at.n : 0, f);
         }
     };

@@ -43,8 +43,7 @@ struct StepArgs {
     int k;
     float alpha, temperature;
 };
-hipError_t launch_set_step_args(StepArgs* dst, const float* images, const int* labels, float lr, long trace_slot,
-                                hipStream_t st);
+hipError_t launch_set_step_args(StepArgs* dst, const StepArgs& args, hipStream_t st);
 // Step tracing: one kernel of one thread that stores the device's constant-
 // rate clock (wall_clock64, 100 MHz) into log[slot * 4 + k] with slot =
 // args->trace_slot (nothing when it is negative); kernels of a stream run in

@@ -1591,18 +1591,12 @@ hipError_t launch_nhwc_to_nchw(int dt, const void* src, float* dst, int Nb, int 
     return hipGetLastError();
 }
 
-__global__ void set_step_args_k(StepArgs* dst, const float* images, const int* labels, float lr, long trace_slot) {
-    if (threadIdx.x == 0 && blockIdx.x == 0) {
-        dst->images = images;
-        dst->labels = labels;
-        dst->lr = lr;
-        dst->trace_slot = trace_slot;
-    }
+__global__ void set_step_args_k(StepArgs* dst, StepArgs args) {
+    if (threadIdx.x == 0 && blockIdx.x == 0) *dst = args;
 }
 
-hipError_t launch_set_step_args(StepArgs* dst, const float* images, const int* labels, float lr, long trace_slot,
-                                hipStream_t st) {
-    launch(set_step_args_k, dim3(1), dim3(64), 0, st, dst, images, labels, lr, trace_slot);
+hipError_t launch_set_step_args(StepArgs* dst, const StepArgs& args, hipStream_t st) {
+    launch(set_step_args_k, dim3(1), dim3(64), 0, st, dst, args);
     return hipGetLastError();
 }
 

@@ -95,20 +95,20 @@ struct Plan {
 // Execution groups.  A group runs one fused kernel sequence and
 // materialises exactly one layer output (`out`); layers inside a group whose
 // outputs feed nothing else are never stored.
-enum GKind { G_CONV, G_BNACT, G_RELU, G_ADD, G_MAXPOOL, G_GAP, G_LINEAR, G_HEAD, G_CONCAT, G_RMS };
+enum GKind { G_CONV, G_BNACT, G_RELU, G_ADD, G_MAXPOOL, G_GAP, G_LINEAR, G_HEAD, G_CONCAT, G_RMS, G_GROUPNORM };
 
 // ops that read a second input (in1)
 inline bool two_inputs(int op) { return op == LPP_ADD || op == LPP_CONCAT; }
 struct Group {
     GKind kind = G_CONV;
     int out = -1;       // the layer whose output this group stores
-    int a = -1;         // G_CONV: conv; G_BNACT: first BN; G_HEAD: pool; G_RMS: norm; else: the layer
+    int a = -1;         // G_CONV: conv; G_BNACT: first BN; G_HEAD: pool; norms; else: the layer
     int stats_bn = -1;  // G_CONV: BN whose batch statistics the conv epilogue computes
     int bn2 = -1;       // G_BNACT: BN of the other branch of the residual add (both normalised)
     int add = -1;       // G_BNACT / G_CONV: the residual add, if any; G_RMS: the add whose output the norm reads
                         //   and which the group computes (and stores) as well, in0 + res
     int res = -1;       // G_BNACT / G_CONV: the residual tensor added unnormalised, if any
-    int relu = -1;      // G_BNACT: the closing ReLU, if any; G_CONV: a ReLU applied by the conv's epilogue
+    int relu = -1;      // G_BNACT, G_GROUPNORM: the closing ReLU, if any; G_CONV: a ReLU applied by the conv's epilogue
     int lin = -1;       // G_HEAD: the linear layer
     bool fold = false;  // G_BNACT: BN + ReLU folded into the consuming conv (nothing launched forward)
     bool rsum = false;  // G_BNACT: its backward sums come from the data gradient of conv rsum_conv
@@ -226,6 +226,13 @@ int build_model(const lpp_model_desc* desc, int P, Model& M) {
             if (bf && (L.in0 < 0 || M.layers[L.in0].dt != lpp::DT_BF16))
                 return fail(LPP_EUNSUPPORTED, std::string(where) + "with bf16 an RMS norm cannot read pooled features");
             Y.np = L.cout;
+            break;
+        case LPP_GROUPNORM:
+            if (L.cout != Y.in0.c) return fail(LPP_EINVAL, std::string(where) + "norm channels do not match the input");
+            if (L.k < 1 || L.cout % L.k) return fail(LPP_EINVAL, std::string(where) + "groups (k) must divide the channels");
+            if (bf && (L.in0 < 0 || M.layers[L.in0].dt != lpp::DT_BF16))
+                return fail(LPP_EUNSUPPORTED, std::string(where) + "with bf16 a group norm cannot read pooled features");
+            Y.np = 2L * L.cout;
             break;
         case LPP_RELU:
             break;
@@ -364,6 +371,7 @@ int build_model(const lpp_model_desc* desc, int P, Model& M) {
 //   BN [-> residual add (+ tensor | + another BN's output)] [-> ReLU], each
 //     link the only consumer of the previous: one elementwise pass forward,
 //     one masked reduce + apply pair backward;
+//   group norm -> ReLU: the norm's kernels apply it;
 //   global average pool -> linear (the logits): one head kernel with the
 //     softmax cross-entropy.
 void build_groups(Model& M, bool fused) {
@@ -408,6 +416,11 @@ void build_groups(Model& M, bool fused) {
                     if (r >= 0 && op(r) == LPP_RELU && !taken[r]) g.relu = g.out = r;
                 }
             }
+        } else if (op_l == LPP_GROUPNORM) {
+            g.kind = G_GROUPNORM;
+            g.a = g.out = l;
+            const int c = fused ? sole(l) : -1;
+            if (c >= 0 && op(c) == LPP_RELU && !taken[c]) g.relu = g.out = c;
         } else if (op_l == LPP_GAP) {
             const int c = fused ? sole(l) : -1;
             if (c == n - 1 && op(c) == LPP_LINEAR && M.layers[l].in0.c % 4 == 0) {
@@ -699,7 +712,7 @@ void for_act8_reads(const Model& M, const Plan& pl, const Group& G, F f) {
 // LPP_ACT8: which outputs share buffers and which are kept as checkpoints (Model).
 // An output and its gradient are touched by the groups from its producer to
 // its last consumer only, in the forward pass and, reversed, in the backward
-// pass.  Batch-norm inputs keep buffers of their own, in full: ReLU
+// pass.  Batch-norm and group-norm inputs keep buffers of their own, in full: ReLU
 // decisions are recomputed from them.  So do the small float32 tensors of
 // the head.
 void plan_act8(Model& M) {
@@ -721,7 +734,7 @@ void plan_act8(Model& M) {
         M.shared[l] = M.stored[l] && op != LPP_GAP && op != LPP_LINEAR;
         M.first_group[l] = M.last_group[l] = group_of[l];
         for (int c : M.consumers[l]) {
-            if (M.layers[c].L.op == LPP_BN) M.shared[l] = 0;
+            if (M.layers[c].L.op == LPP_BN || M.layers[c].L.op == LPP_GROUPNORM) M.shared[l] = 0;
             M.last_group[l] = std::max(M.last_group[l], group_of[c]);
         }
     }
@@ -798,9 +811,11 @@ struct Worker {
     float* ps1 = nullptr;
     float* ps2 = nullptr;
     float* wpart = nullptr;
-    lpp::StepArgs* args = nullptr;          // device: this step's images, labels, lr
-    std::vector<hipGraphExec_t> graphs;     // one per partition, captured on first use
-    std::vector<hipGraphExec_t> tgraphs;    // the same with the step-trace timestamps
+    float* scratch = nullptr;               // workspace of the group norms, the distillation and the top logits
+    lpp::StepArgs* args = nullptr;          // device: this step's images, labels, lr, teacher
+    // one per partition, captured on first use: plain, with the step-trace timestamps (+ 1), with
+    // a teacher (+ 2)
+    std::vector<hipGraphExec_t> graphs[4];
     int last_partition = -1;
 };
 
@@ -821,7 +836,7 @@ struct lpp_ctx {
     long wbuf_floats = 0;
     size_t ws_bytes = 0;
     size_t off_v = 0, off_wbuf = 0, off_g = 0, off_m = 0, off_loss = 0, off_img = 0, off_ps = 0, off_wpart = 0,
-           off_args = 0, off_acc = 0;
+           off_args = 0, off_acc = 0, off_scratch = 0;
     long n_acc = 0;                          // doubles zeroed at the start of every step
     // sequential mode merges batch-norm reductions in a fixed order (bitwise
     // reproducible); async mode through atomic accumulators
@@ -829,6 +844,7 @@ struct lpp_ctx {
     bool act8 = false;                       // activations kept as 8-bit checkpoints (LPP_ACT8)
     bool graphs = true;
     long ps_floats = 0;
+    long scratch_floats = 0;
     long wpart_floats = 0;                   // weight-gradient partials of one reduce batch
     std::unique_ptr<std::atomic<long>[]> counters;
     Timer timer;
@@ -1074,10 +1090,9 @@ void destroy_ctx(lpp_ctx* c) {
     hipSetDevice(c->device);
     for (auto& w : c->workers) {
         if (w.stream) hipStreamSynchronize(w.stream);
-        for (auto g : w.graphs)
-            if (g) hipGraphExecDestroy(g);
-        for (auto g : w.tgraphs)
-            if (g) hipGraphExecDestroy(g);
+        for (auto& graphs : w.graphs)
+            for (auto g : graphs)
+                if (g) hipGraphExecDestroy(g);
         if (w.ws) hipFree(w.ws);
         if (w.own_stream && w.stream) hipStreamDestroy(w.stream);
     }
@@ -1120,9 +1135,9 @@ int bn_stats_standalone(lpp_ctx* c, Worker& w, int b) {
     return LPP_OK;
 }
 
-// Forward pass of worker w at its snapshot; loss and dlogits at the end.  With
-// LPP_ACT8 it leaves the checkpoints that the partition's backward reads.
-int run_forward(lpp_ctx* c, Worker& w, int partition) {
+// Forward pass of worker w at its snapshot; loss and dlogits at the end, with `distill` those of
+// the step's teacher.  With LPP_ACT8 it leaves the checkpoints that the partition's backward reads.
+int run_forward(lpp_ctx* c, Worker& w, int partition, bool distill) {
     Model& M = c->M;
     const Plan& pl = M.plans[partition];
     auto wanted = [&](int l) { return c->has_ckpt(l) && pl.ck[l]; };
@@ -1238,6 +1253,22 @@ int run_forward(lpp_ctx* c, Worker& w, int partition) {
                    lpp::launch_rmsnorm(dt, a, st));
             break;
         }
+        case G_GROUPNORM: {
+            const int C = Y.out.c, P = Y.in0.h * Y.in0.w;
+            lpp::GnArgs a{};
+            a.x = x0;
+            a.y = c->act(w, G.out);
+            a.ldx = a.ldy = C;
+            a.gamma = w.v + Y.poff;
+            a.beta = a.gamma + C;
+            a.mean = c->aux(w, G.a);
+            a.rstd = a.mean + (long)N * Y.L.k;
+            a.ws = w.scratch;
+            a.act = G.relu >= 0 ? lpp::ACT_RELU : lpp::ACT_NONE;
+            a.eps = M.desc.bn_eps;
+            LAUNCH("groupnorm", 2.0 * eb * Mrows * C, st, lpp::launch_groupnorm(dt, a, N, P, C, Y.L.k, st));
+            break;
+        }
         case G_RELU:
             LAUNCH("relu", 2.0 * eb * Mrows * Y.out.c, st,
                    lpp::launch_relu_fwd(dt, x0, c->act(w, G.a), Mrows * Y.out.c, st));
@@ -1289,8 +1320,24 @@ int run_forward(lpp_ctx* c, Worker& w, int partition) {
                                              M.ck_sign[l] ? lpp::ACT8_DECIDES : lpp::ACT8_NEAREST, c->ckpt(w, l), st));
             }
     }
-    if (!loss_done) {
-        const int last = (int)M.layers.size() - 1;
+    const int last = (int)M.layers.size() - 1;
+    if (distill) {
+        // (in place of the head's own loss and gradient)
+        lpp::DistillArgs a{};
+        a.z = c->act(w, last);
+        a.dz = c->dact(w, last);
+        a.ldz = a.lddz = a.C = M.desc.n_classes;
+        a.rows = N;
+        a.loss = w.loss + 1;
+        a.scale = 1.f / (float)N;
+        a.ws = w.scratch;
+        a.step = w.args;
+        LAUNCH("distill", 8.0 * N * M.desc.n_classes, st, lpp::launch_distill(lpp::DT_F32, a, st));
+        // (the fused head's backward forms the mean)
+        if (!loss_done)
+            LAUNCH("distill", 0.0, st,
+                   lpp::launch_head_bwd_w(nullptr, nullptr, N, 1, 1, nullptr, nullptr, w.loss + 1, w.loss, st));
+    } else if (!loss_done) {
         LAUNCH("softmax_ce", 0.0, st,
                lpp::launch_softmax_ce((const float*)c->act(w, last), w.args, (float*)c->dact(w, last), w.loss, N,
                                       M.desc.n_classes, st));
@@ -1610,6 +1657,28 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
                        lpp::launch_rmsnorm_bwd(dt, a, st));
             break;
         }
+        case G_GROUPNORM: {
+            const int C = Y.out.c, P = Y.in0.h * Y.in0.w;
+            lpp::GnBwdArgs a{};
+            a.dy = dy;
+            a.x = x0;
+            a.dx = dx0;
+            if (dx0 && pl.acc0[G.a]) a.dres = dx0;
+            a.lddy = a.ldx = a.lddres = a.lddx = C;
+            a.gamma = w.v + Y.poff;
+            a.beta = a.gamma + C;
+            a.mean = c->aux(w, G.a);
+            a.rstd = a.mean + (long)N * Y.L.k;
+            if (pl.wgrad[G.a]) {
+                a.dgamma = w.g + Y.poff;
+                a.dbeta = a.dgamma + C;
+            }
+            a.ws = w.scratch;
+            a.act = G.relu >= 0 ? lpp::ACT_RELU : lpp::ACT_NONE;
+            LAUNCH("groupnorm_bwd", eb * (2.0 + (a.dx ? 1.0 : 0.0) + (a.dres ? 1.0 : 0.0)) * Min * C, st,
+                   lpp::launch_groupnorm_bwd(dt, a, N, P, C, Y.L.k, st));
+            break;
+        }
         case G_RELU:
             if (dx0)
                 LAUNCH("relu", 3.0 * eb * Min * Y.out.c, st,
@@ -1714,7 +1783,7 @@ int run_backward(lpp_ctx* c, Worker& w, int partition) {
 // of the replica, forward, truncated backward, block update.  Per-step
 // arguments are read from w.args.  `traced` brackets the snapshot and the
 // update with timestamp kernels (their log row comes from w.args).
-int enqueue_step(lpp_ctx* c, Worker& w, int worker, int partition, bool traced) {
+int enqueue_step(lpp_ctx* c, Worker& w, int worker, int partition, bool traced, bool distill) {
     const int q = worker / c->P;
     float* xq = c->replicas + (long)q * c->dpad;
     hipStream_t st = w.stream;
@@ -1722,7 +1791,7 @@ int enqueue_step(lpp_ctx* c, Worker& w, int worker, int partition, bool traced) 
     LAUNCH("snapshot", c->snap_bytes, st,
            lpp::launch_snapshot(c->M.dt, xq, w.v, c->snap_dev, c->n_snap, c->snap_tiles, w.wbuf, st));
     if (traced) HIPCHK(lpp::launch_timestamp(c->trace_log, w.args, -1, 1, st));
-    int rc = run_forward(c, w, partition);
+    int rc = run_forward(c, w, partition, distill);
     if (rc) return rc;
     rc = run_backward(c, w, partition);
     if (rc) return rc;
@@ -1836,6 +1905,8 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
     c->off_args = take(sizeof(lpp::StepArgs));
     c->off_img = take(eb * (size_t)N * M.desc.in_h * M.desc.in_w * M.img_cp);
     long ps = 1, wpart = 1, wsum = 0;
+    long scratch = std::max({1L, lpp::distill_ws(N, M.desc.n_classes),
+                             lpp::top_logits_ws(N, M.desc.n_classes, std::min(M.desc.n_classes, lpp::kDistillMaxK))});
     std::vector<Held> held;   // LPP_ACT8: the shared buffers
     for (int l = 0; l < (int)M.layers.size(); ++l) {
         Layer& Y = M.layers[l];
@@ -1855,6 +1926,14 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
             const long pf = align64((long)lpp::rmsnorm_bwd_parts(rows_out, Y.out.c) * Y.out.c);
             wpart = std::max(wpart, pf);
             wsum += pf;
+        }
+        if (Y.L.op == LPP_GROUPNORM) {
+            const long pixels = (long)Y.out.h * Y.out.w;
+            if (lpp::groupnorm_wgs(N, pixels, Y.out.c, Y.L.k) >= (1L << 30))
+                return fail(LPP_EUNSUPPORTED, "group norm: too many images for one launch");
+            Y.aux = take(sizeof(float) * 2 * (size_t)N * Y.L.k);   // mean, rstd
+            scratch = std::max({scratch, lpp::groupnorm_ws(N, pixels, Y.out.c, Y.L.k),
+                                lpp::groupnorm_bwd_ws(N, pixels, Y.out.c, Y.L.k)});
         }
         if (Y.L.op == LPP_MAXPOOL) Y.aux = take((size_t)rows_out * Y.out.c);
         const long rin = (long)N * Y.in0.h * Y.in0.w;
@@ -1898,6 +1977,8 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
     c->ps_floats = ps;
     c->off_ps = take(sizeof(float) * 3 * ps);
     c->off_wpart = take(sizeof(float) * wpart);
+    c->scratch_floats = scratch;
+    c->off_scratch = take(sizeof(float) * scratch);
     if (!held.empty()) {
         const size_t base = take(place_held(held));
         for (Held& h : held) *h.off += base;
@@ -1939,8 +2020,8 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
         w.ps2 = w.ps1 + c->ps_floats;
         w.wpart = (float*)(w.ws + c->off_wpart);
         w.args = (lpp::StepArgs*)(w.ws + c->off_args);
-        w.graphs.assign(P + 1, nullptr);
-        w.tgraphs.assign(P + 1, nullptr);
+        w.scratch = (float*)(w.ws + c->off_scratch);
+        for (auto& graphs : w.graphs) graphs.assign(P + 1, nullptr);
     }
     if (opt && opt->avg_stream) {
         c->avg_stream = (hipStream_t)opt->avg_stream;
@@ -1959,7 +2040,8 @@ int lpp_destroy(lpp_ctx* c) {
     return LPP_OK;
 }
 
-int lpp_step(lpp_ctx* c, int worker, const lpp_batch* batch, int partition, float lr) {
+// lpp_step, and with a teacher lpp_step_distill
+static int step(lpp_ctx* c, int worker, const lpp_batch* batch, const lpp_teacher* teacher, int partition, float lr) {
     int rc = check_worker(c, worker);
     if (rc) return rc;
     if (!batch || !batch->images || !batch->labels) return fail(LPP_EINVAL, "batch or its buffers are NULL");
@@ -1984,7 +2066,16 @@ int lpp_step(lpp_ctx* c, int worker, const lpp_batch* batch, int partition, floa
             r.counter = s_read;
         }
     }
-    LAUNCH("args", 0.0, st, lpp::launch_set_step_args(w.args, batch->images, batch->labels, lr, slot, st));
+    lpp::StepArgs args{batch->images, batch->labels, lr, slot, nullptr, nullptr, nullptr, 0, 0.f, 1.f};
+    if (teacher) {
+        args.values = teacher->values;
+        args.index = teacher->index;
+        args.rest = teacher->rest;
+        args.k = teacher->k;
+        args.alpha = teacher->alpha;
+        args.temperature = teacher->temperature;
+    }
+    LAUNCH("args", 0.0, st, lpp::launch_set_step_args(w.args, args, st));
     bool timing;
     {
         std::lock_guard<std::mutex> g(c->timer.mu);
@@ -1993,10 +2084,10 @@ int lpp_step(lpp_ctx* c, int worker, const lpp_batch* batch, int partition, floa
     if (c->graphs && !timing) {
         // one graph per (worker, partition): snapshot, forward, truncated
         // backward and update, captured once and replayed
-        hipGraphExec_t& ge = traced ? w.tgraphs[partition] : w.graphs[partition];
+        hipGraphExec_t& ge = w.graphs[(traced ? 1 : 0) + (teacher ? 2 : 0)][partition];
         if (!ge) {
             HIPCHK(hipStreamBeginCapture(st, hipStreamCaptureModeThreadLocal));
-            rc = enqueue_step(c, w, worker, partition, traced);
+            rc = enqueue_step(c, w, worker, partition, traced, teacher != nullptr);
             hipGraph_t graph = nullptr;
             hipError_t e = hipStreamEndCapture(st, &graph);
             if (rc) {
@@ -2013,11 +2104,54 @@ int lpp_step(lpp_ctx* c, int worker, const lpp_batch* batch, int partition, floa
         }
         HIPCHK(hipGraphLaunch(ge, st));
     } else {
-        rc = enqueue_step(c, w, worker, partition, traced);
+        rc = enqueue_step(c, w, worker, partition, traced, teacher != nullptr);
         if (rc) return rc;
     }
     w.last_partition = partition;
     if (c->mode == LPP_SEQUENTIAL) HIPCHK(hipStreamSynchronize(st));
+    return LPP_OK;
+}
+
+int lpp_step(lpp_ctx* c, int worker, const lpp_batch* batch, int partition, float lr) {
+    return step(c, worker, batch, nullptr, partition, lr);
+}
+
+int lpp_step_distill(lpp_ctx* c, int worker, const lpp_batch* batch, const lpp_teacher* t, int partition, float lr) {
+    if (!t || !t->values || !t->index) return fail(LPP_EINVAL, "teacher or its buffers are NULL");
+    if (((uintptr_t)t->values | (uintptr_t)t->index | (uintptr_t)t->rest) % 4)
+        return fail(LPP_EINVAL, "the teacher's buffers must be floats and ints");
+    if (t->k < 1) return fail(LPP_EINVAL, "k must be at least 1");
+    if (t->k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
+    if (!(t->alpha >= 0.f && t->alpha <= 1.f)) return fail(LPP_EINVAL, "alpha must be in [0, 1]");
+    if (!(t->temperature > 0.f) || !std::isfinite(t->temperature))
+        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    return step(c, worker, batch, t, partition, lr);
+}
+
+int lpp_top_logits(lpp_ctx* c, int worker, int k, float temperature, float* values, int* index, float* rest) {
+    int rc = check_worker(c, worker);
+    if (rc) return rc;
+    Worker& w = c->workers[worker];
+    const Model& M = c->M;
+    if (!values || !index || ((uintptr_t)values | (uintptr_t)index | (uintptr_t)rest) % 4)
+        return fail(LPP_EINVAL, "values, index and rest must be buffers of floats and ints");
+    if (k < 1 || k > M.desc.n_classes) return fail(LPP_EINVAL, "k must be in [1, n_classes]");
+    if (k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
+    if (!(temperature > 0.f) || !std::isfinite(temperature))
+        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (w.last_partition < 0) return fail(LPP_ESTATE, "the worker has made no step");
+    lpp::TopArgs a{};
+    a.z = c->act(w, (int)M.layers.size() - 1);
+    a.ldz = a.C = M.desc.n_classes;
+    a.rows = M.desc.batch;
+    a.k = k;
+    a.temp = temperature;
+    a.values = values;
+    a.index = index;
+    a.rest = rest;
+    a.ws = w.scratch;
+    LAUNCH("top_logits", 4.0 * a.rows * a.C, w.stream, lpp::launch_top_logits(lpp::DT_F32, a, w.stream));
+    if (c->mode == LPP_SEQUENTIAL) HIPCHK(hipStreamSynchronize(w.stream));
     return LPP_OK;
 }
 

@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblpp.so")
 _LIB = None
 
-CONV, BN, RELU, ADD, MAXPOOL, GAP, LINEAR, CONCAT, RMSNORM = range(9)
+CONV, BN, RELU, ADD, MAXPOOL, GAP, LINEAR, CONCAT, RMSNORM, GROUPNORM = range(10)
 FP32, BF16 = 0, 1
 SEQUENTIAL, ASYNC = 0, 1
 ACT8 = 0x100
@@ -50,6 +50,11 @@ class Options(C.Structure):
 
 class Batch(C.Structure):
     _fields_ = [("images", C.c_void_p), ("labels", C.c_void_p), ("n", C.c_int)]
+
+
+class Teacher(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("index", C.c_void_p), ("rest", C.c_void_p), ("k", C.c_int),
+                ("alpha", C.c_float), ("temperature", C.c_float)]
 
 
 class TraceStep(C.Structure):
@@ -127,6 +132,8 @@ def lib():
             "lpp_describe": ([C.POINTER(ModelDesc), C.c_int, C.POINTER(ModelInfo)], C.c_int),
             "lpp_init": ([C.POINTER(ModelDesc), C.c_int, C.c_int, C.POINTER(Options), C.POINTER(ctx)], C.c_int),
             "lpp_step": ([ctx, C.c_int, C.POINTER(Batch), C.c_int, C.c_float], C.c_int),
+            "lpp_step_distill": ([ctx, C.c_int, C.POINTER(Batch), C.POINTER(Teacher), C.c_int, C.c_float], C.c_int),
+            "lpp_top_logits": ([ctx, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p], C.c_int),
             "lpp_average": ([ctx, C.POINTER(C.c_int), C.c_int], C.c_int),
             "lpp_set_params": ([ctx, C.c_int, fp, C.c_long], C.c_int),
             "lpp_get_params": ([ctx, C.c_int, fp, C.c_long], C.c_int),
@@ -244,6 +251,24 @@ class Context:
         """images: device float32 NCHW tensor; labels: device int32 tensor."""
         b = Batch(images.data_ptr(), labels.data_ptr(), images.shape[0])
         _check(lib().lpp_step(self._ctx, worker, C.byref(b), partition, lr))
+
+    def step_distill(self, worker, images, labels, values, index, partition, lr, rest=None, alpha=0.9, temperature=1.0):
+        """A step whose loss is alpha parts distillation from a teacher's list (values,
+        index [batch][k], rest [batch]: device tensors, see top_logits)."""
+        dev = _current_device(images)
+        vp, ip, k = _list(values, index, self.batch, dev)
+        rp = _floats(rest, self.batch, "rest", dev) if rest is not None else None
+        b = Batch(images.data_ptr(), labels.data_ptr(), images.shape[0])
+        t = Teacher(vp, ip, rp, k, alpha, temperature)
+        _check(lib().lpp_step_distill(self._ctx, worker, C.byref(b), C.byref(t), partition, lr))
+
+    def top_logits(self, worker, values, index, rest=None, temperature=1.0):
+        """The k largest logits of each image of the worker's last step into values, index
+        [batch][k], and the log weight of the others into rest [batch] (device tensors)."""
+        dev = _current_device(values)
+        vp, ip, k = _list(values, index, self.batch, dev)
+        rp = _floats(rest, self.batch, "rest", dev) if rest is not None else None
+        _check(lib().lpp_top_logits(self._ctx, worker, k, temperature, vp, ip, rp))
 
     def average(self, replicas=None):
         if replicas is None:

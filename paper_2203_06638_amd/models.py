@@ -12,7 +12,7 @@ every layer.
 """
 from __future__ import annotations
 
-from .lpp import ADD, BN, CONCAT, CONV, GAP, LINEAR, MAXPOOL, RELU, RMSNORM
+from .lpp import ADD, BN, CONCAT, CONV, GAP, GROUPNORM, LINEAR, MAXPOOL, RELU, RMSNORM
 
 
 class Model:
@@ -59,6 +59,12 @@ class Model:
         self.specs += [("rms_gamma", c, 0)]
         return self._emit((RMSNORM, x, -1, c, c, 0, 1, 0, 0, 0), self._shape(x))
 
+    def groupnorm(self, x, groups):
+        c = self._shape(x)[0]
+        assert c % groups == 0
+        self.specs += [("gn_gamma", c, 0), ("gn_beta", c, 0)]
+        return self._emit((GROUPNORM, x, -1, c, c, groups, 1, 0, 0, 0), self._shape(x))
+
     def relu(self, x):
         return self._emit((RELU, x, -1, 0, 0, 0, 1, 0, 0, 0), self._shape(x))
 
@@ -94,7 +100,7 @@ class Model:
         assert len(unit_to_block) == self.n_units
         assert list(unit_to_block) == sorted(unit_to_block)
         for rec, u in zip(self.layers, self.unit_of):
-            rec[9] = unit_to_block[u] if rec[0] in (CONV, BN, LINEAR, RMSNORM) else 0
+            rec[9] = unit_to_block[u] if rec[0] in (CONV, BN, LINEAR, RMSNORM, GROUPNORM) else 0
         self.P = max(unit_to_block)
         return self
 
@@ -106,15 +112,21 @@ class Model:
 # ---------------------------------------------------------------------------
 # residual units
 
-def post_act_unit(m, x, cout, stride, act=True):
+def norm_layer(m, groups):
+    """Batch norms, or with groups > 0 group norms of so many groups: a model's
+    answer to an image then depends on that image alone."""
+    return (lambda t: m.groupnorm(t, groups)) if groups else m.bn
+
+
+def post_act_unit(m, x, cout, stride, act=True, groups=0):
     """conv3x3-BN-ReLU-conv3x3-BN (+ identity or 1x1/BN projection), ReLU.
-    act=False leaves the ReLUs out."""
+    act=False leaves the ReLUs out; groups: group norms (norm_layer)."""
     m.new_unit()
-    relu = m.relu if act else (lambda t: t)
+    relu, norm = m.relu if act else (lambda t: t), norm_layer(m, groups)
     cin = m.shapes[x][0] if x >= 0 else m.in_shape[0]
-    y = relu(m.bn(m.conv(x, cout, 3, stride)))
-    y = m.bn(m.conv(y, cout, 3, 1))
-    sc = m.bn(m.conv(x, cout, 1, stride, 0)) if (stride != 1 or cin != cout) else x
+    y = relu(norm(m.conv(x, cout, 3, stride)))
+    y = norm(m.conv(y, cout, 3, 1))
+    sc = norm(m.conv(x, cout, 1, stride, 0)) if (stride != 1 or cin != cout) else x
     return relu(m.add(y, sc))
 
 
@@ -173,23 +185,24 @@ def tiny_cnn(n_classes=10, hw=32):
     return m.assign_blocks([1, 2])
 
 
-def resnet_cifar(depth=20, widths=(16, 32, 64), n_classes=10, hw=32, blocks=None, act=True):
+def resnet_cifar(depth=20, widths=(16, 32, 64), n_classes=10, hw=32, blocks=None, act=True, groups=0):
     n = (depth - 2) // 6
     m = Model("resnet%d" % depth, (3, hw, hw), n_classes)
-    x = m.bn(m.conv(-1, widths[0], 3))
+    x = norm_layer(m, groups)(m.conv(-1, widths[0], 3))
     x = m.relu(x) if act else x
     for si, wdt in enumerate(widths):
         for u in range(n):
-            x = post_act_unit(m, x, wdt, 2 if (si and not u) else 1, act)
+            x = post_act_unit(m, x, wdt, 2 if (si and not u) else 1, act, groups)
     m.new_unit()
     m.linear(m.gap(x), n_classes)
     return m.assign_blocks(blocks or [1] * m.n_units)
 
 
-def resnet20(n_classes=10, act=True):
+def resnet20(n_classes=10, act=True, groups=0):
     """ResNet-20, P = 4 blocks of residual units balanced by forward work:
-    {stem, s1u1, s1u2} {s1u3, s2u1} {s2u2, s2u3, s3u1} {s3u2, s3u3, head}."""
-    return resnet_cifar(20, (16, 32, 64), n_classes, blocks=[1, 1, 1, 2, 2, 3, 3, 3, 4, 4, 4], act=act)
+    {stem, s1u1, s1u2} {s1u3, s2u1} {s2u2, s2u3, s3u1} {s3u2, s3u3, head}.
+    groups: group norms of so many groups in place of the batch norms."""
+    return resnet_cifar(20, (16, 32, 64), n_classes, blocks=[1, 1, 1, 2, 2, 3, 3, 3, 4, 4, 4], act=act, groups=groups)
 
 
 def wide_resnet(depth=16, k=8, n_classes=100, hw=32, blocks=None, act=True):

@@ -45,8 +45,8 @@ def init_params(specs, seed: int) -> np.ndarray:
       'conv_w'   -> N(0, 2 / fan_in)            (He normal)
       'linear_w' -> U(-1/sqrt(fan_in), +1/sqrt(fan_in))
       'bias'     -> 0
-      'bn_gamma', 'rms_gamma' -> 1
-      'bn_beta'  -> 0
+      'bn_gamma', 'rms_gamma', 'gn_gamma' -> 1
+      'bn_beta', 'gn_beta'  -> 0
     """
     rng = _rng(seed + 1_000_003)
     parts = []
@@ -56,9 +56,9 @@ def init_params(specs, seed: int) -> np.ndarray:
         elif kind == "linear_w":
             b = np.float32(1.0 / np.sqrt(fan_in))
             parts.append(rng.uniform(-b, b, size=numel).astype(np.float32))
-        elif kind in ("bias", "bn_beta"):
+        elif kind in ("bias", "bn_beta", "gn_beta"):
             parts.append(np.zeros(numel, np.float32))
-        elif kind in ("bn_gamma", "rms_gamma"):
+        elif kind in ("bn_gamma", "rms_gamma", "gn_gamma"):
             parts.append(np.ones(numel, np.float32))
         else:
             raise ValueError(kind)

@@ -123,3 +123,22 @@ def test_reference_gradient(rest):
         num = 0.5 * (R.distill(z + e * d, *args)[0] - R.distill(z - e * d, *args)[0]).sum() / (2 * e)
         # (central differences: e^2 of the third derivative, and rounding 2^-53 / e)
         assert abs(num - (dz * d).sum()) < 1e-7 * dz.abs().sum()
+
+
+def test_step_refusals():
+    """A teacher is looked at before the context is."""
+    L = lpp.lib()
+
+    def f(**kw):
+        t = lpp.Teacher(OKP, OKP, OKP, 4, 0.5, 2.0)
+        for k, x in kw.items():
+            setattr(t, k, x)
+        return L.lpp_step_distill(None, 0, None, C.byref(t), 0, 0.1)
+    refused(L.lpp_step_distill(None, 0, None, None, 0, 0.1))
+    nan, inf = float("nan"), float("inf")
+    for kw in ({}, dict(values=None), dict(index=None), dict(values=OKP + 2), dict(index=OKP + 1), dict(rest=OKP + 2),
+               dict(k=0), dict(k=-3), dict(alpha=-0.5), dict(alpha=2.0), dict(alpha=nan), dict(temperature=0.0),
+               dict(temperature=nan), dict(temperature=inf)):
+        refused(f(**kw))
+    refused(f(k=129), lpp.EUNSUPPORTED)
+    refused(L.lpp_top_logits(None, 0, 3, 1.0, OKP, OKP, OKP))

@@ -106,3 +106,24 @@ def test_reference_gradient(name):
         up, down = (loss(*(t + s * e * d for t, d in zip((x, gamma, beta), v))) for s in (1, -1))
         # (central differences: e^2 of the third derivative, and rounding 2^-53 / e)
         assert abs((up - down) / (2 * e) - sum((a * d).sum() for a, d in zip(got, v))) < 1e-6 * sum(a.abs().sum() for a in got)
+
+
+def test_layer():
+    """A layer's parameters and what lpp_describe refuses."""
+    from paper_2203_06638_amd import models as PM
+
+    def model(groups, c=16):
+        m = PM.Model("m", (3, 8, 8), 8)
+        t = m.conv(-1, 16, 3)
+        m.layers.append([lpp.GROUPNORM, t, -1, c, c, groups, 1, 0, 0, 0])
+        m.unit_of.append(0)
+        m.shapes.append(m.shapes[t])
+        m.linear(m.gap(1), 8)
+        return lpp.describe(m.assign_blocks([1]), 2)
+    assert model(4).d == 16 * 27 + 2 * 16 + 16 * 8 + 8
+    for kw in (dict(groups=0), dict(groups=-2), dict(groups=3), dict(groups=32), dict(groups=4, c=8)):
+        with pytest.raises(lpp.LppError) as e:
+            model(**kw)
+        assert e.value.code == lpp.EINVAL
+    m = PM.resnet20(groups=8)
+    assert lpp.describe(m, 4).d == PM.resnet20().d
