@@ -14,6 +14,7 @@
 // Sums are float32 in a fixed order.  exp(x) is taken as 2^(x log2 e) of x <= 0, whose
 // relative error grows with |x| while its share of a sum falls as e^x.
 #include <algorithm>
+#include <type_traits>
 
 #include "act8.h"
 #include "kernels.h"
@@ -59,6 +60,9 @@ struct RowChunks {
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 enum RowMode { WHOLE, PIECE_SUMS, PIECE_GRAD };
+// What a row's gradient takes: exp(z / T) alone (or exp(z) alone); both; or both with T = 2 or T = 4,
+// where exp(z) is a power of the other.
+enum RowExps { ONE_EXP, TWO_EXPS, SQUARE, FOURTH };
 
 // ---- distillation ------------------------------------------------------------
 
@@ -71,7 +75,7 @@ constexpr int kListPitch = kDistillMaxK + 4;   // floats of a row's list in the 
 // Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
 // other, are covered by other rows.
 constexpr int distill_waves(int values, bool both) {
-    return both ? (values <= 16 ? 5 : values <= 40 ? 4 : 2) : values <= 32 ? 6 : 4;
+    return both ? (values <= 16 ? 5 : values <= 40 ? 4 : 2) : values <= 64 ? 4 : 3;
 }
 
 // WHOLE: a row to TPR threads, in their registers, so that z is read once.  PIECE_SUMS: a
@@ -80,10 +84,11 @@ constexpr int distill_waves(int values, bool both) {
 // The listed classes and the label are taken out of the row (set to -inf) and have their
 // parts of the sums, and their gradients, from the list, which the row's first wave
 // works on: its teacher's side while the row is on its way, its student's side between
-// the sums and the gradient.  BOTH: exp(z) and exp(z / T) are both wanted; they stay in
-// registers from the sums to the gradient.
-template <typename T, int TPR, int NC, int MODE, bool BOTH, bool ST>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int)sizeof(T), BOTH)) void distill_k(DistillArgs p) {
+// the sums and the gradient.  The exponentials stay in registers from the sums to the
+// gradient.
+template <typename T, int TPR, int NC, int MODE, int EXPS, bool ST>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int)sizeof(T), EXPS == TWO_EXPS)) void distill_k(DistillArgs p) {
+    constexpr bool BOTH = EXPS != ONE_EXP;
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
     constexpr int LW = TPR < 64 ? TPR : 64;      // lanes that work on the list
@@ -131,9 +136,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int
     for (int e = t; e < (TPR * NC * V + 31) / 32; e += TPR) mask[e] = 0u;
     row_sync<TPR>();
     float tm = rest, ts = 0.f;
+    bool twice = false;               // a class is listed twice
     if (lead) {
         bool bad = rest != rest;      // (a maximum drops a NaN)
-        for (int e = t; e <= k; e += LW) {
+        auto entry = [&](int e) {
             const int c = cls[e];
             // (dz may be z: the pieces' workgroups keep z at the listed classes for each other)
             float* kept = p.ws + 4 * p.rows * p.pieces + r * kListPitch;
@@ -141,15 +147,25 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int
             if (c >= 0) v = MODE == PIECE_GRAD ? kept[e] : ld1(z, c);
             zc[e] = v;
             if (MODE == PIECE_SUMS && c >= c0 && c < c1) kept[e] = v;
-            if (c >= c0 && c < c1) atomicOr(&mask[(c - c0) >> 5], 1u << ((c - c0) & 31));
-            if (MODE == PIECE_SUMS) continue;
+            // whether the class is listed before (all of a row's entries are one wave's, the label
+            // comes last)
             int seen = 0;
+            if (c >= c0 && c < c1) {
+                const uint32_t bit = 1u << ((c - c0) & 31);
+                seen = (atomicOr(&mask[(c - c0) >> 5], bit) & bit) != 0;
+            }
+            if (MODE == PIECE_GRAD) {
+                seen = 0;
 #pragma unroll 4
-            for (int o = 0; o < e; ++o) seen |= cls[o] == c;
+                for (int o = 0; o < e; ++o) seen |= cls[o] == c;
+            }
             again[e] = seen;
+            twice |= seen && e < k;
             tm = fmaxf(tm, pr[e]);
             bad |= pr[e] != pr[e];
-        }
+        };
+        for (int e = t; e < k; e += LW) entry(e);
+        if (t == k % LW) entry(k);
         // the teacher's probabilities
         tm = row_max<LW>(tm, slots, none);
         for (int e = t; e < k; e += LW) ts += cls[e] >= 0 && tm > -INFINITY ? pow2((pr[e] - tm) * kLog2e) : 0.f;
@@ -160,7 +176,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int
     row_sync<TPR>();
 
     // the row, then its exponentials: a of z / T (of z where only that is wanted), b of z
-    float a[NC][V], b[BOTH ? NC : 1][V];
+    float a[NC][V], b[EXPS == TWO_EXPS ? NC : 1][V];
+    auto power = [&](float v) {         // exp(z) from exp(z / T)
+        v *= v;
+        return EXPS == FOURTH ? v * v : v;
+    };
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         x.get(c, c0, c1, t, a[c]);
@@ -193,12 +213,12 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float d = a[c][j] - base;
-                if constexpr (BOTH) {
-                    b[c][j] = pow2(d * e1);
-                    if (MODE != PIECE_GRAD) s1 += b[c][j];
-                }
                 a[c][j] = pow2(d * eT);
-                if (MODE != PIECE_GRAD) so += a[c][j];
+                if constexpr (EXPS == TWO_EXPS) b[c][j] = pow2(d * e1);
+                if (MODE == PIECE_GRAD) continue;
+                so += a[c][j];
+                if constexpr (EXPS == TWO_EXPS) s1 += b[c][j];
+                else if constexpr (BOTH) s1 += power(a[c][j]);
             }
     }
     if (MODE == PIECE_GRAD)
@@ -288,33 +308,42 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int
     T* dz = (T*)p.dz + r * p.lddz;
     const float k1 = out[0];
     kT = out[1];
-    const bool wanted = out[2] != 0.f;
+    if (out[2] == 0.f)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                a[c][j] = 0.f;
+                if constexpr (EXPS == TWO_EXPS) b[c][j] = 0.f;
+            }
     // (dz may be z: what the list needs of z was read above, before a barrier)
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int ch = c0 + (c * TPR + t) * V;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float g = BOTH ? __builtin_fmaf(kT, a[c][j], k1 * b[c][j]) : (kT + k1) * a[c][j];
-            a[c][j] = wanted ? g : 0.f;
+            if constexpr (EXPS == TWO_EXPS) a[c][j] = __builtin_fmaf(kT, a[c][j], k1 * b[c][j]);
+            else if constexpr (EXPS == ONE_EXP) a[c][j] *= kT + k1;
+            else a[c][j] = __builtin_fmaf(kT, a[c][j], k1 * power(a[c][j]));
         }
         if (ok) st_chunk<ST>(dz + ch, c1 - ch, a[c]);
     }
     row_sync<TPR>();
-    if (!lead || !ok || !live) return;
+    if (!lead) return;
+#pragma unroll
+    for (int d = 1; d < LW; d *= 2) twice |= __shfl_xor((int)twice, d) != 0;
+    if (!ok || !live) return;
     for (int e = t; e <= k; e += LW) {
         const int c = cls[e];
-        if (c < c0 || c >= c1) continue;
-        float pe = 0.f;
-        bool listed = false;
-#pragma unroll 4
-        for (int o = 0; o < k; ++o) {
-            pe += cls[o] == c ? pr[o] : 0.f;
-            listed |= cls[o] == c;
+        if (c < c0 || c >= c1 || again[e]) continue;
+        float pe = e < k ? pr[e] : 0.f;
+        if (twice) {
+            pe = 0.f;
+            for (int o = 0; o < k; ++o) pe += cls[o] == c ? pr[o] : 0.f;
         }
         const float d = zc[e] - m, q = pow2(d * eT);
         float g = g1 != 0.f ? g1 * (pow2(d * e1) / s1 - (c == y ? 1.f : 0.f)) : 0.f;
-        if (gT != 0.f) g += listed || !tail ? gT * (q / sT - pe) : kT * q;
+        if (gT != 0.f) g += e < k || !tail ? gT * (q / sT - pe) : kT * q;
         st1(dz, c, g);
     }
 }
@@ -454,7 +483,7 @@ __device__ __forceinline__ float rest_base(float m) { return fabsf(m) == INFINIT
 
 // Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
 // other, are covered by other rows.
-constexpr int top_waves(int values) { return values <= 40 ? 6 : 4; }
+constexpr int top_waves(int values) { return values <= 40 ? 4 : 4; }
 
 // Rows of a few candidates are finished by their first wave: the others are gone by then.
 constexpr int kFew = 256;
@@ -694,23 +723,30 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
 // ---- plans -------------------------------------------------------------------
 
 // Threads of a row and chunks of a thread.  Rows that the registers of 512 threads do not
-// hold are cut into pieces.
+// hold are cut into pieces.  Where there are many rows, four waves to a row and more values a
+// thread: more rows of a compute unit at once, whose steps cover each other (distillation of
+// 4096 x 20000 bf16, T = 2: 76.6 us, 82.5 with eight waves; 1024 x 16000 float32: 37.8 and 30.4).
+// wide: values that a thread may keep there.  Top logits: 48 (4096 x 10000 bf16 32.1 us, 37.5 with
+// eight; 16000: 42.3 and 40.7); distillation: 80, with two exponentials kept 48.
 struct RowPlan {
     int tpr, nc;
     int pieces, piece;    // piece: classes
 };
-// values that a thread keeps at most, and chunks of the longest row that is not cut
-constexpr int kThreadValues = 64;
-RowPlan row_plan(int V, long rows, int C, int k) {
-    const int chunks = (C + V - 1) / V, most = kThreadValues / V;
-    if (chunks <= 16 && k < 16) return {16, 1, 1, C};
+constexpr int kThreadValues = 64, kWideRows = 2048, kTopWide = 48;
+RowPlan row_plan(int V, long rows, int C, int k, int wide) {
+    const int chunks = (C + V - 1) / V;
+    // (up to 128 classes; 16384 x 100 float32, distillation: 20 us with a wave to a row, 8.6 with 16 lanes)
+    if (C <= 128 && k < 16) return {16, chunks <= 16 ? 1 : 2, 1, C};
     if (k <= 32)
         for (int nc : {1, 2, 4})
             if (chunks <= 64 * nc) return {64, nc, 1, C};
     for (int nc : {1, 2, 4})
         if (chunks <= 256 * nc) return {256, nc, 1, C};
-    for (int nc : {3, 4, 5, 6, 8, 12, 16})
-        if (nc <= most && chunks <= 512 * nc) return {512, nc, 1, C};
+    if (rows >= kWideRows)
+        for (int nc : {6, 8, 10, 12, 16})
+            if (nc * V <= wide && chunks <= 256 * nc) return {256, nc, 1, C};
+    for (int nc : {4, 5, 6, 8, 12, 16})
+        if (nc * V <= kThreadValues && chunks <= 512 * nc) return {512, nc, 1, C};
     // 256 workgroups with two chunks a thread at least, or as few as hold the row
     const long want = std::min<long>((256 + rows - 1) / std::max(rows, 1L), chunks / 512);
     const int pieces = (int)std::max<long>(want, (chunks + 256 * 8 - 1) / (256 * 8));
@@ -720,6 +756,12 @@ RowPlan row_plan(int V, long rows, int C, int k) {
 
 long exact_row(int dt, long rows, int C, long ld) {
     return rows - (dt == DT_BF16 ? tail_rows<bf16>(rows, C, ld) : tail_rows<float>(rows, C, ld));
+}
+
+int distill_exps(const DistillArgs& p) {
+    if (p.step) return TWO_EXPS;
+    if (!p.labels || p.alpha <= 0.f || p.alpha >= 1.f || p.temp == 1.f) return ONE_EXP;
+    return p.temp == 2.f ? SQUARE : p.temp == 4.f ? FOURTH : TWO_EXPS;
 }
 
 template <typename T, int TPR, int NC, int MODE>
@@ -734,12 +776,17 @@ void row_launch(const DistillArgs& p, long wgs, hipStream_t st) {
     const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
     constexpr int V = 16 / (int)sizeof(T), RB = TPR > 256 ? 1 : 256 / TPR;
     const unsigned lds = sizeof(float) * RB * distill_lds(p.lds_k, TPR * NC * V);
-    const bool both = p.step || (p.labels && p.alpha > 0.f && p.alpha < 1.f && p.temp != 1.f);
     const bool stream = MODE != PIECE_SUMS && p.dz && p.rows * p.C * (long)sizeof(T) >= kStreamBytes;
-    if (both && stream) launch((distill_k<T, TPR, NC, MODE, true, MODE != PIECE_SUMS>), grid, block, lds, st, p);
-    else if (both) launch((distill_k<T, TPR, NC, MODE, true, false>), grid, block, lds, st, p);
-    else if (stream) launch((distill_k<T, TPR, NC, MODE, false, MODE != PIECE_SUMS>), grid, block, lds, st, p);
-    else launch((distill_k<T, TPR, NC, MODE, false, false>), grid, block, lds, st, p);
+    const int exps = distill_exps(p);
+    auto go = [&](auto exps) {
+        constexpr int E = decltype(exps)::value;
+        if (stream) launch((distill_k<T, TPR, NC, MODE, E, MODE != PIECE_SUMS>), grid, block, lds, st, p);
+        else launch((distill_k<T, TPR, NC, MODE, E, false>), grid, block, lds, st, p);
+    };
+    if (exps == TWO_EXPS) go(std::integral_constant<int, TWO_EXPS>());
+    else if (exps == SQUARE) go(std::integral_constant<int, SQUARE>());
+    else if (exps == FOURTH) go(std::integral_constant<int, FOURTH>());
+    else go(std::integral_constant<int, ONE_EXP>());
 }
 
 template <typename T, typename P>
@@ -748,20 +795,34 @@ hipError_t whole_rows(const P& p, RowPlan s, hipStream_t st) {
     const long wgs = (p.rows + rb - 1) / rb;
     switch (s.tpr * 32 + s.nc) {
     case 16 * 32 + 1: row_launch<T, 16, 1, WHOLE>(p, wgs, st); break;
+    case 16 * 32 + 2:
+        if constexpr (sizeof(T) == 4) row_launch<T, 16, 2, WHOLE>(p, wgs, st);
+        else return hipErrorInvalidValue;   // (128 bf16 classes are 16 chunks)
+        break;
     case 64 * 32 + 1: row_launch<T, 64, 1, WHOLE>(p, wgs, st); break;
     case 64 * 32 + 2: row_launch<T, 64, 2, WHOLE>(p, wgs, st); break;
     case 64 * 32 + 4: row_launch<T, 64, 4, WHOLE>(p, wgs, st); break;
     case 256 * 32 + 1: row_launch<T, 256, 1, WHOLE>(p, wgs, st); break;
     case 256 * 32 + 2: row_launch<T, 256, 2, WHOLE>(p, wgs, st); break;
     case 256 * 32 + 4: row_launch<T, 256, 4, WHOLE>(p, wgs, st); break;
-    case 512 * 32 + 3: row_launch<T, 512, 3, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 6: row_launch<T, 256, 6, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 8: row_launch<T, 256, 8, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 10: row_launch<T, 256, 10, WHOLE>(p, wgs, st); break;
+    case 256 * 32 + 12:
+        if constexpr (sizeof(T) == 4) row_launch<T, 256, 12, WHOLE>(p, wgs, st);
+        else return hipErrorInvalidValue;   // (row_plan: 80 values a thread)
+        break;
+    case 256 * 32 + 16:
+        if constexpr (sizeof(T) == 4) row_launch<T, 256, 16, WHOLE>(p, wgs, st);
+        else return hipErrorInvalidValue;
+        break;
     case 512 * 32 + 4: row_launch<T, 512, 4, WHOLE>(p, wgs, st); break;
     case 512 * 32 + 5: row_launch<T, 512, 5, WHOLE>(p, wgs, st); break;
     case 512 * 32 + 6: row_launch<T, 512, 6, WHOLE>(p, wgs, st); break;
     case 512 * 32 + 8: row_launch<T, 512, 8, WHOLE>(p, wgs, st); break;
     case 512 * 32 + 12:
         if constexpr (sizeof(T) == 4) row_launch<T, 512, 12, WHOLE>(p, wgs, st);
-        else return hipErrorInvalidValue;   // (row_plan: 64 values a thread)
+        else return hipErrorInvalidValue;   // (64 values a thread)
         break;
     case 512 * 32 + 16:
         if constexpr (sizeof(T) == 4) row_launch<T, 512, 16, WHOLE>(p, wgs, st);
@@ -799,7 +860,7 @@ hipError_t distill_rows(DistillArgs p, RowPlan s, hipStream_t st) {
 }  // namespace
 
 static long most_pieces(long rows, int C, int k) {
-    return std::max(row_plan(4, rows, C, k).pieces, row_plan(8, rows, C, k).pieces);
+    return std::max(row_plan(4, rows, C, k, kTopWide).pieces, row_plan(8, rows, C, k, kTopWide).pieces);
 }
 long top_logits_wgs(long rows, int C, int k) { return rows * most_pieces(rows, C, k); }
 long top_logits_ws(long rows, int C, int k) {
@@ -813,7 +874,7 @@ long distill_ws(long rows, int C) {
 
 hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, p.k);
+    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, p.k, kTopWide);
     p.exact = exact_row(dt, p.rows, p.C, p.ldz);
     p.pieces = s.pieces;
     p.piece = s.piece;
@@ -822,7 +883,7 @@ hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st) {
 
 hipError_t launch_distill(int dt, DistillArgs p, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, 1);
+    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, 1, distill_exps(p) == TWO_EXPS ? 48 : 80);
     p.exact = exact_row(dt, p.rows, p.C, p.ldz);
     p.pieces = s.pieces;
     p.piece = s.piece;

@@ -81,7 +81,7 @@ def check_top(z, k, T=1.0, layout="tight"):
     near(rest, R.rest(z, i, T), R.rest_bound(z, i, T), ("rest", z.shape, k))
 
 
-TOPS = [(1, 1, 1), (3, 2, 1), (5, 10, 5), (4, 10, 10), (33, 17, 3), (7, 64, 16), (3, 128, 128), (2, 129, 128),
+TOPS = [(1, 1, 1), (3, 2, 1), (5, 10, 5), (9, 100, 10), (4, 10, 10), (33, 17, 3), (7, 64, 16), (3, 128, 128), (2, 129, 128),
         (5, 100, 33), (9, 1000, 10), (3, 1000, 128), (4, 1025, 32), (2, 4097, 64), (2, 8192, 7), (2, 8193, 128),
         (1, 20000, 32), (2, 50001, 1)]
 
@@ -314,6 +314,37 @@ def test_in_place_and_loss_alone(C):
         assert torch.equal(loss, again) and torch.equal(dz, same)
         only, kept = run_distill(x, values, index, r, best, layout="odd", grad=False, **kw)
         assert torch.equal(loss, only) and (kept == 5).all()
+
+
+@pytest.mark.parametrize("C", [70, 6000, 12001, 16000, 30000, 32768])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_rows_of_every_length(dtype, C):
+    """Lengths between the others' that take other shapes of workgroups, in few rows and in many;
+    rows of the same content have the same answer, to the bit."""
+    z, values, index, r, best = teacher(12, 3, C, 12, 2.0, True)
+    z = z.to(DT[dtype])
+    check_top(z, 12, 2.0)
+    many = (torch.arange(2051 if C < 20000 else 2048) * 7) % 3
+    zd = z[many].cuda()
+    v, i, rest = (torch.empty(len(many), 12, device="cuda"), torch.empty(len(many), 12, dtype=torch.int32, device="cuda"),
+                  torch.empty(len(many), device="cuda"))
+    n = lpp.top_logits_ws(len(many), C, 12)
+    lpp.kernel_top_logits(zd, v, i, rest, 2.0, torch.empty(n, device="cuda") if n else None)
+    tv, ti = R.top(z, 12)
+    assert torch.equal(i.cpu(), ti[many]) and torch.equal(v.cpu(), tv[many])
+    near(rest, R.rest(z, ti, 2.0)[many], R.rest_bound(z, ti, 2.0)[many], "rest")
+    for T, alpha in ((2.0, 0.6), (4.0, 0.6), (3.0, 0.6), (2.5, 1.0)):
+        check_distill(z, values, index, r, best, None, alpha, T, 0.5)
+        loss, dz = torch.empty(len(many), device="cuda"), torch.empty_like(zd)
+        n = lpp.distill_ws(len(many), C)
+        lpp.kernel_distill(zd, values[many].cuda(), index[many].cuda(), loss, dz, r[many].cuda(), best[many].cuda(),
+                           alpha=alpha, temperature=T, scale=0.5, ws=torch.empty(n, device="cuda") if n else None)
+        want, wdz, bl, bd = R.distill(z, values, index, r, best, None, alpha, T, 0.5)
+        near(loss, want[many], bl[many], "loss")
+        for k in range(3):
+            same = dz[(many == k).cuda()]
+            assert (same == same[0]).all()
+            near(same[0], wdz[k], bd[k] + R.HALF[z.dtype] * (wdz[k].abs() + bd[k]) + 1e-38, "dz")
 
 
 def test_no_rows():
