@@ -246,6 +246,55 @@ def test_in_place(dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), which
 
 
+# maps that take every shape of workgroup: many images, groups inside a vector, whole vectors, any
+LARGE = [(100, 3136, 16, 4), (100, 3136, 32, 4), (100, 3136, 16, 16), (260, 100, 64, 2), (600, 49, 64, 32),
+         (24, 784, 100, 4), (300, 196, 48, 16), (64, 1000, 40, 8), (1100, 16, 32, 8), (40, 600, 64, 32), (270, 1024, 16, 2),
+         (60, 900, 24, 8), (60, 400, 24, 3), (60, 400, 32, 16), (2000, 100, 16, 2), (560, 1500, 8, 4), (520, 800, 16, 2),
+         (600, 700, 16, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", LARGE, ids=lambda s: "x".join(map(str, s)))
+def test_large(shape, dtype):
+    n, p, C, G = shape
+    act = ("relu", "silu", "none")[(n + G) % 3]
+    x, gamma, beta, dy, dres, mean, rstd = gradient_inputs(n, n, p, C, G, dtype, act)
+    got = run_forward(x, n, G, gamma, beta, act)
+    want = R.forward(x, n, G, gamma, beta, EPS, act)
+    bounds = R.forward_bounds(x, n, G, gamma, beta, EPS, act)
+    for k in range(3):
+        near(got[k], want[k], bounds[k], ("forward", k))
+    dx, dg, db = torch.empty_like(x, device="cuda"), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    b, ws = space(lpp.groupnorm_bwd_ws(n, p, C, G))
+    lpp.kernel_groupnorm_bwd(dy.cuda(), x.cuda(), n, G, gamma.cuda(), beta.cuda(), mean.cuda(), rstd.cuda(), dx, dg, db, ws,
+                             act=ACT[act])
+    assert guarded(b)
+    want = R.backward(dy, x, n, G, gamma, beta, mean, rstd, act)
+    bounds = list(R.backward_bounds(dy, x, n, G, gamma, beta, mean, rstd, act))
+    bounds[0] = bounds[0] + R.HALF[x.dtype] * (want[0].abs() + bounds[0]) + 1e-38
+    for k in range(3):
+        near((dx, dg, db)[k], want[k], bounds[k], ("gradient", k))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_gradient_decides_as_the_forward_pass(dtype):
+    """Where a ReLU let nothing through its gradient does not either, also next to 0: the output
+    itself says, and dy = 1 without the statistics' terms (one value a group)."""
+    n, p, C, G = 2, 1500, 16, 4
+    x, gamma, beta, _, _ = make(8, n, p, C, "fp32")
+    beta = -gamma * 0.25
+    x = x.to(DT[dtype])
+    y, mean, rstd = run_forward(x, n, G, gamma, beta, "relu")
+    db = torch.empty(C, device="cuda")
+    for c in range(0, C, 5):      # dbeta of a one-hot column counts its open decisions
+        dy = torch.zeros_like(x)
+        dy[:, c] = 1
+        ws = torch.empty(lpp.groupnorm_bwd_ws(n, p, C, G), device="cuda")
+        lpp.kernel_groupnorm_bwd(dy.cuda(), x.cuda(), n, G, gamma.cuda(), beta.cuda(), mean, rstd, dbeta=db, ws=ws,
+                                 act=ACT["relu"])
+        assert db[c] == (y[:, c] > 0).sum() and int((db != 0).sum()) <= 1
+
+
 def test_no_images():
     dg, db = torch.full((12,), 5.0, device="cuda"), torch.full((12,), 5.0, device="cuda")
     z, v = torch.empty(0, 12, device="cuda"), torch.ones(12, device="cuda")
