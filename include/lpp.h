@@ -510,8 +510,8 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* args, void* stream);
  * ws: lpp_groupnorm_ws / lpp_groupnorm_bwd_ws floats of device memory (16-byte aligned, may
  * be NULL where that is 0), scratch of this call until it has run: calls that may
  * overlap need their own.  -1 for sizes that the calls refuse, LPP_EUNSUPPORTED for more
- * than 2^31 workgroups (more than 2^24 channels or 2^40 elements: LPP_EINVAL).  dtype, streams,
- * capture and errors as above.
+ * than 2^32 threads in a launch, 256 an image at least (more than 2^24 channels or 2^40 elements:
+ * LPP_EINVAL).  dtype, streams, capture and errors as above.
  */
 enum lpp_act { LPP_ACT_NONE = 0, LPP_ACT_RELU = 1, LPP_ACT_SILU = 2 };
 typedef struct {
@@ -562,8 +562,9 @@ int lpp_kernel_groupnorm_bwd(const lpp_groupnorm_bwd_args* args, void* stream);
  * are equal; a NaN is above everything) and, if rest is not NULL (float32 [rows]),
  *     rest = log of the sum of exp(z / temperature) over all other classes
  * (-inf where none has a value above -inf).  1 <= k <= min(classes, 128)
- * (LPP_EUNSUPPORTED for more than 128); temperature > 0 and finite.  ws:
- * lpp_top_logits_ws(rows, classes, k) floats, as above.  rows == 0 is valid.
+ * (LPP_EUNSUPPORTED for more than 128, and for more than 2^32 threads in a launch, up to 1024 a
+ * row); temperature > 0 and finite.  ws: lpp_top_logits_ws(rows, classes, k) floats, as above.
+ * rows == 0 is valid.
  */
 typedef struct {
     const void* z;
@@ -598,8 +599,8 @@ int lpp_kernel_top_logits(const lpp_top_logits_args* args, void* stream);
  * has loss 0 and gradient 0, whatever it holds.  weight: float32 [rows], NULL for 1.  A class that
  * is listed twice counts with both entries.  Logits of -inf (masked classes) take no
  * part; a row with an infinity or NaN otherwise is NaN.
- * 1 <= k <= 128; classes >= 1; 0 <= alpha <= 1; temperature > 0; scale finite.  ws:
- * lpp_distill_ws(rows, classes) floats, as above.  rows == 0 is valid.
+ * 1 <= k <= 128; classes >= 1; 0 <= alpha <= 1; temperature > 0; scale finite; threads of a
+ * launch as above.  ws: lpp_distill_ws(rows, classes) floats, as above.  rows == 0 is valid.
  */
 typedef struct {
     const void* z;

@@ -481,9 +481,7 @@ __device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slo
 // base m where that is finite
 __device__ __forceinline__ float rest_base(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
 
-// Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
-// other, are covered by other rows.
-constexpr int top_waves(int values) { return values <= 40 ? 4 : 4; }
+constexpr int kTopWaves = 4;      // a SIMD, that the registers are kept to
 
 // Rows of a few candidates are finished by their first wave: the others are gone by then.
 constexpr int kFew = 256;
@@ -499,7 +497,7 @@ constexpr int kFew = 256;
 // where the values under it add up to less than 1, so that the bound may lie far above them,
 // they are summed again relative to their largest.
 template <typename T, int TPR, int NC, int MODE, int G>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves(NC * 16 / (int)sizeof(T))) void top_logits_k(TopArgs p) {
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, kTopWaves) void top_logits_k(TopArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
     constexpr int LW = TPR < 64 ? TPR : 64;
@@ -732,7 +730,9 @@ struct RowPlan {
     int tpr, nc;
     int pieces, piece;    // piece: classes
 };
-constexpr int kThreadValues = 64, kWideRows = 2048, kTopWide = 48;
+constexpr int kThreadValues = 64, kWideRows = 2048, kTopWide = 48, kDistillWide = 80, kTwoWide = 48;
+// whether a row of TPR threads with `values` each is one of row_plan's with `wide`
+constexpr bool planned(int tpr, int values, int wide) { return tpr != 256 || values <= wide; }
 RowPlan row_plan(int V, long rows, int C, int k, int wide) {
     const int chunks = (C + V - 1) / V;
     // (up to 128 classes; 16384 x 100 float32, distillation: 20 us with a wave to a row, 8.6 with 16 lanes)
@@ -767,9 +767,14 @@ int distill_exps(const DistillArgs& p) {
 template <typename T, int TPR, int NC, int MODE>
 void row_launch(const TopArgs& p, long wgs, hipStream_t st) {
     const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
+    constexpr int values = NC * 16 / (int)sizeof(T);
     if constexpr (TPR <= 64) launch((top_logits_k<T, TPR, NC, MODE, TPR>), grid, block, 0, st, p);
-    else if (p.k <= 32) launch((top_logits_k<T, TPR, NC, MODE, 64>), grid, block, 0, st, p);
-    else launch((top_logits_k<T, TPR, NC, MODE, 256>), grid, block, 0, st, p);
+    else if constexpr (MODE != WHOLE || planned(TPR, values, kTopWide)) {
+        // (TPR 256, NC 1: k > 32, fewer would be a wave's)
+        if constexpr (TPR != 256 || NC > 1)
+            if (p.k <= 32) return launch((top_logits_k<T, TPR, NC, MODE, 64>), grid, block, 0, st, p);
+        launch((top_logits_k<T, TPR, NC, MODE, 256>), grid, block, 0, st, p);
+    }
 }
 template <typename T, int TPR, int NC, int MODE>
 void row_launch(const DistillArgs& p, long wgs, hipStream_t st) {
@@ -783,8 +788,9 @@ void row_launch(const DistillArgs& p, long wgs, hipStream_t st) {
         if (stream) launch((distill_k<T, TPR, NC, MODE, E, MODE != PIECE_SUMS>), grid, block, lds, st, p);
         else launch((distill_k<T, TPR, NC, MODE, E, false>), grid, block, lds, st, p);
     };
-    if (exps == TWO_EXPS) go(std::integral_constant<int, TWO_EXPS>());
-    else if (exps == SQUARE) go(std::integral_constant<int, SQUARE>());
+    if (exps == TWO_EXPS) {
+        if constexpr (MODE != WHOLE || planned(TPR, NC * V, kTwoWide)) go(std::integral_constant<int, TWO_EXPS>());
+    } else if (exps == SQUARE) go(std::integral_constant<int, SQUARE>());
     else if (exps == FOURTH) go(std::integral_constant<int, FOURTH>());
     else go(std::integral_constant<int, ONE_EXP>());
 }
@@ -862,7 +868,17 @@ hipError_t distill_rows(DistillArgs p, RowPlan s, hipStream_t st) {
 static long most_pieces(long rows, int C, int k) {
     return std::max(row_plan(4, rows, C, k, kTopWide).pieces, row_plan(8, rows, C, k, kTopWide).pieces);
 }
-long top_logits_wgs(long rows, int C, int k) { return rows * most_pieces(rows, C, k); }
+static long row_threads(long rows, int C, int k, int wide) {
+    long most = 0;
+    for (int V : {4, 8}) {
+        const RowPlan s = row_plan(V, rows, C, k, wide);
+        const int rb = s.tpr < 256 ? 256 / s.tpr : 1;
+        most = std::max(most, s.pieces > 1 ? rows * std::max(256 * s.pieces, kMergeThreads) : (rows + rb - 1) / rb * rb * s.tpr);
+    }
+    return most;
+}
+long top_logits_threads(long rows, int C, int k) { return row_threads(rows, C, k, kTopWide); }
+long distill_threads(long rows, int C) { return std::max(row_threads(rows, C, 1, kDistillWide), row_threads(rows, C, 1, kTwoWide)); }
 long top_logits_ws(long rows, int C, int k) {
     const long pieces = most_pieces(rows, C, k);
     return pieces > 1 ? (rows * pieces * (2L * k) + 3) / 4 * 4 + rows * pieces * 4 : 0;
@@ -883,7 +899,7 @@ hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st) {
 
 hipError_t launch_distill(int dt, DistillArgs p, hipStream_t st) {
     if (p.rows <= 0) return hipSuccess;
-    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, 1, distill_exps(p) == TWO_EXPS ? 48 : 80);
+    const RowPlan s = row_plan(dt == DT_BF16 ? 8 : 4, p.rows, p.C, 1, distill_exps(p) == TWO_EXPS ? kTwoWide : kDistillWide);
     p.exact = exact_row(dt, p.rows, p.C, p.ldz);
     p.pieces = s.pieces;
     p.piece = s.piece;

@@ -504,6 +504,9 @@ GnShape gn_shape(int V, long images, long pixels, int C, int G) {
     return s;
 }
 
+// workgroups that sum dgamma and dbeta, a multiple of the 8 XCDs
+int column_wgs(const GnShape& s) { return ((2 * s.cp + kColumns - 1) / kColumns + 7) / 8 * 8; }
+
 template <typename T, int ACT>
 void gn_launch(const GnArgs& p, unsigned wgs, hipStream_t st) {
     launch((gn_stats_k<T>), dim3(wgs), dim3(TB), 0, st, p);
@@ -516,8 +519,7 @@ template <typename T, int ACT>
 void gn_bwd_launch(GnBwdArgs p, unsigned wgs, hipStream_t st) {
     if (wgs) launch((gn_bwd_sums_k<T, ACT>), dim3(wgs), dim3(TB), 0, st, p);
     // (workgroups with the same rows go to the same XCD in both kernels)
-    const unsigned columns = (unsigned)((2 * p.s.cp + kColumns - 1) / kColumns);
-    p.extra = p.dgamma || p.dbeta ? (int)(columns + 7) / 8 * 8 : 0;
+    p.extra = p.dgamma || p.dbeta ? column_wgs(p.s) : 0;
     const unsigned grid = p.extra + (p.dx ? wgs : 0);
     if (grid == 0) return;
     if (p.s.images * p.s.pixels * p.s.C * (long)sizeof(T) >= kStreamBytes)
@@ -528,13 +530,13 @@ void gn_bwd_launch(GnBwdArgs p, unsigned wgs, hipStream_t st) {
 
 }  // namespace
 
-long groupnorm_wgs(long images, long pixels, int C, int G) {
+long groupnorm_threads(long images, long pixels, int C, int G) {
     long most = 0;
     for (int V : {4, 8}) {
         const GnShape s = gn_shape(V, images, pixels, C, G);
-        most = std::max(most, images * s.slabs * s.splits);
+        most = std::max(most, images * s.slabs * s.splits + column_wgs(s));
     }
-    return most;
+    return most * TB;
 }
 long groupnorm_ws(long images, long pixels, int C, int G) {
     long most = 0;

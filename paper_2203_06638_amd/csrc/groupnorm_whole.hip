@@ -384,6 +384,9 @@ void whole_launch(const GnBwdArgs& p, const GnWhole& s, hipStream_t st) {
     else
         launch((gn_whole_bwd_k<T, TB, NC, S, false>), grid, dim3(TB), lds, st, p, s);
 }
+// (bf16 channels with statistics of their own, gradient: the registers of 8 chunks would spill)
+template <typename T, int S>
+constexpr int kBwdChunks = S == 8 && sizeof(T) == 2 ? 4 : 8;
 template <typename T, int S>
 hipError_t whole_dispatch(const GnArgs& p, const GnWhole& s, hipStream_t st) {
     switch (s.threads * 32 + s.nc) {
@@ -409,12 +412,18 @@ hipError_t whole_dispatch(const GnBwdArgs& p, const GnWhole& s, hipStream_t st) 
     case 256 * 32 + 1: whole_launch<T, 256, 1, S>(p, s, st); break;
     case 256 * 32 + 2: whole_launch<T, 256, 2, S>(p, s, st); break;
     case 256 * 32 + 4: whole_launch<T, 256, 4, S>(p, s, st); break;
-    case 256 * 32 + 8: whole_launch<T, 256, 8, S>(p, s, st); break;
+    case 256 * 32 + 8:
+        if constexpr (kBwdChunks<T, S> >= 8) whole_launch<T, 256, 8, S>(p, s, st);
+        break;
     case 512 * 32 + 4: whole_launch<T, 512, 4, S>(p, s, st); break;
-    case 512 * 32 + 8: whole_launch<T, 512, 8, S>(p, s, st); break;
+    case 512 * 32 + 8:
+        if constexpr (kBwdChunks<T, S> >= 8) whole_launch<T, 512, 8, S>(p, s, st);
+        break;
     case 1024 * 32 + 2: whole_launch<T, 1024, 2, S>(p, s, st); break;
     case 1024 * 32 + 4: whole_launch<T, 1024, 4, S>(p, s, st); break;
-    case 1024 * 32 + 8: whole_launch<T, 1024, 8, S>(p, s, st); break;
+    case 1024 * 32 + 8:
+        if constexpr (kBwdChunks<T, S> >= 8) whole_launch<T, 1024, 8, S>(p, s, st);
+        break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -496,9 +505,9 @@ GnWhole groupnorm_whole(int V, long images, long pixels, int C, int G, long ld, 
     // 32 images, gradient, 320 workgroups: 41 us against 35).
     const long slots = 256 * (1024 / size->threads), rounds = (wgs + slots - 1) / slots;
     if (size->nc > 8 && wgs < 96) return s;
-    // (bf16 channels with statistics of their own: their registers spill)
-    if (bwd && s.slots == 8 && size->nc == 8) return s;
+    if (bwd && s.slots == 8 && size->nc > kBwdChunks<bf16, 8>) return s;
     if (size->nc >= 8 && wgs > slots && wgs < 0.7 * rounds * slots) return s;
+    if (8L * s.per_xcd * size->threads > kLaunchThreads) return s;
     s.threads = size->threads;
     s.nc = size->nc;
     return s;

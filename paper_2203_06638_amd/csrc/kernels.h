@@ -479,6 +479,7 @@ hipError_t launch_rmsnorm_bwd(int dt, RmsBwdArgs p, hipStream_t st);
 // As lpp_kernel_top_logits and lpp_kernel_distill; the fields after the blank line are set
 // by the launcher.  step: the teacher and the labels are read from there on the device.
 constexpr int kDistillMaxK = 128;
+constexpr long kLaunchThreads = 0xffffffffl;   // of one launch (its size is a 32-bit count of threads)
 struct TopArgs {
     const void* z;
     long ldz, rows;
@@ -510,10 +511,11 @@ struct DistillArgs {
     long exact;
     int pieces, piece, grid_pieces, lds_k;
 };
-// floats of ws, and the workgroups of a launch
+// floats of ws, and the threads of a launch
 long top_logits_ws(long rows, int C, int k);
-long top_logits_wgs(long rows, int C, int k);
+long top_logits_threads(long rows, int C, int k);
 long distill_ws(long rows, int C);
+long distill_threads(long rows, int C);
 hipError_t launch_top_logits(int dt, TopArgs p, hipStream_t st);
 hipError_t launch_distill(int dt, DistillArgs p, hipStream_t st);
 
@@ -570,10 +572,10 @@ struct GnBwdArgs {
 hipError_t launch_groupnorm_whole(int dt, const GnArgs& p, const GnWhole& s, hipStream_t st);
 // (p.ws null: the image's sums are dgamma and dbeta; else [image][2][p.s.cp])
 hipError_t launch_groupnorm_whole_bwd(int dt, const GnBwdArgs& p, const GnWhole& s, hipStream_t st);
-// floats of ws, and the workgroups of a launch
+// floats of ws, and the threads of a launch
 long groupnorm_ws(long images, long pixels, int C, int G);
 long groupnorm_bwd_ws(long images, long pixels, int C, int G);
-long groupnorm_wgs(long images, long pixels, int C, int G);
+long groupnorm_threads(long images, long pixels, int C, int G);
 hipError_t launch_groupnorm(int dt, GnArgs p, long images, long pixels, int C, int G, hipStream_t st);
 hipError_t launch_groupnorm_bwd(int dt, GnBwdArgs p, long images, long pixels, int C, int G, hipStream_t st);
 

@@ -1929,7 +1929,7 @@ int lpp_init(const lpp_model_desc* desc, int K, int P, const lpp_options* opt, l
         }
         if (Y.L.op == LPP_GROUPNORM) {
             const long pixels = (long)Y.out.h * Y.out.w;
-            if (lpp::groupnorm_wgs(N, pixels, Y.out.c, Y.L.k) >= (1L << 30))
+            if (lpp::groupnorm_threads(N, pixels, Y.out.c, Y.L.k) > lpp::kLaunchThreads)
                 return fail(LPP_EUNSUPPORTED, "group norm: too many images for one launch");
             Y.aux = take(sizeof(float) * 2 * (size_t)N * Y.L.k);   // mean, rstd
             scratch = std::max({scratch, lpp::groupnorm_ws(N, pixels, Y.out.c, Y.L.k),
@@ -2125,6 +2125,8 @@ int lpp_step_distill(lpp_ctx* c, int worker, const lpp_batch* batch, const lpp_t
     if (!(t->alpha >= 0.f && t->alpha <= 1.f)) return fail(LPP_EINVAL, "alpha must be in [0, 1]");
     if (!(t->temperature > 0.f) || !std::isfinite(t->temperature))
         return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (c && lpp::distill_threads(c->M.desc.batch, c->M.desc.n_classes) > lpp::kLaunchThreads)
+        return fail(LPP_EUNSUPPORTED, "the batch has too many images for one launch");
     return step(c, worker, batch, t, partition, lr);
 }
 
@@ -2140,6 +2142,8 @@ int lpp_top_logits(lpp_ctx* c, int worker, int k, float temperature, float* valu
     if (!(temperature > 0.f) || !std::isfinite(temperature))
         return fail(LPP_EINVAL, "temperature must be positive and finite");
     if (w.last_partition < 0) return fail(LPP_ESTATE, "the worker has made no step");
+    if (lpp::top_logits_threads(M.desc.batch, M.desc.n_classes, k) > lpp::kLaunchThreads)
+        return fail(LPP_EUNSUPPORTED, "the batch has too many images for one launch");
     lpp::TopArgs a{};
     a.z = c->act(w, (int)M.layers.size() - 1);
     a.ldz = a.C = M.desc.n_classes;
@@ -2781,7 +2785,7 @@ int lpp_kernel_groupnorm(const lpp_groupnorm_args* a, void* stream) {
     const long need = lpp::groupnorm_ws(a->images, a->pixels, a->channels, a->groups);
     if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
         return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_groupnorm_ws floats");
-    if (lpp::groupnorm_wgs(a->images, a->pixels, a->channels, a->groups) >= (1L << 31) - 1)
+    if (lpp::groupnorm_threads(a->images, a->pixels, a->channels, a->groups) > lpp::kLaunchThreads)
         return fail(LPP_EUNSUPPORTED, "too many images for one launch");
     lpp::GnArgs p{};
     p.x = a->x;
@@ -2824,7 +2828,7 @@ int lpp_kernel_groupnorm_bwd(const lpp_groupnorm_bwd_args* a, void* stream) {
     const long need = lpp::groupnorm_bwd_ws(a->images, a->pixels, a->channels, a->groups);
     if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
         return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_groupnorm_bwd_ws floats");
-    if (lpp::groupnorm_wgs(a->images, a->pixels, a->channels, a->groups) >= (1L << 30))
+    if (lpp::groupnorm_threads(a->images, a->pixels, a->channels, a->groups) > lpp::kLaunchThreads)
         return fail(LPP_EUNSUPPORTED, "too many images for one launch");
     lpp::GnBwdArgs p{};
     p.dy = a->dy;
@@ -2874,7 +2878,7 @@ int lpp_kernel_top_logits(const lpp_top_logits_args* a, void* stream) {
     const long need = lpp::top_logits_ws(a->rows, a->classes, a->k);
     if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
         return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_top_logits_ws floats");
-    if (lpp::top_logits_wgs(a->rows, a->classes, a->k) >= (1L << 31) - 1)
+    if (lpp::top_logits_threads(a->rows, a->classes, a->k) > lpp::kLaunchThreads)
         return fail(LPP_EUNSUPPORTED, "too many rows for one launch");
     lpp::TopArgs p{};
     p.z = a->z;
@@ -2915,7 +2919,7 @@ int lpp_kernel_distill(const lpp_distill_args* a, void* stream) {
     const long need = lpp::distill_ws(a->rows, a->classes);
     if (need > 0 && (!a->ws || ((uintptr_t)a->ws & 15) || a->ws_floats < need))
         return fail(LPP_EINVAL, "ws must be 16-byte aligned and hold lpp_distill_ws floats");
-    if (lpp::top_logits_wgs(a->rows, a->classes, 1) >= (1L << 31) - 1)
+    if (lpp::distill_threads(a->rows, a->classes) > lpp::kLaunchThreads)
         return fail(LPP_EUNSUPPORTED, "too many rows for one launch");
     lpp::DistillArgs p{};
     p.z = a->z;

@@ -51,6 +51,10 @@ def test_top_refusals():
                dict(classes=(1 << 24) + 1, ldz=1 << 25), dict(rows=1 << 39)):
         refused(f(**kw))
     refused(f(k=129), lpp.EUNSUPPORTED)
+    # more threads than a launch has: 256, and 1024 that merge pieces, to a row
+    refused(f(rows=1 << 24, classes=500, ldz=500, k=100, ws=None, ws_floats=0), lpp.EUNSUPPORTED)
+    rows = 1 << 22
+    refused(f(rows=rows, classes=70000, ldz=70000, ws_floats=lpp.top_logits_ws(rows, 70000, 5)), lpp.EUNSUPPORTED)
 
 
 def test_distill_refusals():
@@ -76,6 +80,7 @@ def test_distill_refusals():
                dict(ws_floats=need - 1), dict(rows=1 << 39), dict(classes=(1 << 24) + 1, ldz=1 << 25, lddz=1 << 25)):
         refused(f(**kw))
     refused(f(k=129), lpp.EUNSUPPORTED)
+    refused(f(rows=1 << 24, classes=5000, ldz=5000, lddz=5000, ws=None, ws_floats=0), lpp.EUNSUPPORTED)
 
 
 def test_binding_refuses():

@@ -48,6 +48,8 @@ def test_forward_refusals():
                            dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(ldx=1 << 50),
                            dict(ws=None), dict(ws=OKP + 8), dict(ws_floats=need - 1)]:
         refused(f(**kw))
+    # more threads than a launch has: 256 to an image
+    refused(f(images=1 << 24, pixels=1, ws_floats=lpp.groupnorm_ws(1 << 24, 1, 40, 4)), lpp.EUNSUPPORTED)
 
 
 def test_backward_refusals():
@@ -70,6 +72,7 @@ def test_backward_refusals():
                            dict(dres=OKP + 2), dict(dx=OKP + 2), dict(dtype=-1), dict(act=7), dict(ws=None),
                            dict(ws=OKP + 4), dict(ws_floats=need - 1)]:
         refused(f(**kw))
+    refused(f(images=1 << 24, pixels=1, ws_floats=lpp.groupnorm_bwd_ws(1 << 24, 1, 40, 4)), lpp.EUNSUPPORTED)
 
 
 def test_binding_refuses():
