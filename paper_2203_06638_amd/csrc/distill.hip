@@ -47,6 +47,12 @@ struct RowChunks {
 #pragma unroll
         for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(w[c]));
     }
+    // value j of chunk c
+    __device__ __forceinline__ float one(int c, int j) const {
+        const int i = sizeof(T) == 4 ? j : j >> 1;
+        const uint32_t word = i & 2 ? (i & 1 ? w[c].w : w[c].z) : (i & 1 ? w[c].y : w[c].x);
+        return __uint_as_float(sizeof(T) == 4 ? word : j & 1 ? word & 0xffff0000u : word << 16);
+    }
     // the values of chunk c, -inf behind the end
     __device__ __forceinline__ void get(int c, int c0, int c1, int t, float* v) const {
         const int n = c1 - (c0 + (c * TPR + t) * V);
@@ -73,9 +79,13 @@ __host__ __device__ inline int distill_lds(int k, int values) { return 4 * (k + 
 constexpr int kListPitch = kDistillMaxK + 4;   // floats of a row's list in the workspace
 
 // Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
-// other, are covered by other rows.
-constexpr int distill_waves(int values, bool both) {
-    return both ? (values <= 16 ? 5 : values <= 40 ? 4 : 2) : values <= 64 ? 4 : 3;
+// other, are covered by other rows.  A workgroup of 512 threads takes two of them.  (64 float32
+// values a thread, 2048 x 16000, T = 2: 61.2 us with three waves, 74.7 with four, which spill; as bf16,
+// 4096 rows: 78.0 and 76.3; two exponentials of 40 float32 values, 4096 x 10000, T = 3: 84.9 and 98.4.)
+template <typename T>
+constexpr int distill_waves(int values, bool both, int tpr) {
+    if (both) return values <= 16 ? 5 : values < 40 || (values == 40 && tpr > 256) ? 4 : tpr > 256 || values > 48 ? 2 : 3;
+    return values < 64 || (values == 64 && (tpr > 256 || sizeof(T) == 2)) ? 4 : 3;
 }
 
 // WHOLE: a row to TPR threads, in their registers, so that z is read once.  PIECE_SUMS: a
@@ -87,7 +97,7 @@ constexpr int distill_waves(int values, bool both) {
 // the sums and the gradient.  The exponentials stay in registers from the sums to the
 // gradient.
 template <typename T, int TPR, int NC, int MODE, int EXPS, bool ST>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves(NC * 16 / (int)sizeof(T), EXPS == TWO_EXPS)) void distill_k(DistillArgs p) {
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves<T>(NC * 16 / (int)sizeof(T), EXPS == TWO_EXPS, TPR)) void distill_k(DistillArgs p) {
     constexpr bool BOTH = EXPS != ONE_EXP;
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
@@ -481,7 +491,10 @@ __device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slo
 // base m where that is finite
 __device__ __forceinline__ float rest_base(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
 
-constexpr int kTopWaves = 4;      // a SIMD, that the registers are kept to
+// Waves a SIMD that the registers are kept to (2048 x 16000 float32, 32 values a thread, five waves
+// are two workgroups of 512 threads, six are three: 38.5 and 31.6 us).
+template <typename T>
+constexpr int top_waves(int values) { return values <= (sizeof(T) == 2 ? 40 : 32) ? 6 : values <= 40 ? 5 : 4; }
 
 // Rows of a few candidates are finished by their first wave: the others are gone by then.
 constexpr int kFew = 256;
@@ -497,7 +510,7 @@ constexpr int kFew = 256;
 // where the values under it add up to less than 1, so that the bound may lie far above them,
 // they are summed again relative to their largest.
 template <typename T, int TPR, int NC, int MODE, int G>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256, kTopWaves) void top_logits_k(TopArgs p) {
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves<T>(NC * 16 / (int)sizeof(T))) void top_logits_k(TopArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
     constexpr int LW = TPR < 64 ? TPR : 64;
@@ -533,20 +546,23 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, kTopWaves) void top_logits_k
     row_sync<TPR>();
     float bound;
     {
-        // (up to 64 groups every wave finds it by itself)
-        const float mine = maxima[rl][t % G];
+        // (a group's threads share the other groups)
+        constexpr int S = TPR / G, N = G / S;
+        const float* others = &maxima[rl][t % S * N];
         int larger = 0;
 #pragma unroll 4
-        for (int o = 0; o < G; o += 4) {
-            const f4 v = *(const f4*)&maxima[rl][o];
-            larger += (v[0] > mine) + (v[1] > mine) + (v[2] > mine) + (v[3] > mine);
+        for (int o = 0; o < N; o += 4) {
+            const f4 v = *(const f4*)(others + o);
+            larger += (v[0] > best) + (v[1] > best) + (v[2] > best) + (v[3] > best);
         }
-        bound = larger < p.k ? -mine : -INFINITY;
-        if constexpr (G <= 64) bound = -row_max<(G < LW ? G : LW)>(bound, fslots, none);
-        else bound = -row_max<TPR>(bound, fslots, turn);
+#pragma unroll
+        for (int d = 1; d < S; d *= 2) larger += __shfl_xor(larger, d);
+        bound = -row_max<TPR>(larger < p.k ? -best : -INFINITY, fslots, turn);
     }
+    // z / T - base / T, in powers of two, as one fma: shift is the rounded base / T, and the
+    // sum is corrected by what the rounding left out
     const float eT = kLog2e / p.temp;
-    const float base0 = rest_base(bound);
+    const float base0 = rest_base(bound), shift = base0 * eT;
     float s = 0.f;
     x.again();
 #pragma unroll
@@ -555,18 +571,25 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, kTopWaves) void top_logits_k
         x.get(c, c0, c1, t, v);
         if (!(top[c] < bound)) {
             const int ch = c0 + (c * TPR + t) * V;
+            uint32_t over = 0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                if (v[j] < bound) continue;
-                if (ch + j < c1) space.add(rank_key(v[j], ch + j));
-                v[j] = -INFINITY;
+                const bool under = v[j] < bound;
+                over |= under ? 0u : 1u << j;
+                v[j] = under ? v[j] : -INFINITY;
+            }
+            if (c1 - ch < V) over &= c1 > ch ? (1u << (c1 - ch)) - 1u : 0u;
+            for (; over; over &= over - 1) {
+                const int j = __builtin_ctz(over);
+                space.add(rank_key(x.one(c, j), ch + j));
             }
         }
         if (p.rest)
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += pow2((v[j] - base0) * eT);
+            for (int j = 0; j < V; ++j) s += pow2(__builtin_fmaf(v[j], eT, -shift));
     }
     s = row_sum<TPR>(s, fslots, turn);     // (its barrier is the candidates' too)
+    s *= pow2(-__builtin_fmaf(base0, eT, -shift));
     row_sync<LW>();
     const int n = space.count;
     u64* keys = MODE == WHOLE ? nullptr : (u64*)p.ws + (r * p.pieces + piece) * p.k;
