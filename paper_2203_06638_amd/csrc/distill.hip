@@ -96,8 +96,14 @@ constexpr int distill_waves(int values, bool both, int tpr) {
 // works on: its teacher's side while the row is on its way, its student's side between
 // the sums and the gradient.  The exponentials stay in registers from the sums to the
 // gradient.
+// 4096 x 20000 bf16, 32 listed (328 MB, 64 us at a large copy's rate): 87 us with T = 1, 88.7 with
+// T = 2, 89.9 with T = 4, 113 with T = 3, where both exponentials of a value are kept (eight waves to a
+// row).  A compute unit holds three rows, each of which loads, sums and writes in turn: half of the
+// time its vector units wait.
+// 1024 x 1000 float32 7.8 us, 128 x 10 6.2: the latency of a row's steps, not its bytes (1.6, 0.002).
 template <typename T, int TPR, int NC, int MODE, int EXPS, bool ST>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves<T>(NC * 16 / (int)sizeof(T), EXPS == TWO_EXPS, TPR)) void distill_k(DistillArgs p) {
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves<T>(NC * 16 / (int)sizeof(T), EXPS == TWO_EXPS, TPR)) void
+distill_k(DistillArgs p) {
     constexpr bool BOTH = EXPS != ONE_EXP;
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int TB = TPR > 256 ? TPR : 256, RB = TB / TPR;
@@ -509,6 +515,10 @@ constexpr int kFew = 256;
 // the bound (equal values, or values laid out against the threads) top_keys takes over, and
 // where the values under it add up to less than 1, so that the bound may lie far above them,
 // they are summed again relative to their largest.
+// 4096 x 20000 bf16, k = 32 (164 MB, 32 us at a large copy's rate): 51.5 us, of which the vector
+// instructions (about 17 a value, an exponential among them) are issued for 40; k = 128: 95.7, whose
+// candidates the first wave places.  128 x 1000 float32 6.6 us, and 8 x 131072 in pieces 13.2 + 7.5 for the
+// merge: latency of 4 to 8 dependent steps.
 template <typename T, int TPR, int NC, int MODE, int G>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves<T>(NC * 16 / (int)sizeof(T))) void top_logits_k(TopArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -672,7 +682,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves<T>(NC * 16 / (int)
 }
 
 // A row's answer from its pieces' lists, which are in descending order.  With j = 2 k / P
-// (P pieces) at least k keys reach the ceil(k / j)-th largest of the pieces' j-th keys.
+// (P pieces) at least k keys reach the ceil(k / j)-th largest of the pieces' j-th keys.  (8 rows of
+// 32 pieces, k = 64: 7.5 us, barriers.)
 constexpr int kMergeThreads = 1024, kMergeKeys = 4;
 __global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
     constexpr int TPR = kMergeThreads;
@@ -745,8 +756,8 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
 
 // Threads of a row and chunks of a thread.  Rows that the registers of 512 threads do not
 // hold are cut into pieces.  Where there are many rows, four waves to a row and more values a
-// thread: more rows of a compute unit at once, whose steps cover each other (distillation of
-// 4096 x 20000 bf16, T = 2: 76.6 us, 82.5 with eight waves; 1024 x 16000 float32: 37.8 and 30.4).
+// thread: more rows of a compute unit at once, whose steps cover each other (distillation of the same
+// 4096 x 20000 bf16 again and again, T = 2: 76.6 us, 82.5 with eight waves; 1024 x 16000 float32: 37.8 and 30.4).
 // wide: values that a thread may keep there.  Top logits: 48 (4096 x 10000 bf16 32.1 us, 37.5 with
 // eight; 16000: 42.3 and 40.7); distillation: 80, with two exponentials kept 48.
 struct RowPlan {

@@ -13,6 +13,11 @@
 // z is the same expression in both directions, so that a ReLU's gradient decides as the
 // forward pass did.  Statistics and sums are float32: means and sums of squared deviations of parts are
 // merged (never sums of squares of the values), everything in a fixed order.
+//
+// This file's kernels spread an image over the chip: partial sums, then a second pass over the
+// data, which takes part of it from the caches.  Maps that a workgroup's registers hold take
+// groupnorm_whole.hip, which reads them once.  Both do about 8 operations a value forward, 16
+// backward: bandwidth bounds them.
 #include <algorithm>
 
 #include "act8.h"
@@ -100,7 +105,9 @@ __device__ __forceinline__ void each_part(const GnShape& s, const float2* ws, lo
 
 // Mean and squared deviations of every part (a group's channels in a slab, a split of
 // the rows), into ws [image][split][part] as pairs; part = group + slab.  A thread sums
-// each of its channels about the first value that it reads.
+// each of its channels about the first value that it reads.  Four loads a thread are under way
+// at once (U); with gn_apply_k 16 x 3136 x 256 bf16 takes 26.8 us (16.1 at a large copy's rate if the
+// data were read once).
 template <typename T>
 __global__ __launch_bounds__(TB) void gn_stats_k(GnArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -202,7 +209,8 @@ __global__ __launch_bounds__(TB) void gn_stats_k(GnArgs p) {
     }
 }
 
-// Mean and rstd of the slab's groups from their parts, then y.
+// Mean and rstd of the slab's groups from their parts, then y.  Every workgroup merges its groups'
+// parts by itself (some KB from the L2): one launch less than a kernel in between.
 template <typename T, int ACT, bool ST>
 __global__ __launch_bounds__(TB) void gn_apply_k(GnArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -284,7 +292,8 @@ struct Channels {
 };
 
 // Sums over a split's rows of dz and dz * u: for every channel, into ws behind the
-// parts' [image][split][2][cp], and gamma times them for every part.
+// parts' [image][split][2][cp], and gamma times them for every part.  (32 x 784 x 250 float32: 13.2 us,
+// 50 MB at 3.8 TB/s.)
 template <typename T, int ACT>
 __global__ __launch_bounds__(TB) void gn_bwd_sums_k(GnBwdArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -370,7 +379,8 @@ __global__ __launch_bounds__(TB) void gn_bwd_sums_k(GnBwdArgs p) {
 }
 
 // dgamma and dbeta: kColumns columns of the channels' sums a workgroup, 32 threads to four
-// columns, over all images and splits
+// columns, over all images and splits.  No atomics, so that the order is fixed; a launch of its
+// own takes 3.9 us for 128 images of 128 channels: latency.
 constexpr int kColumns = TB / 32 * 4;
 __device__ void gn_columns(const GnBwdArgs& p, int block, float* sm) {
     const int t = threadIdx.x, q = t % (kColumns / 4), l = t / (kColumns / 4), col = block * kColumns + q * 4;
@@ -400,9 +410,12 @@ __global__ __launch_bounds__(TB) void gn_columns_k(GnBwdArgs p) {
     gn_columns(p, blockIdx.x, sm);
 }
 
-// dx; the first `extra` workgroups sum dgamma and dbeta beside it.
+// dx; the first `extra` workgroups sum dgamma and dbeta beside it.  Four waves a SIMD in float32: the 784
+// workgroups of 32 x 784 x 250 with a residual then run at once (18.8 us, 100 MB at 5.3 TB/s; 21.9 with
+// three); bf16's registers would spill.  With gn_bwd_sums_k 32 x 3136 x 256 bf16 takes 57 us
+// (30 at a large copy's rate if x and dy were read once).
 template <typename T, int ACT, bool ST>
-__global__ __launch_bounds__(TB) void gn_bwd_apply_k(GnBwdArgs p) {
+__global__ __launch_bounds__(TB, sizeof(T) == 4 ? 4 : 3) void gn_bwd_apply_k(GnBwdArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     __shared__ __attribute__((aligned(16))) float sm[2 * 64 * V > 1024 ? 2 * 64 * V : 1024];
     if ((int)blockIdx.x < p.extra) {
