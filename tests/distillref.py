@@ -38,14 +38,15 @@ def rest_bound(z, index, T):
     """An exponent carries two roundings of |z / T - max| log2 e and 2^x one unit in the
     last place; log adds one, and the largest value its own.  The largest value may be
     replaced by a bound above it, relative to which the sum is at least 1, so that it is at most
-    T log C higher: every exponent is that much longer."""
+    T log C higher: every exponent is that much longer.  The exponents are relative to a rounded
+    bound / T; what the rounding left out is one more power and product of the sum, 3 units."""
     taken = torch.zeros(z.shape, dtype=torch.bool).scatter_(1, index.long(), True)
     u = (z.double() / T).masked_fill(taken, -INF)
     m = u.amax(1, keepdim=True)
     p = torch.softmax(u, 1)
     spread = torch.where(p > 0, p * (m - u), 0.0).sum(1)
     r = torch.logsumexp(u, 1)
-    return (3 * spread + 3 * math.log(z.shape[1]) + path(z.shape[1]) + 6) * U + 4 * U * (m[:, 0].abs() + (r - m[:, 0]).abs())
+    return (3 * spread + 3 * math.log(z.shape[1]) + path(z.shape[1]) + 9) * U + 4 * U * (m[:, 0].abs() + (r - m[:, 0]).abs())
 
 
 def distill(z, values, index, rest=None, labels=None, weight=None, alpha=1.0, T=1.0, scale=1.0):

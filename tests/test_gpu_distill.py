@@ -94,6 +94,14 @@ def test_top(dtype, layout):
         check_top(logits(n, rows, C, dtype)[0], k, (1.0, 2.0, 3.5)[n % 3], layout)
 
 
+@pytest.mark.parametrize("T", [1e-30, 0.02, 300.0, 1e30])
+def test_top_temperatures(T):
+    """z / T far from 0, where its rounding is many times the distance of two logits."""
+    for n, (rows, C, k) in enumerate([(9, 100, 10), (3, 1000, 40), (2, 8192, 7), (1, 60000, 32)]):
+        say("top", T, rows, C, k)
+        check_top(logits(n, rows, C, "fp32")[0] + 5000.0, k, T)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("C", [10, 700, 1500, 9000, 20000])
 def test_top_orders(dtype, C):
