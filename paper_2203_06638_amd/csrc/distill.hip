@@ -73,8 +73,8 @@ enum RowExps { ONE_EXP, TWO_EXPS, SQUARE, FOURTH };
 // ---- distillation ------------------------------------------------------------
 
 // LDS of a row: the list (classes, teacher's values and then probabilities, student's
-// logits, whether a class is listed before; the label behind it), four results, and a bit for
-// each class of the piece that is listed
+// logits, whether a class is listed before; the label behind it), three results
+// and the largest listed logit, and a bit for each class of the piece that is listed
 __host__ __device__ inline int distill_lds(int k, int values) { return 4 * (k + 1) + 4 + (values + 31) / 32; }
 constexpr int kListPitch = kDistillMaxK + 4;   // floats of a row's list in the workspace
 
@@ -155,6 +155,7 @@ distill_k(DistillArgs p) {
     bool twice = false;               // a class is listed twice
     if (lead) {
         bool bad = rest != rest;      // (a maximum drops a NaN)
+        float lm = -INFINITY;         // the largest listed logit
         auto entry = [&](int e) {
             const int c = cls[e];
             // (dz may be z: the pieces' workgroups keep z at the listed classes for each other)
@@ -162,6 +163,7 @@ distill_k(DistillArgs p) {
             float v = 0.f;
             if (c >= 0) v = MODE == PIECE_GRAD ? kept[e] : ld1(z, c);
             zc[e] = v;
+            if (MODE != PIECE_SUMS && c >= 0 && e < k) lm = fmaxf(lm, v);
             if (MODE == PIECE_SUMS && c >= c0 && c < c1) kept[e] = v;
             // whether the class is listed before (all of a row's entries are one wave's, the label
             // comes last)
@@ -184,6 +186,10 @@ distill_k(DistillArgs p) {
         if (t == k % LW) entry(k);
         // the teacher's probabilities
         tm = row_max<LW>(tm, slots, none);
+        if (MODE != PIECE_SUMS) {
+            lm = row_max<LW>(lm, slots, none);
+            if (t == 0) out[3] = lm;  // (it waits there for the row's sums: registers)
+        }
         for (int e = t; e < k; e += LW) ts += cls[e] >= 0 && tm > -INFINITY ? pow2((pr[e] - tm) * kLog2e) : 0.f;
         ts = row_sum<LW>(bad ? NAN : ts, slots, none) + (rest > -INFINITY ? pow2((rest - tm) * kLog2e) : 0.f);
     }
@@ -206,8 +212,9 @@ distill_k(DistillArgs p) {
 #pragma unroll
             for (int j = 0; j < V; ++j) a[c][j] = (gone >> j) & 1u ? -INFINITY : a[c][j];
     }
-    // largest value, and the sums of exp(z - m) and exp((z - m) / T) over the classes that are
-    // not listed
+    // m: the largest of the classes that are not listed, and their sums of exp(z - m) and
+    // exp((z - m) / T).  Relative to the row's largest value they would vanish where a listed class lies far
+    // above them, and with them the rest's answer, which is a ratio of them.
     float m = -INFINITY, s1 = 0.f, so = 0.f;
     const f4* all = (const f4*)p.ws + r * p.pieces;
     if (MODE == PIECE_GRAD) {
@@ -218,11 +225,10 @@ distill_k(DistillArgs p) {
 #pragma unroll
             for (int j = 0; j < V; ++j) m = fmaxf(m, a[c][j]);
     }
-    if (MODE != PIECE_SUMS && lead)
-        for (int e = t; e <= k; e += LW) m = fmaxf(m, cls[e] >= 0 ? zc[e] : -INFINITY);
+    if (MODE != PIECE_SUMS && lead && t == k % LW && cls[k] >= 0 && !again[k]) m = fmaxf(m, zc[k]);
     m = row_max<TPR>(m, slots, turn);
-    // (a piece of nothing but -inf: sums of 0)
-    const float base = MODE == PIECE_SUMS && m == -INFINITY ? 0.f : m;
+    // (nothing but -inf: sums of 0)
+    const float base = m == -INFINITY ? 0.f : m;
     if (MODE != PIECE_GRAD || p.dz) {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -240,8 +246,8 @@ distill_k(DistillArgs p) {
     if (MODE == PIECE_GRAD)
         for (int e = t; e < p.pieces; e += TPR) {
             const f4 s = all[e];
-            if (BOTH) s1 += s[1] * pow2((s[0] - m) * e1);
-            so += s[2] * pow2((s[0] - m) * eT);
+            if (BOTH) s1 += s[1] * pow2((s[0] - base) * e1);
+            so += s[2] * pow2((s[0] - base) * eT);
         }
     if (BOTH) row_sum2<TPR>(s1, so, slots, turn);
     else so = row_sum<TPR>(so, slots, turn);
@@ -257,20 +263,22 @@ distill_k(DistillArgs p) {
     const bool live = w != 0.f && (g1 != 0.f || gT != 0.f);   // (a row without a loss has no gradient, whatever it holds)
     float sT = 0.f, kT = 0.f;
     if (lead) {
+        const float most = fmaxf(m, out[3]);     // of all classes
         // what the listed classes add: once each, the label's to the first sum (and to the
-        // other classes' of the second, if it is not listed)
+        // other classes' of the second, if it is not listed).  Sums over all classes are relative to most.
         float l1 = 0.f, lT = 0.f, ly = 0.f;
         for (int e = t; e <= k; e += LW) {
             if (cls[e] < 0 || again[e]) continue;
-            const float d = zc[e] - m, q = pow2(d * eT);
+            const float d = zc[e] - most;
             if (BOTH) l1 += pow2(d * e1);
-            if (e < k) lT += q;
-            else ly = q;
+            if (e < k) lT += pow2(d * eT);
+            else ly = pow2((zc[e] - base) * eT);
         }
         row_sum2<LW>(lT, ly, slots, none);
-        if (BOTH) s1 += row_sum<LW>(l1, slots, none);
+        const float away = m - most, far1 = pow2(away * e1), farT = pow2(away * eT);   // (NaN for a row of -inf)
+        if (BOTH) s1 = s1 * far1 + row_sum<LW>(l1, slots, none);
         so += ly;
-        sT = so + lT;
+        sT = so * farT + lT;
         if (!BOTH) s1 = sT;
         const float lt = logf(ts), lq = logf(sT);
         float soft = 0.f, sp = 0.f;
@@ -279,7 +287,7 @@ distill_k(DistillArgs p) {
                 pr[e] = 0.f;
                 continue;
             }
-            const float v = pr[e] - tm, pe = pow2(v * kLog2e) / ts, u = (zc[e] - m) * iT - lq, d = v - lt - u;
+            const float v = pr[e] - tm, pe = pow2(v * kLog2e) / ts, u = (zc[e] - most) * iT - lq, d = v - lt - u;
             pr[e] = pe;
             sp += pe;
             if (tail) {
@@ -294,11 +302,11 @@ distill_k(DistillArgs p) {
             }
         }
         row_sum2<LW>(soft, sp, slots, none);
-        float others = 1.f / sT;      // what gT times exp((z - m) / T) of a class that is not listed has
+        float others = farT / sT;     // what gT times exp((z - m) / T) of a class that is not listed has
         if (tail) {
-            const float q = so / sT, pe = some && rest > -INFINITY ? pow2((rest - tm) * kLog2e) / ts : 0.f;
+            const float q = so * farT / sT, pe = some && rest > -INFINITY ? pow2((rest - tm) * kLog2e) / ts : 0.f;
             if (some) {
-                const float d = (rest - tm) - lt - logf(q);
+                const float d = (rest - tm) - lt - (logf(so) + away * iT - lq);
                 if (pe > 0.f) soft += d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + q;
                 else soft += q;
             }
@@ -310,11 +318,11 @@ distill_k(DistillArgs p) {
         if (t == 0) {
             if (ok && piece == 0) {
                 float l = 0.f;
-                if (y >= 0 && use1) l += a1 * (logf(s1) - (zc[k] - m));
+                if (y >= 0 && use1) l += a1 * (logf(s1) - (zc[k] - most));
                 if (some) l += aT * temp * soft;
                 p.loss[r] = w != 0.f ? w * l : 0.f;
             }
-            out[0] = g1 != 0.f ? g1 / s1 : 0.f;
+            out[0] = g1 != 0.f ? g1 / s1 * far1 : 0.f;
             out[1] = kT;
             out[2] = live ? 1.f : 0.f;
         }
@@ -349,6 +357,7 @@ distill_k(DistillArgs p) {
 #pragma unroll
     for (int d = 1; d < LW; d *= 2) twice |= __shfl_xor((int)twice, d) != 0;
     if (!ok || !live) return;
+    const float most = fmaxf(m, out[3]);
     for (int e = t; e <= k; e += LW) {
         const int c = cls[e];
         if (c < c0 || c >= c1 || again[e]) continue;
@@ -357,9 +366,9 @@ distill_k(DistillArgs p) {
             pe = 0.f;
             for (int o = 0; o < k; ++o) pe += cls[o] == c ? pr[o] : 0.f;
         }
-        const float d = zc[e] - m, q = pow2(d * eT);
+        const float d = zc[e] - most;
         float g = g1 != 0.f ? g1 * (pow2(d * e1) / s1 - (c == y ? 1.f : 0.f)) : 0.f;
-        if (gT != 0.f) g += e < k || !tail ? gT * (q / sT - pe) : kT * q;
+        if (gT != 0.f) g += e < k || !tail ? gT * (pow2(d * eT) / sT - pe) : kT * pow2((zc[e] - base) * eT);
         st1(dz, c, g);
     }
 }

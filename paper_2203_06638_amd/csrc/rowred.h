@@ -78,11 +78,27 @@ __device__ __forceinline__ void row_sync() {
     }
 }
 
-// the largest of a value over the TPR threads of a row (a NaN only where all are)
+// the largest of v and its value on a lane that DPP control CTRL names
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+    return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true)));
+}
+
+// the largest of a value over the TPR threads of a row (a NaN only where all are), as row_sum
 template <int TPR>
 __device__ __forceinline__ float row_max(float v, float* slots, int& turn) {
-#pragma unroll
-    for (int d = 1; d < 64 && d < TPR; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+    v = dpp_max<0xB1>(v);
+    if constexpr (TPR > 2) v = dpp_max<0x4E>(v);
+    if constexpr (TPR > 4) v = dpp_max<0x141>(v);
+    if constexpr (TPR > 8) v = dpp_max<0x140>(v);
+    if constexpr (TPR > 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    if constexpr (TPR > 32) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         float* s = slots + turn * W;

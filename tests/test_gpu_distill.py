@@ -429,3 +429,42 @@ def test_past_two_to_31_elements():
     lpp.kernel_distill(z, values, index, loss, z, rest, ws=torch.empty(max(1, n), device="cuda"))
     # the student is the teacher: nothing to learn
     assert loss.abs().max() < 1e-6 and z[-1].float().abs().max() < 1e-5 and z[0].float().abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("C", [6, 100, 700, 3000, 20000, 70000])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_student_far_favourites(dtype, C):
+    """A listed class of the student so far above all others that their exponentials relative to it are 0
+    in float32: the rest's loss and the unlisted classes' gradients are those of the logits all the same.
+    Rows of one workgroup and rows in pieces; the label the favourite, another class or none.  (An
+    exponential relative to the favourite that is under 2^-126 may count as 0, with the gradient's
+    factors: of the hard term, and of the soft one where the list stands for all.)"""
+    rows, k, scale = 12, 3, 0.5
+    gap = torch.tensor([60.0, 86.0, 88.0, 89.5, 100.0, 103.0, 104.5, 110.0, 150.0, 300.0, 500.0, 650.0])
+    for n, (T, alpha, labelled) in enumerate([(1.0, 1.0, 0), (2.0, 0.6, 1), (4.0, 0.5, 1), (3.0, 0.7, 1), (1.0, 0.3, 1),
+                                              (10.0, 1.0, 0), (3.0, 0.0, 1)]):
+        for rest in (True, False):
+            say("far favourites", dtype, C, T, alpha, rest)
+            z, values, index, r, best = teacher(40 + n, rows, C, k, T, rest)
+            labels = best.clone()
+            labels[::4] = (index[::4, -1] + 1) % C
+            labels[1::4] = index[1::4, 0]
+            labels = labels if labelled else None
+            z = z.scatter(1, index[:, :1].long(), (z.amax(1) + gap * max(1.0, T)).unsqueeze(1)).to(DT[dtype])
+            loss, dz = run_distill(z, values, index, r, labels, alpha=alpha, temperature=T, scale=scale)
+            want, wdz, bl, bd = R.distill(z, values, index, r, labels, None, alpha, T, scale)
+            near(loss, want, bl + 1e-38, ("loss", T, alpha, rest))
+            flushed = 2.0 ** -126 * (2 + scale * (1 - alpha + alpha * T))
+            near(dz, wdz, bd + R.HALF[z.dtype] * (wdz.abs() + bd) + flushed, ("dz", T, alpha, rest))
+
+
+def test_student_far_favourite_by_hand():
+    """10 classes, one listed at 100 and the others at 0; the teacher gives the rest 31 of 100."""
+    z = torch.zeros(1, 10)
+    z[0, 4] = 100.0
+    values, index = torch.full((1, 1), math.log(0.69)), torch.full((1, 1), 4, dtype=torch.int32)
+    loss, dz = run_distill(z, values, index, torch.full((1,), math.log(0.31)))
+    # p log(p / q): q = 1 and 9 e^-100
+    want = 0.69 * math.log(0.69) + 0.31 * (math.log(0.31) - math.log(9) + 100)
+    assert abs(loss.item() - want) < 40 * R.U * want
+    assert abs(dz[0, 4].item() - 0.31) < 8 * R.U and (dz[0, :4] + 0.31 / 9).abs().max() < 8 * R.U / 9
