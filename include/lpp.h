@@ -194,7 +194,8 @@ int lpp_step(lpp_ctx* ctx, int worker, const lpp_batch* batch, int partition, fl
  * The same iteration with a teacher: the loss of image n is that of
  * lpp_kernel_distill for its logits, (1 - alpha) * cross-entropy of its label +
  * alpha * temperature^2 * distillation loss of the teacher's list, and lpp_get_loss
- * returns its mean over the batch.  The teacher's buffers (device) hold a list for
+ * returns its mean over the batch.  An image whose label is outside [0, n_classes) has the
+ * teacher's part alone.  The teacher's buffers (device) hold a list for
  * every image of the batch, as lpp_top_logits or lpp_kernel_top_logits leaves
  * it, and must stay valid as long as the batch's.  1 <= k <= 128 (LPP_EUNSUPPORTED for
  * more), 0 <= alpha <= 1, temperature > 0 and finite.

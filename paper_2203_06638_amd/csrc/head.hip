@@ -61,7 +61,8 @@ __device__ void softmax_ce_row(const float* z_s, int O, int y, int Nb, float* re
 // ---- fused form --------------------------------------------------------
 
 // One workgroup per sample: pooled features f (also written out for the
-// weight gradient where feat is not null), logits W f + b, softmax cross-entropy.  Pooling: thread
+// weight gradient where feat is not null), logits W f + b, softmax cross-entropy (dz
+// null: none, and the labels are not read).  Pooling: thread
 // (q, l) sums channel quad q over pixels l, l + rl, ...; the rl partial sums
 // of a quad are added in LDS in a fixed order.  C % 4 == 0.
 template <class T>
@@ -116,6 +117,7 @@ __global__ __launch_bounds__(256) void head_fwd_k(const T* __restrict__ x, int N
             logits[(long)n * O + o] = z;
         }
     }
+    if (!dz) return;
     __syncthreads();
     softmax_ce_row(z_s, O, args->labels[n], Nb, red, dz + (long)n * O, loss_per + n);
 }
@@ -379,7 +381,7 @@ hipError_t launch_head_fwd(int dt, const void* x, int Nb, int HW, int C, const f
         if (e != hipSuccess) return e;
         const dim3 grid(nblk(O, 16), nblk(Nb, 16 * kTiles));
         launch(head_logits_k, grid, dim3(64 * kWaves), 0, st, W, b, (const float*)feat, logits, Nb, C, O);
-        launch(head_softmax_k, dim3(Nb), dim3(256), 0, st, (const float*)logits, Nb, O, args, dz, loss_per);
+        if (dz) launch(head_softmax_k, dim3(Nb), dim3(256), 0, st, (const float*)logits, Nb, O, args, dz, loss_per);
         return hipGetLastError();
     }
     if (C > kHeadMaxC) return hipErrorInvalidValue;

@@ -273,6 +273,7 @@ hipError_t launch_bn_bwd_apply(int dt, const BnBwdArgs& a, const BnBwdCoef& k, v
 // product + softmax; narrow ones as one fused kernel per sample.
 constexpr long kHeadWideMin = 16384;
 bool head_wide(int C, int O);
+// dz null: the logits alone, no label is read
 hipError_t launch_head_fwd(int dt, const void* x, int Nb, int HW, int C, const float* W, const float* b, int O,
                            const StepArgs* args, float* feat, float* logits, float* dz, float* loss_per,
                            hipStream_t st);

@@ -1304,7 +1304,7 @@ int run_forward(lpp_ctx* c, Worker& w, int partition, bool distill) {
             LAUNCH("head", eb * Mrows * Y.in0.c + 2.0 * L.macs, st,
                    lpp::launch_head_fwd(dt, x0, N, Y.in0.h * Y.in0.w, Y.in0.c, W, L.L.bias ? W + L.wcount : nullptr,
                                         L.L.cout, w.args, (float*)c->act(w, G.a), (float*)c->act(w, G.lin),
-                                        (float*)c->dact(w, G.lin), w.loss + 1, st));
+                                        distill ? nullptr : (float*)c->dact(w, G.lin), w.loss + 1, st));
             loss_done = true;
             break;
         }
@@ -1322,7 +1322,7 @@ int run_forward(lpp_ctx* c, Worker& w, int partition, bool distill) {
     }
     const int last = (int)M.layers.size() - 1;
     if (distill) {
-        // (in place of the head's own loss and gradient)
+        // (in place of the head's own loss and gradient, which take every label to be a class)
         lpp::DistillArgs a{};
         a.z = c->act(w, last);
         a.dz = c->dact(w, last);

@@ -348,3 +348,31 @@ def test_student_learns_the_teacher_asynchronously():
         ctx.sync()
         assert all(math.isfinite(ctx.get_loss(w)) for w in range(4))
         assert np.isfinite(ctx.get_params(0)).all() and ctx.counter(0) == 20
+
+
+def heads(how):
+    """Models whose logits one kernel forms with the loss, a matrix product, a linear layer of its own or
+    a pool."""
+    if how in ("narrow", "unfused"):
+        return resnet(act=False)
+    m = PM.Model(how, (3, 8, 8), 1200 if how == "wide" else 12)
+    t = m.groupnorm(m.conv(-1, 16, 3), 4)
+    if how == "wide":
+        m.linear(m.gap(m.conv(t, 128, 3)), 1200)
+    else:
+        m.gap(m.conv(t, 12, 1, 1, 0, bias=True))
+    return m.assign_blocks([1])
+
+
+@pytest.mark.parametrize("how", ["narrow", "wide", "pool", "unfused"])
+def test_step_distill_images_without_a_label(how):
+    """Labels that are no class: those images have the teacher's part alone."""
+    m = heads(how)
+    img, lab, x, tensors = inputs(m, 8, 23)
+    lab = lab.astype(np.int32)
+    lab[[0, 2, 3, 5, 6]] = [-1, m.n_classes, -100, 2 ** 31 - 1, -2 ** 31]
+    for alpha in (0.6, 1.0, 0.0):
+        say("no label", how, alpha)
+        t = (*lists(8, m.n_classes, 4, 2.0, 5), alpha, 2.0)
+        got = step(m, img, lab, x, teacher=t, steps=2, unfused=how == "unfused")
+        check(m, got, reference(m, img, lab, x, t), tensors, 0, len(x), how)
