@@ -131,7 +131,8 @@ typedef struct {
 
 typedef struct {
     const float* images; /* device, NCHW float32 [batch][in_c][in_h][in_w]       */
-    const int* labels;   /* device, int32 [batch], 0 <= y < n_classes            */
+    const int* labels;   /* device, int32 [batch], 0 <= y < n_classes (with a
+                            teacher see lpp_step_distill)                        */
     int n;               /* must equal the model's batch                         */
 } lpp_batch;
 
@@ -195,7 +196,7 @@ int lpp_step(lpp_ctx* ctx, int worker, const lpp_batch* batch, int partition, fl
  * lpp_kernel_distill for its logits, (1 - alpha) * cross-entropy of its label +
  * alpha * temperature^2 * distillation loss of the teacher's list, and lpp_get_loss
  * returns its mean over the batch.  An image whose label is outside [0, n_classes) has the
- * teacher's part alone.  The teacher's buffers (device) hold a list for
+ * teacher's part alone, and so have all where the batch's labels are NULL.  The teacher's buffers (device) hold a list for
  * every image of the batch, as lpp_top_logits or lpp_kernel_top_logits leaves
  * it, and must stay valid as long as the batch's.  1 <= k <= 128 (LPP_EUNSUPPORTED for
  * more), 0 <= alpha <= 1, temperature > 0 and finite.

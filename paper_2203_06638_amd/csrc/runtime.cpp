@@ -2044,7 +2044,7 @@ int lpp_destroy(lpp_ctx* c) {
 static int step(lpp_ctx* c, int worker, const lpp_batch* batch, const lpp_teacher* teacher, int partition, float lr) {
     int rc = check_worker(c, worker);
     if (rc) return rc;
-    if (!batch || !batch->images || !batch->labels) return fail(LPP_EINVAL, "batch or its buffers are NULL");
+    if (!batch || !batch->images || (!batch->labels && !teacher)) return fail(LPP_EINVAL, "batch or its buffers are NULL");
     if (batch->n != c->M.desc.batch) return fail(LPP_EINVAL, "batch->n must equal the model's batch");
     if (partition < 0 || partition > c->P) return fail(LPP_EINVAL, "partition must be in [0, P]");
     if (!std::isfinite(lr)) return fail(LPP_EINVAL, "lr must be finite");

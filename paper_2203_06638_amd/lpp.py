@@ -254,11 +254,13 @@ class Context:
 
     def step_distill(self, worker, images, labels, values, index, partition, lr, rest=None, alpha=0.9, temperature=1.0):
         """A step whose loss is alpha parts distillation from a teacher's list (values,
-        index [batch][k], rest [batch]: device tensors, see top_logits)."""
+        index [batch][k], rest [batch]: device tensors, see top_logits); labels None: from the
+        list alone."""
         dev = _current_device(images)
         vp, ip, k = _list(values, index, self.batch, dev)
         rp = _floats(rest, self.batch, "rest", dev) if rest is not None else None
-        b = Batch(images.data_ptr(), labels.data_ptr(), images.shape[0])
+        lp = None if labels is None else _ints(labels, self.batch, "labels", dev)
+        b = Batch(images.data_ptr(), lp, images.shape[0])
         t = Teacher(vp, ip, rp, k, alpha, temperature)
         _check(lib().lpp_step_distill(self._ctx, worker, C.byref(b), C.byref(t), partition, lr))
 

@@ -376,3 +376,55 @@ def test_step_distill_images_without_a_label(how):
         t = (*lists(8, m.n_classes, 4, 2.0, 5), alpha, 2.0)
         got = step(m, img, lab, x, teacher=t, steps=2, unfused=how == "unfused")
         check(m, got, reference(m, img, lab, x, t), tensors, 0, len(x), how)
+
+
+@pytest.mark.parametrize("how", ["narrow", "wide", "pool"])
+def test_step_distill_without_labels(how):
+    """A batch without labels steps as one whose labels are no classes; replayed in turn with labelled
+    ones.  A step without a teacher needs them."""
+    m = heads(how)
+    img, lab, x, _ = inputs(m, 6, 24)
+    im, lb = torch.from_numpy(img).cuda(), torch.from_numpy(lab).cuda()
+    none = torch.full_like(lb, -1)
+    v, i, r = (t.cuda() for t in lists(6, m.n_classes, 4, 2.0, 6))
+    with lpp.Context(m, K=1, batch=6) as ctx:
+        got = {}
+        for labels in (lb, None, none, lb, None):
+            ctx.set_params(x)
+            ctx.step_distill(0, im, labels, v, i, 0, 0.1, r, 0.6, 2.0)
+            now = ctx.get_loss(0), ctx.get_grad(0)
+            key = "with" if labels is lb else "without"
+            before = got.setdefault(key, now)
+            assert now[0] == before[0] and np.array_equal(now[1], before[1])
+        assert got["with"][0] != got["without"][0]
+        for bad in (lb.long(), lb[:5], lb.cpu()):
+            with pytest.raises(lpp.LppError) as e:
+                ctx.step_distill(0, im, bad, v, i, 0, 0.1, r, 0.6, 2.0)
+            assert e.value.code == lpp.EINVAL
+        with pytest.raises(lpp.LppError) as e:
+            lpp._check(lpp.lib().lpp_step(ctx._ctx, 0, lpp.C.byref(lpp.Batch(im.data_ptr(), None, 6)), 0, 0.1))
+        assert e.value.code == lpp.EINVAL
+    want = reference(m, img, np.full(6, -1, np.int32), x, (v.cpu(), i.cpu(), r.cpu(), 0.6, 2.0))
+    assert abs(got["without"][0] - want[0]) <= 1e-5 * abs(want[0])
+
+
+@pytest.mark.parametrize("how", ["bf16", "act8"])
+def test_step_distill_in_fewer_bits(how):
+    """bf16 activations, and 8-bit checkpoints, whose forward pass and loss are the full step's."""
+    m = resnet(act=how == "act8")
+    img, lab, x, tensors = inputs(m, 8, 25, how == "bf16")
+    t = (*lists(8, 10, 4, 2.0, 7), 0.7, 2.0)
+    loss, z, g = reference(m, img, lab, x, t)
+    if how == "bf16":
+        got = step(m, img, lab, x, dtype=lpp.BF16, teacher=t, steps=2, plain_first=True)
+        assert PR.relerr(got[1], z, PR.TAU_BF16) <= PR.TOL_BF16
+        for kind, lo, n in tensors:
+            assert PR.relerr(got[2][lo:lo + n], g[lo:lo + n], PR.TAU_BF16) <= PR.TOL_BF16, (kind, lo)
+        # the loss and its gradient at the logits that the step had
+        want = D.distill(torch.from_numpy(got[1]), t[0], t[1], t[2], torch.from_numpy(lab.astype(np.int32)), None, 0.7, 2.0)
+        bound = want[2].mean().item() + 16 * D.U * want[0].abs().mean().item()
+        assert abs(got[0] - want[0].mean().item()) <= bound
+    else:
+        got, full = step(m, img, lab, x, act8=True, teacher=t, steps=2), step(m, img, lab, x, teacher=t)
+        assert got[0] == full[0] and np.array_equal(got[1], full[1])
+        assert np.linalg.norm(got[2] - g) <= 0.05 * np.linalg.norm(g)
