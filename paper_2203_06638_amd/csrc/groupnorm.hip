@@ -78,6 +78,20 @@ __device__ __forceinline__ int first_slab(const GnShape& s, int g) { return g * 
 template <int V>
 __device__ __forceinline__ int last_slab(const GnShape& s, int g) { return ((g + 1) * s.cg - 1) / (V << s.lw); }
 
+// f(q, l, ll) for the groups of a workgroup's slab, 2^ll lanes to each, l the thread's.  A group that lies
+// in other slabs too has a whole wave in each of them, so that its parts are merged in one order
+// everywhere: it has one mean and one rstd, the stored ones.  (The slab's other groups share all
+// threads.)
+template <int V, class F>
+__device__ __forceinline__ void each_group(const GnShape& s, const Place<V>& at, F f) {
+    const int t = threadIdx.x, wave = t >> 6;
+    const bool before = at.c0 != at.g0 * s.cg, behind = at.c1 != (at.g0 + at.np) * s.cg;
+    const int ll = item_lanes(TB, at.np), first = before, last = at.np - behind;
+    for (int q = first + (t >> ll); q < last; q += TB >> ll) f(q, t & ((1 << ll) - 1), ll);
+    const int q = wave == 0 ? 0 : at.np - 1;
+    if ((wave == 0 && before) || (wave == 1 && behind && !(before && at.np == 1))) f(q, t & 63, 6);
+}
+
 // f(split, slab, part) for every 2^ll-th of a group's parts, l the first: slabs sa .. sa + ns - 1 of
 // every split.  Four loads are under way at once.
 template <class F>
@@ -216,9 +230,7 @@ __global__ __launch_bounds__(TB) void gn_apply_k(GnArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
     __shared__ float smean[64 * V], srstd[64 * V];
     const Place<V> at(p.s, blockIdx.x);
-    const int t = threadIdx.x;
-    const int ll = item_lanes(TB, at.np), l = t & ((1 << ll) - 1);
-    for (int q = t >> ll; q < at.np; q += TB >> ll) {
+    each_group(p.s, at, [&](int q, int l, int ll) {
         const int g = at.g0 + q, sa = first_slab<V>(p.s, g), ns = last_slab<V>(p.s, g) - sa + 1;
         Moments a{0.f, 0.f, 0.f};
         each_part(p.s, (const float2*)p.ws, at.image, g, sa, ns, l, ll, [&](int split, int slab, float2 m) {
@@ -239,7 +251,7 @@ __global__ __launch_bounds__(TB) void gn_apply_k(GnArgs p) {
                 if (p.rstd) p.rstd[at.image * p.s.G + g] = rstd;
             }
         }
-    }
+    });
     __syncthreads();
     float mu[V], rs[V], ga[V], be[V];
 #pragma unroll
@@ -424,10 +436,8 @@ __global__ __launch_bounds__(TB, sizeof(T) == 4 ? 4 : 3) void gn_bwd_apply_k(GnB
     }
     const Place<V> at(p.s, blockIdx.x - p.extra);
     float *s1 = sm, *s2 = sm + 64 * V;
-    const int t = threadIdx.x;
-    const int ll = item_lanes(TB, at.np), l = t & ((1 << ll) - 1);
     const float size = (float)p.s.pixels * (float)p.s.cg;
-    for (int q = t >> ll; q < at.np; q += TB >> ll) {
+    each_group(p.s, at, [&](int q, int l, int ll) {
         const int g = at.g0 + q, sa = first_slab<V>(p.s, g), ns = last_slab<V>(p.s, g) - sa + 1;
         float a = 0.f, b = 0.f;
         each_part(p.s, (const float2*)p.ws, at.image, g, sa, ns, l, ll, [&](int, int, float2 m) {
@@ -442,7 +452,7 @@ __global__ __launch_bounds__(TB, sizeof(T) == 4 ? 4 : 3) void gn_bwd_apply_k(GnB
             s1[q] = a / size;
             s2[q] = b / size;
         }
-    }
+    });
     Channels<V> k;
     k.load(p, at);
     __syncthreads();

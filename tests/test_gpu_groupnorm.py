@@ -378,3 +378,32 @@ def test_past_two_to_31_elements():
     ref = r * (dz * 1.5 - s1 - u * s2)
     assert ((y[last].float() - ref).abs() <= 2.0 ** -8 * ref.abs() + 0.02).all()
     assert torch.isfinite(dg).all() and torch.isfinite(db).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_groups_across_slabs(dtype):
+    """A group that lies in two workgroups' channels has one mean and one rstd: equal values with equal
+    gamma and beta give equal outputs on both sides, those of the stored statistics, and the
+    gradient's ReLU decides as the forward pass did.  (Slabs end at channel 256 and 512.)"""
+    C, G, edge = (320, 32, 256) if dtype == "fp32" else (640, 32, 512)
+    for n, p in ((1, 2300), (3, 3000), (2, 5001)):
+        say("across slabs", dtype, n, p)
+        x, gamma, beta, _, _ = make(n, n, p, C, dtype)
+        beta = -0.25 * gamma
+        a, b = edge - 2, edge + 1
+        assert a // (C // G) == b // (C // G)
+        x[:, b], gamma[b], beta[b] = x[:, a], gamma[a], beta[a]
+        for act in ("none", "relu"):
+            y, mean, rstd = run_forward(x, n, G, gamma, beta, act)
+            assert torch.equal(y[:, a], y[:, b])
+        db = torch.empty(C, device="cuda")
+        ws = torch.empty(lpp.groupnorm_bwd_ws(n, p, C, G), device="cuda")
+        for c in range(a - 8, edge + 8):
+            dy = torch.zeros_like(x, device="cuda")
+            dy[:, c] = 1
+            dx = torch.empty_like(dy)
+            lpp.kernel_groupnorm_bwd(dy, x.cuda(), n, G, gamma.cuda(), beta.cuda(), mean, rstd, dx, dbeta=db, ws=ws,
+                                     act=ACT["relu"])
+            assert db[c] == (y[:, c] > 0).sum() and int((db != 0).sum()) <= 1
+            if c != a and c != b:       # (no gradient of its own: what the group's means take from both is the same)
+                assert torch.equal(dx[:, a], dx[:, b])
