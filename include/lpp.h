@@ -499,7 +499,7 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* args, void* stream);
  *     rstd = 1 / sqrt(var + eps),  u = (x - mean) * rstd,
  *     z = u * gamma + beta,  y = act(z),
  * act: enum lpp_act.  A ReLU lets z > 0 through (a NaN becomes 0, as in LPP_RELU); SiLU is
- * z / (1 + e^-z).  y may be x.  mean and rstd (float32 [images][groups]) may be NULL.
+ * z / (1 + e^-z) (inf for inf, NaN for -inf; act' is 1 and 0 there).  y may be x.  mean and rstd (float32 [images][groups]) may be NULL.
  * The gradient, with dz = dy * act'(z), z from x, mean and rstd as above:
  *     dbeta = sum of dz, dgamma = sum of dz * u over images and pixels,
  *     dx = rstd * (dz * gamma - (s1 + u * s2)) (+ dres),

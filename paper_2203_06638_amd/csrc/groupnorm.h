@@ -11,7 +11,7 @@ namespace lpp {
 
 // 1 / (1 + e^-z): e^-z = 2^t (1 + r ln 2) with t = -z log2 e rounded and r what that lost,
 // so that large |z| cost no accuracy; the reciprocal is the unit's, off by one unit in the
-// last place.
+// last place.  |z| under 2^126: beyond, t would be infinite and r NaN.
 __device__ __forceinline__ float sigmoid(float z) {
     const float t = z * -1.44269504f, r = __builtin_fmaf(z, -1.44269504f, -t) + z * -1.9259630e-8f;
     const float e = __builtin_amdgcn_exp2f(t);
@@ -20,7 +20,8 @@ __device__ __forceinline__ float sigmoid(float z) {
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
     if (ACT == ACT_RELU) return fmaxf(z, 0.f);      // (0 for NaN)
-    if (ACT == ACT_SILU) return z * sigmoid(z);
+    // (from 128 on the sigmoid is 1, from -128 on 0; a NaN stays one through the other factor)
+    if (ACT == ACT_SILU) return z * sigmoid(__builtin_amdgcn_fmed3f(z, -128.f, 128.f));
     return z;
 }
 // dy * act'(z)
@@ -28,6 +29,8 @@ template <int ACT>
 __device__ __forceinline__ float act_grad(float dy, float z) {
     if (ACT == ACT_RELU) return z > 0.f ? dy : 0.f;
     if (ACT == ACT_SILU) {
+        // (the same for the derivative, 1 and 0 there; a NaN stays one)
+        z = __builtin_elementwise_maximum(__builtin_elementwise_minimum(z, 128.f), -128.f);
         const float s = sigmoid(z);
         return dy * (s * (1.f + z * (1.f - s)));
     }

@@ -407,3 +407,38 @@ def test_groups_across_slabs(dtype):
             assert db[c] == (y[:, c] > 0).sum() and int((db != 0).sum()) <= 1
             if c != a and c != b:       # (no gradient of its own: what the group's means take from both is the same)
                 assert torch.equal(dx[:, a], dx[:, b])
+
+
+@pytest.mark.parametrize("pixels", [40, 4000])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_silu_of_large_values(dtype, pixels):
+    """z / (1 + e^-z) and its derivative where e^-z, or z log2 e, is past float32: SiLU of an infinity is
+    itself, of a very negative number -0, and the derivative 1 and 0.  Both kernels."""
+    n, C, G = 2, 32, 4
+    x, gamma, beta, dy, _ = make(4, n, pixels, C, dtype)
+    big = torch.tensor([87.0, 89.0, 104.0, 1e4, 1e30, 2.3e38, 2.5e38, 3e38, math.inf])
+    high, low = slice(2, 2 + len(big)), slice(16, 16 + len(big))
+    beta[high], beta[low] = big, -big
+    y, mean, rstd = run_forward(x, n, G, gamma, beta, "silu")
+    y = y.float().cpu()
+    want, _, _ = R.forward(x, n, G, gamma, beta, EPS, "silu")
+    # (at 87 and more SiLU is its argument to 2^-120, whose own roundings the bounds have)
+    by = R.forward_bounds(x, n, G, gamma, beta, EPS, "silu")[0]
+    finite = torch.isfinite(want)
+    finite[:, low] = False
+    near(torch.where(finite, y, 0.0), torch.where(finite, want, 0.0), by.nan_to_num(0.0, 0.0), "y")
+    assert (y[:, 2 + len(big) - 1] == math.inf).all()
+    # (z is within 7 of beta; |z e^z| < 1e-32 from -80 on)
+    assert (y[:, 16:16 + len(big) - 1].abs() < 1e-30).all()
+    # -inf / (1 + inf)
+    assert torch.isnan(y[:, 16 + len(big) - 1]).all()
+    dx = torch.empty_like(x, device="cuda")
+    dg, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    ws = torch.empty(max(1, lpp.groupnorm_bwd_ws(n, pixels, C, G)), device="cuda")
+    lpp.kernel_groupnorm_bwd(dy.cuda(), x.cuda(), n, G, gamma.cuda(), beta.cuda(), mean, rstd, dx, dg, db, ws, act=ACT["silu"])
+    assert torch.isfinite(dx).all() and torch.isfinite(dg).all()
+    sums = dy.double().sum(0)
+    # (float32 sums of 2 * pixels values)
+    bound = (R.backward_bounds(dy, x, n, G, gamma, torch.zeros(C), mean.cpu(), rstd.cpu(), "none")[2])
+    near(db[high], sums[high], bound[high], "dbeta")
+    assert (db[low].abs() < 1e-30).all()
