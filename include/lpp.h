@@ -499,7 +499,8 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* args, void* stream);
  *     rstd = 1 / sqrt(var + eps),  u = (x - mean) * rstd,
  *     z = u * gamma + beta,  y = act(z),
  * act: enum lpp_act.  A ReLU lets z > 0 through (a NaN becomes 0, as in LPP_RELU); SiLU is
- * z / (1 + e^-z) (inf for inf, NaN for -inf; act' is 1 and 0 there).  y may be x.  mean and rstd (float32 [images][groups]) may be NULL.
+ * z / (1 + e^-z) (inf for inf, NaN for -inf; act' is 1 and 0 there).  y may be x.  mean
+ * and rstd (float32 [images][groups]) may be NULL.
  * The gradient, with dz = dy * act'(z), z from x, mean and rstd as above:
  *     dbeta = sum of dz, dgamma = sum of dz * u over images and pixels,
  *     dx = rstd * (dz * gamma - (s1 + u * s2)) (+ dres),
@@ -507,8 +508,8 @@ int lpp_kernel_rmsnorm_bwd(const lpp_rmsnorm_bwd_args* args, void* stream);
  * dx (storage type; it may be dy, dres or x), dgamma and dbeta (float32 [channels],
  * written) may be NULL, one at least is wanted.  dres may be NULL.
  * Statistics and sums are float32, merged in a fixed order.  A group whose squared
- * deviations add up to more than float32 holds has rstd = 0; one that holds an infinity or
- * NaN has a NaN mean.  images == 0 is valid (dgamma and dbeta become 0); pixels >= 1.
+ * deviations add up to more than float32 holds has rstd = 0 (and its mean, where all values
+ * are under 2^127); one that holds an infinity or NaN has a NaN mean.  images == 0 is valid (dgamma and dbeta become 0); pixels >= 1.
  * ws: lpp_groupnorm_ws / lpp_groupnorm_bwd_ws floats of device memory (16-byte aligned, may
  * be NULL where that is 0), scratch of this call until it has run: calls that may
  * overlap need their own.  -1 for sizes that the calls refuse, LPP_EUNSUPPORTED for more

@@ -37,6 +37,12 @@ __device__ __forceinline__ float act_grad(float dy, float z) {
     return dy;
 }
 
+// 2^-e with 2^(e - 1) <= n < 2^e: sums of n values are taken of the values times it, an exact
+// factor, so that they are as small as the values
+__device__ __forceinline__ float sum_scale(float n) {
+    return __uint_as_float((253u << 23) - (__float_as_uint(n) & 0x7f800000u));
+}
+
 // lanes (a power of two, one wave at most) that a workgroup has for each of n items
 __device__ __forceinline__ int item_lanes(int threads, int n) {
     int l = 6;

@@ -134,13 +134,16 @@ __global__ __launch_bounds__(TB) void gn_stats_k(GnArgs p) {
     chunk_values<T>(ld_chunk(x + lead * p.ldx, at.n, lead >= p.exact), k);
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = ss[j] = 0.f;
+    const long mine = at.r1 - at.r0 - at.rl;
+    float cnt = mine > 0 ? (float)((mine - 1) / at.RL + 1) : 0.f;
+    const float scale = sum_scale(cnt);
     auto add = [&](u4 w) {
         float v[V];
         chunk_values<T>(w, v);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float d = v[j] - k[j];
-            s[j] += d;
+            s[j] = __builtin_fmaf(d, scale, s[j]);
             ss[j] = __builtin_fmaf(d, d, ss[j]);
         }
     };
@@ -154,11 +157,9 @@ __global__ __launch_bounds__(TB) void gn_stats_k(GnArgs p) {
         for (int u = 0; u < U; ++u) add(w[u]);
     }
     for (; r < at.r1; r += at.RL) add(ld_chunk(x + r * p.ldx, at.n, r >= p.exact));
-    const long mine = at.r1 - at.r0 - at.rl;
-    float cnt = mine > 0 ? (float)((mine - 1) / at.RL + 1) : 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const float e = cnt > 0.f ? s[j] / cnt : 0.f;
+        const float e = cnt > 0.f ? s[j] / (cnt * scale) : 0.f;
         s[j] = cnt > 0.f ? k[j] + e : 0.f;
         // (an infinite sum stays one; rounding leaves nothing below 0)
         const float m2 = ss[j] == INFINITY ? ss[j] : ss[j] - e * (e * cnt);

@@ -190,7 +190,7 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
     }
     int q[V];
     if (S == V) slab_groups<V>(at.w, s.cg, at.np, q);
-    const float size = (float)s.pixels * (float)s.cg;
+    const float size = (float)s.pixels * (float)s.cg, scale = sum_scale(size), scaled = size * scale;
     float v[2][S];
 #pragma unroll
     for (int j = 0; j < S; ++j) v[0][j] = 0.f;
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
         chunk_values<T>(w[c], f);
         if (c * at.RL + at.rl < s.pixels)
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[0][j / Q] += f[j];
+            for (int j = 0; j < V; ++j) v[0][j / Q] = __builtin_fmaf(f[j], scale, v[0][j / Q]);
     }
     if (S == V)
 #pragma unroll
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
     float mu[S];
 #pragma unroll
     for (int j = 0; j < S; ++j) {
-        mu[j] = v[0][j] / size;
+        mu[j] = v[0][j] / scaled;
         v[0][j] = v[1][j] = 0.f;
     }
 #pragma unroll
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float d = f[j] - mu[j / Q];
-                v[0][j / Q] += d;
+                v[0][j / Q] = __builtin_fmaf(d, scale, v[0][j / Q]);
                 v[1][j / Q] = __builtin_fmaf(d, d, v[1][j / Q]);
             }
     }
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
     float rs[S];
 #pragma unroll
     for (int j = 0; j < S; ++j) {
-        const float e = v[0][j] / size;
+        const float e = v[0][j] / scaled;
         const float var = v[1][j] == INFINITY ? v[1][j] : v[1][j] / size - e * e;
         rs[j] = 1.f / sqrtf((var < 0.f ? 0.f : var) + p.eps);
         mu[j] += e;

@@ -442,3 +442,20 @@ def test_silu_of_large_values(dtype, pixels):
     bound = (R.backward_bounds(dy, x, n, G, gamma, torch.zeros(C), mean.cpu(), rstd.cpu(), "none")[2])
     near(db[high], sums[high], bound[high], "dbeta")
     assert (db[low].abs() < 1e-30).all()
+
+
+@pytest.mark.parametrize("pixels", [600, 6000])
+def test_values_past_float32_sums(pixels):
+    """Values whose sum, and whose squared deviations, float32 does not hold: the mean is theirs and
+    rstd 0.  Both kernels."""
+    n, C, G = 2, 8, 2
+    for size in (1e34, 3e36, 1.5e38):
+        x, gamma, beta, _, _ = make(6, n, pixels, C, "fp32")
+        x[:, :4] = size * (1 - 0.5 * torch.rand(n * pixels, 4, generator=torch.Generator().manual_seed(1)))
+        x[pixels:, :4] *= torch.where(torch.arange(pixels) % 3 == 0, -1.0, 1.0).unsqueeze(1)
+        y, mean, rstd = run_forward(x, n, G, gamma, beta, "none")
+        want, bound = R.forward(x, n, G, gamma, beta, EPS, "none"), R.forward_bounds(x, n, G, gamma, beta, EPS, "none")
+        near(mean, want[1], bound[1], ("mean", size))
+        assert (rstd[:, 0] == 0).all() and (rstd[:, 1] > 0).all()
+        assert torch.equal(y.cpu()[:, :4], beta[:4].expand(n * pixels, 4))
+        assert torch.isfinite(y).all()
