@@ -199,7 +199,7 @@ int lpp_step(lpp_ctx* ctx, int worker, const lpp_batch* batch, int partition, fl
  * teacher's part alone, and so have all where the batch's labels are NULL.  The teacher's buffers (device) hold a list for
  * every image of the batch, as lpp_top_logits or lpp_kernel_top_logits leaves
  * it, and must stay valid as long as the batch's.  1 <= k <= 128 (LPP_EUNSUPPORTED for
- * more), 0 <= alpha <= 1, temperature > 0 and finite.
+ * more), 0 <= alpha <= 1, 2^-60 <= temperature <= 2^60.
  */
 typedef struct {
     const float* values;     /* float32 [batch][k]                                 */
@@ -566,7 +566,7 @@ int lpp_kernel_groupnorm_bwd(const lpp_groupnorm_bwd_args* args, void* stream);
  *     rest = log of the sum of exp(z / temperature) over all other classes
  * (-inf where none has a value above -inf).  1 <= k <= min(classes, 128)
  * (LPP_EUNSUPPORTED for more than 128, and for more than 2^32 threads in a launch, up to 1024 a
- * row); temperature > 0 and finite.  ws: lpp_top_logits_ws(rows, classes, k) floats, as above.
+ * row); temperature >= 2^-126 and finite.  ws: lpp_top_logits_ws(rows, classes, k) floats, as above.
  * rows == 0 is valid.
  */
 typedef struct {
@@ -602,7 +602,9 @@ int lpp_kernel_top_logits(const lpp_top_logits_args* args, void* stream);
  * has loss 0 and gradient 0, whatever it holds.  weight: float32 [rows], NULL for 1.  A class that
  * is listed twice counts with both entries.  Logits of -inf (masked classes) take no
  * part; a row with an infinity or NaN otherwise is NaN.
- * 1 <= k <= 128; classes >= 1; 0 <= alpha <= 1; temperature > 0; scale finite; threads of a
+ * 1 <= k <= 128; classes >= 1; 0 <= alpha <= 1; 2^-60 <= temperature <= 2^60 (p and q are
+ * float32: at high T, where they are alike, their last digits count T times in dz and in the loss, so
+ * that T should stay in the thousands); scale finite; threads of a
  * launch as above.  ws: lpp_distill_ws(rows, classes) floats, as above.  rows == 0 is valid.
  */
 typedef struct {

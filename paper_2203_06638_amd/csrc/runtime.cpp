@@ -2040,6 +2040,11 @@ int lpp_destroy(lpp_ctx* c) {
     return LPP_OK;
 }
 
+// Temperatures T for which T^2 and 1 / T leave float32 room for the loss and the logits that they are
+// multiplied by; and those with 1 / T.
+static bool distill_temperature(float T) { return T >= 0x1p-60f && T <= 0x1p60f; }
+static bool top_temperature(float T) { return T >= 0x1p-126f && std::isfinite(T); }
+
 // lpp_step, and with a teacher lpp_step_distill
 static int step(lpp_ctx* c, int worker, const lpp_batch* batch, const lpp_teacher* teacher, int partition, float lr) {
     int rc = check_worker(c, worker);
@@ -2123,8 +2128,7 @@ int lpp_step_distill(lpp_ctx* c, int worker, const lpp_batch* batch, const lpp_t
     if (t->k < 1) return fail(LPP_EINVAL, "k must be at least 1");
     if (t->k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
     if (!(t->alpha >= 0.f && t->alpha <= 1.f)) return fail(LPP_EINVAL, "alpha must be in [0, 1]");
-    if (!(t->temperature > 0.f) || !std::isfinite(t->temperature))
-        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (!distill_temperature(t->temperature)) return fail(LPP_EINVAL, "temperature must be in [2^-60, 2^60]");
     if (c && lpp::distill_threads(c->M.desc.batch, c->M.desc.n_classes) > lpp::kLaunchThreads)
         return fail(LPP_EUNSUPPORTED, "the batch has too many images for one launch");
     return step(c, worker, batch, t, partition, lr);
@@ -2139,8 +2143,7 @@ int lpp_top_logits(lpp_ctx* c, int worker, int k, float temperature, float* valu
         return fail(LPP_EINVAL, "values, index and rest must be buffers of floats and ints");
     if (k < 1 || k > M.desc.n_classes) return fail(LPP_EINVAL, "k must be in [1, n_classes]");
     if (k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
-    if (!(temperature > 0.f) || !std::isfinite(temperature))
-        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (!top_temperature(temperature)) return fail(LPP_EINVAL, "temperature must be in [2^-126, 2^128)");
     if (w.last_partition < 0) return fail(LPP_ESTATE, "the worker has made no step");
     if (lpp::top_logits_threads(M.desc.batch, M.desc.n_classes, k) > lpp::kLaunchThreads)
         return fail(LPP_EUNSUPPORTED, "the batch has too many images for one launch");
@@ -2870,8 +2873,7 @@ int lpp_kernel_top_logits(const lpp_top_logits_args* a, void* stream) {
     if (a->k > a->classes) return fail(LPP_EINVAL, "k is more than the classes");
     if (a->k > lpp::kDistillMaxK) return fail(LPP_EUNSUPPORTED, "k is at most 128");
     if (const char* e = bad_matrix(a->z, a->dtype, a->rows, a->classes, a->ldz)) return fail(LPP_EINVAL, e);
-    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature))
-        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (!top_temperature(a->temperature)) return fail(LPP_EINVAL, "temperature must be in [2^-126, 2^128)");
     if ((a->rows > 0 && (!a->values || !a->index)) ||
         ((uintptr_t)a->values | (uintptr_t)a->index | (uintptr_t)a->rest) % 4)
         return fail(LPP_EINVAL, "values, index and rest must be buffers of floats and ints");
@@ -2908,8 +2910,7 @@ int lpp_kernel_distill(const lpp_distill_args* a, void* stream) {
     if (const char* e = bad_matrix(a->z, a->dtype, a->rows, a->classes, a->ldz)) return fail(LPP_EINVAL, e);
     if (a->dz)
         if (const char* e = bad_matrix(a->dz, a->dtype, a->rows, a->classes, a->lddz)) return fail(LPP_EINVAL, e);
-    if (!(a->temperature > 0.f) || !std::isfinite(a->temperature))
-        return fail(LPP_EINVAL, "temperature must be positive and finite");
+    if (!distill_temperature(a->temperature)) return fail(LPP_EINVAL, "temperature must be in [2^-60, 2^60]");
     if (!(a->alpha >= 0.f && a->alpha <= 1.f)) return fail(LPP_EINVAL, "alpha must be in [0, 1]");
     if (!std::isfinite(a->scale)) return fail(LPP_EINVAL, "scale must be finite");
     if ((a->rows > 0 && (!a->values || !a->index || !a->loss)) ||

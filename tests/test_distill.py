@@ -147,3 +147,26 @@ def test_step_refusals():
         refused(f(**kw))
     refused(f(k=129), lpp.EUNSUPPORTED)
     refused(L.lpp_top_logits(None, 0, 3, 1.0, OKP, OKP, OKP))
+
+
+def test_temperatures():
+    """Distillation takes temperatures whose squares and reciprocals float32 holds with room for what they
+    are multiplied by, [2^-60, 2^60]; the top logits every one with a reciprocal in float32."""
+    L = lpp.lib()
+    z, k, t = 100, 5, 0
+
+    def top(T):
+        return L.lpp_kernel_top_logits(C.byref(lpp.TopLogitsArgs(OKP, z, 4, z, k, lpp.FP32, T, OKP, OKP, OKP, None, 0)), None)
+
+    def distill(T):
+        return L.lpp_kernel_distill(C.byref(lpp.DistillArgs(OKP, OKP, z, z, 4, z, k, lpp.FP32, OKP, OKP, OKP, OKP, OKP, OKP,
+                                                            0.5, T, 1.0, None, 0)), None)
+
+    def step(T):
+        return L.lpp_step_distill(None, 0, None, C.byref(lpp.Teacher(OKP, OKP, OKP, 4, 0.5, T)), 0, 0.1)
+    for T in (1e-45, 1e-39, 2.0 ** -127):
+        refused(top(T))
+    for T in (1e-45, 1e-38, 2.0 ** -60 * (1 - 2.0 ** -24), 2.0 ** 60 * (1 + 2.0 ** -23), 1e20, 3e38):
+        for f in (distill, step):
+            refused(f(T))
+            assert b"temperature" in L.lpp_last_error()

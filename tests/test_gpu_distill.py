@@ -468,3 +468,28 @@ def test_student_far_favourite_by_hand():
     want = 0.69 * math.log(0.69) + 0.31 * (math.log(0.31) - math.log(9) + 100)
     assert abs(loss.item() - want) < 40 * R.U * want
     assert abs(dz[0, 4].item() - 0.31) < 8 * R.U and (dz[0, :4] + 0.31 / 9).abs().max() < 8 * R.U / 9
+
+
+@pytest.mark.parametrize("T", [2.0 ** -60, 1e-6, 0.05, 2.0 ** 60])
+def test_distill_temperatures_of_the_range(T):
+    """Down to where a softmax is its largest class, and up to the border, where the answers stay finite.
+
+    The bounds of tests/distillref.py take the teacher's exponents to be off as their differences are, which
+    holds for T of about 1 and more.  values * (1 / T) has two roundings, 2 U |values| / T each way; p is
+    softmax of these (and rest, which is exact), so that it is off by at most twice that of itself:
+    dz by scale * alpha * T * 4 U max |values| / T * p, for the classes that are not listed their share of
+    the rest's."""
+    for n, (rows, C, k) in enumerate([(9, 10, 5), (4, 1000, 40), (2, 20000, 16), (2, 70000, 9)]):
+        say("distill", T, rows, C, k)
+        z, values, index, r, best = teacher(80 + n, rows, C, k, T, True)
+        p = torch.softmax(torch.cat([values.double() / T, r.double().unsqueeze(1)], 1), 1)
+        others = torch.softmax((z.double() / T).scatter(1, index.long(), -INF), 1) * p[:, k:]
+        target = others.scatter(1, index.long(), p[:, :k])
+        for alpha in (1.0, 0.6):
+            loss, dz = run_distill(z, values, index, r, best, alpha=alpha, temperature=T, scale=1 / rows)
+            assert torch.isfinite(loss).all() and torch.isfinite(dz).all()
+            if T < 1:
+                want, wdz, bl, bd = R.distill(z, values, index, r, best, None, alpha, T, 1 / rows)
+                near(loss, want, bl, "loss")
+                more = alpha / rows * 4 * R.U * values.abs().amax(1, keepdim=True) * target
+                near(dz, wdz, bd + more + R.U * (wdz.abs() + bd) + 1e-38, "dz")
