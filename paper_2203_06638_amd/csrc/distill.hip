@@ -290,21 +290,21 @@ distill_k(DistillArgs p) {
             const float v = pr[e] - tm, pe = pow2(v * kLog2e) / ts, u = (zc[e] - most) * iT - lq, d = v - lt - u;
             pr[e] = pe;
             sp += pe;
-            if (tail) {
-                // both sides' probabilities add up to 1: p log(p / q) - p + q in place of
-                // p log(p / q) keeps the sum exact where p is near q
-                if (pe > 0.f)
-                    soft += again[e] ? pe * d - pe : d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + pow2(u * kLog2e);
-                else if (pe != pe) soft = pe;
-                else if (!again[e]) soft += pow2(u * kLog2e);
-            } else if (pe != 0.f) {
-                soft += pe * d;
-            }
+            // both sides' probabilities add up to 1 (the student's with what it gives the classes
+            // that are not listed): p log(p / q) - p + q in place of p log(p / q) keeps the sum
+            // exact where p is near q
+            if (pe > 0.f)
+                soft += again[e] ? pe * d - pe : d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + pow2(u * kLog2e);
+            else if (pe != pe) soft = pe;
+            else if (!again[e]) soft += pow2(u * kLog2e);
         }
         row_sum2<LW>(soft, sp, slots, none);
         float others = farT / sT;     // what gT times exp((z - m) / T) of a class that is not listed has
-        if (tail) {
-            const float q = so * farT / sT, pe = some && rest > -INFINITY ? pow2((rest - tm) * kLog2e) / ts : 0.f;
+        const float q = so * farT / sT;
+        if (!tail) {
+            soft += q;
+        } else {
+            const float pe = some && rest > -INFINITY ? pow2((rest - tm) * kLog2e) / ts : 0.f;
             if (some) {
                 const float d = (rest - tm) - lt - (logf(so) + away * iT - lq);
                 if (pe > 0.f) soft += d > -1.f ? pe * (d + expm1f(-d)) : pe * d - pe + q;

@@ -493,3 +493,27 @@ def test_distill_temperatures_of_the_range(T):
                 near(loss, want, bl, "loss")
                 more = alpha / rows * 4 * R.U * values.abs().amax(1, keepdim=True) * target
                 near(dz, wdz, bd + more + R.U * (wdz.abs() + bd) + 1e-38, "dz")
+
+
+@pytest.mark.parametrize("T", [10.0, 20.0, 100.0, 1000.0])
+@pytest.mark.parametrize("rest", [False, True])
+def test_distill_high_temperatures(T, rest):
+    """T^2 times a loss of about (spread / T)^2 / 2, which keeps its digits: also with a list of all
+    classes and no rest."""
+    for n, (rows, C, k) in enumerate([(9, 10, 10), (9, 10, 5), (5, 100, 100), (4, 1000, 40), (2, 20000, 128), (2, 70000, 9)]):
+        say("distill", T, rest, rows, C, k)
+        z, values, index, r, best = teacher(60 + n, rows, C, k, T, rest)
+        for alpha in (1.0, 0.6):
+            check_distill(z, values, index, r, best, None, alpha, T, 1 / rows)
+        if k == C:
+            # a term p (d + e^-d - 1), d = log(p / q), moves by p - q of what d is off (and its square).
+            # That is: quotients of numbers under 16 (two roundings each) and their differences (under 24), 200 / T
+            # in all; the two logs (of at most C and at least 1) and what they are added to, 8 log C; the
+            # sums in them, 16 additions or exponentials each, and expm1's last digits: 40.  p itself is off by
+            # about as much of the term.
+            loss, _ = run_distill(z, values, index, r, temperature=T)
+            want = R.distill(z, values, index, r, None, None, 1.0, T)[0]
+            e = (200 / T + 8 * math.log(C) + 40) * R.U
+            p = torch.softmax(values.double() / T, 1)
+            q = torch.softmax(z.double() / T, 1).gather(1, index.long())
+            near(loss, want, T * T * (2 * e * (p - q).abs().sum(1) + e * e) + 2 * e * want, "loss")
