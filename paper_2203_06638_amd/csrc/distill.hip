@@ -807,35 +807,41 @@ int distill_exps(const DistillArgs& p) {
     return p.temp == 2.f ? SQUARE : p.temp == 4.f ? FOURTH : TWO_EXPS;
 }
 
+// (hipErrorInvalidValue: a shape that row_plan does not make, and that has no kernel)
 template <typename T, int TPR, int NC, int MODE>
-void row_launch(const TopArgs& p, long wgs, hipStream_t st) {
+hipError_t row_launch(const TopArgs& p, long wgs, hipStream_t st) {
     const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
     constexpr int values = NC * 16 / (int)sizeof(T);
     if constexpr (TPR <= 64) launch((top_logits_k<T, TPR, NC, MODE, TPR>), grid, block, 0, st, p);
     else if constexpr (MODE != WHOLE || planned(TPR, values, kTopWide)) {
-        // (TPR 256, NC 1: k > 32, fewer would be a wave's)
-        if constexpr (TPR != 256 || NC > 1)
-            if (p.k <= 32) return launch((top_logits_k<T, TPR, NC, MODE, 64>), grid, block, 0, st, p);
-        launch((top_logits_k<T, TPR, NC, MODE, 256>), grid, block, 0, st, p);
-    }
+        if (p.k > 32) launch((top_logits_k<T, TPR, NC, MODE, 256>), grid, block, 0, st, p);
+        else if constexpr (TPR != 256 || NC > 1) launch((top_logits_k<T, TPR, NC, MODE, 64>), grid, block, 0, st, p);
+        else return hipErrorInvalidValue;   // (a wave's)
+    } else return hipErrorInvalidValue;
+    return hipGetLastError();
 }
 template <typename T, int TPR, int NC, int MODE>
-void row_launch(const DistillArgs& p, long wgs, hipStream_t st) {
-    const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
-    constexpr int V = 16 / (int)sizeof(T), RB = TPR > 256 ? 1 : 256 / TPR;
-    const unsigned lds = sizeof(float) * RB * distill_lds(p.lds_k, TPR * NC * V);
-    const bool stream = MODE != PIECE_SUMS && p.dz && p.rows * p.C * (long)sizeof(T) >= kStreamBytes;
-    const int exps = distill_exps(p);
-    auto go = [&](auto exps) {
-        constexpr int E = decltype(exps)::value;
-        if (stream) launch((distill_k<T, TPR, NC, MODE, E, MODE != PIECE_SUMS>), grid, block, lds, st, p);
-        else launch((distill_k<T, TPR, NC, MODE, E, false>), grid, block, lds, st, p);
-    };
-    if (exps == TWO_EXPS) {
-        if constexpr (MODE != WHOLE || planned(TPR, NC * V, kTwoWide)) go(std::integral_constant<int, TWO_EXPS>());
-    } else if (exps == SQUARE) go(std::integral_constant<int, SQUARE>());
-    else if (exps == FOURTH) go(std::integral_constant<int, FOURTH>());
-    else go(std::integral_constant<int, ONE_EXP>());
+hipError_t row_launch(const DistillArgs& p, long wgs, hipStream_t st) {
+    if constexpr (TPR == 256 && NC == 1) return hipErrorInvalidValue;   // (a wave's)
+    else {
+        const dim3 grid((unsigned)wgs), block(TPR > 256 ? TPR : 256);
+        constexpr int V = 16 / (int)sizeof(T), RB = TPR > 256 ? 1 : 256 / TPR;
+        const unsigned lds = sizeof(float) * RB * distill_lds(p.lds_k, TPR * NC * V);
+        const bool stream = MODE != PIECE_SUMS && p.dz && p.rows * p.C * (long)sizeof(T) >= kStreamBytes;
+        const int exps = distill_exps(p);
+        auto go = [&](auto exps) {
+            constexpr int E = decltype(exps)::value;
+            if (stream) launch((distill_k<T, TPR, NC, MODE, E, MODE != PIECE_SUMS>), grid, block, lds, st, p);
+            else launch((distill_k<T, TPR, NC, MODE, E, false>), grid, block, lds, st, p);
+        };
+        if (exps == TWO_EXPS) {
+            if constexpr (MODE != WHOLE || planned(TPR, NC * V, kTwoWide)) go(std::integral_constant<int, TWO_EXPS>());
+            else return hipErrorInvalidValue;
+        } else if (exps == SQUARE) go(std::integral_constant<int, SQUARE>());
+        else if (exps == FOURTH) go(std::integral_constant<int, FOURTH>());
+        else go(std::integral_constant<int, ONE_EXP>());
+        return hipGetLastError();
+    }
 }
 
 template <typename T, typename P>
@@ -843,55 +849,50 @@ hipError_t whole_rows(const P& p, RowPlan s, hipStream_t st) {
     const int rb = s.tpr < 256 ? 256 / s.tpr : 1;
     const long wgs = (p.rows + rb - 1) / rb;
     switch (s.tpr * 32 + s.nc) {
-    case 16 * 32 + 1: row_launch<T, 16, 1, WHOLE>(p, wgs, st); break;
+    case 16 * 32 + 1: return row_launch<T, 16, 1, WHOLE>(p, wgs, st);
     case 16 * 32 + 2:
-        if constexpr (sizeof(T) == 4) row_launch<T, 16, 2, WHOLE>(p, wgs, st);
+        if constexpr (sizeof(T) == 4) return row_launch<T, 16, 2, WHOLE>(p, wgs, st);
         else return hipErrorInvalidValue;   // (128 bf16 classes are 16 chunks)
-        break;
-    case 64 * 32 + 1: row_launch<T, 64, 1, WHOLE>(p, wgs, st); break;
-    case 64 * 32 + 2: row_launch<T, 64, 2, WHOLE>(p, wgs, st); break;
-    case 64 * 32 + 4: row_launch<T, 64, 4, WHOLE>(p, wgs, st); break;
-    case 256 * 32 + 1: row_launch<T, 256, 1, WHOLE>(p, wgs, st); break;
-    case 256 * 32 + 2: row_launch<T, 256, 2, WHOLE>(p, wgs, st); break;
-    case 256 * 32 + 4: row_launch<T, 256, 4, WHOLE>(p, wgs, st); break;
-    case 256 * 32 + 6: row_launch<T, 256, 6, WHOLE>(p, wgs, st); break;
-    case 256 * 32 + 8: row_launch<T, 256, 8, WHOLE>(p, wgs, st); break;
-    case 256 * 32 + 10: row_launch<T, 256, 10, WHOLE>(p, wgs, st); break;
+    case 64 * 32 + 1: return row_launch<T, 64, 1, WHOLE>(p, wgs, st);
+    case 64 * 32 + 2: return row_launch<T, 64, 2, WHOLE>(p, wgs, st);
+    case 64 * 32 + 4: return row_launch<T, 64, 4, WHOLE>(p, wgs, st);
+    case 256 * 32 + 1: return row_launch<T, 256, 1, WHOLE>(p, wgs, st);
+    case 256 * 32 + 2: return row_launch<T, 256, 2, WHOLE>(p, wgs, st);
+    case 256 * 32 + 4: return row_launch<T, 256, 4, WHOLE>(p, wgs, st);
+    case 256 * 32 + 6: return row_launch<T, 256, 6, WHOLE>(p, wgs, st);
+    case 256 * 32 + 8: return row_launch<T, 256, 8, WHOLE>(p, wgs, st);
+    case 256 * 32 + 10: return row_launch<T, 256, 10, WHOLE>(p, wgs, st);
     case 256 * 32 + 12:
-        if constexpr (sizeof(T) == 4) row_launch<T, 256, 12, WHOLE>(p, wgs, st);
+        if constexpr (sizeof(T) == 4) return row_launch<T, 256, 12, WHOLE>(p, wgs, st);
         else return hipErrorInvalidValue;   // (row_plan: 80 values a thread)
-        break;
     case 256 * 32 + 16:
-        if constexpr (sizeof(T) == 4) row_launch<T, 256, 16, WHOLE>(p, wgs, st);
+        if constexpr (sizeof(T) == 4) return row_launch<T, 256, 16, WHOLE>(p, wgs, st);
         else return hipErrorInvalidValue;
-        break;
-    case 512 * 32 + 4: row_launch<T, 512, 4, WHOLE>(p, wgs, st); break;
-    case 512 * 32 + 5: row_launch<T, 512, 5, WHOLE>(p, wgs, st); break;
-    case 512 * 32 + 6: row_launch<T, 512, 6, WHOLE>(p, wgs, st); break;
-    case 512 * 32 + 8: row_launch<T, 512, 8, WHOLE>(p, wgs, st); break;
+    case 512 * 32 + 4: return row_launch<T, 512, 4, WHOLE>(p, wgs, st);
+    case 512 * 32 + 5: return row_launch<T, 512, 5, WHOLE>(p, wgs, st);
+    case 512 * 32 + 6: return row_launch<T, 512, 6, WHOLE>(p, wgs, st);
+    case 512 * 32 + 8: return row_launch<T, 512, 8, WHOLE>(p, wgs, st);
     case 512 * 32 + 12:
-        if constexpr (sizeof(T) == 4) row_launch<T, 512, 12, WHOLE>(p, wgs, st);
+        if constexpr (sizeof(T) == 4) return row_launch<T, 512, 12, WHOLE>(p, wgs, st);
         else return hipErrorInvalidValue;   // (64 values a thread)
-        break;
     case 512 * 32 + 16:
-        if constexpr (sizeof(T) == 4) row_launch<T, 512, 16, WHOLE>(p, wgs, st);
+        if constexpr (sizeof(T) == 4) return row_launch<T, 512, 16, WHOLE>(p, wgs, st);
         else return hipErrorInvalidValue;
-        break;
     default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 template <typename T, int MODE, typename P>
-void piece_rows(const P& p, int nc, long wgs, hipStream_t st) {
-    if (nc == 2) row_launch<T, 256, 2, MODE>(p, wgs, st);
-    else if (nc == 4) row_launch<T, 256, 4, MODE>(p, wgs, st);
-    else row_launch<T, 256, 8, MODE>(p, wgs, st);
+hipError_t piece_rows(const P& p, int nc, long wgs, hipStream_t st) {
+    return nc == 2   ? row_launch<T, 256, 2, MODE>(p, wgs, st)
+           : nc == 4 ? row_launch<T, 256, 4, MODE>(p, wgs, st)
+                     : row_launch<T, 256, 8, MODE>(p, wgs, st);
 }
 
 template <typename T>
 hipError_t top_rows(TopArgs p, RowPlan s, hipStream_t st) {
     if (s.pieces == 1) return whole_rows<T>(p, s, st);
-    piece_rows<T, PIECE_SUMS>(p, s.nc, p.rows * p.pieces, st);
+    hipError_t e = piece_rows<T, PIECE_SUMS>(p, s.nc, p.rows * p.pieces, st);
+    if (e != hipSuccess) return e;
     launch(top_merge_k, dim3((unsigned)p.rows), dim3(kMergeThreads), 0, st, p);
     return hipGetLastError();
 }
@@ -900,10 +901,10 @@ template <typename T>
 hipError_t distill_rows(DistillArgs p, RowPlan s, hipStream_t st) {
     if (s.pieces == 1) return whole_rows<T>(p, s, st);
     p.grid_pieces = s.pieces;
-    piece_rows<T, PIECE_SUMS>(p, s.nc, p.rows * s.pieces, st);
+    hipError_t e = piece_rows<T, PIECE_SUMS>(p, s.nc, p.rows * s.pieces, st);
+    if (e != hipSuccess) return e;
     p.grid_pieces = p.dz ? s.pieces : 1;
-    piece_rows<T, PIECE_GRAD>(p, s.nc, p.rows * p.grid_pieces, st);
-    return hipGetLastError();
+    return piece_rows<T, PIECE_GRAD>(p, s.nc, p.rows * p.grid_pieces, st);
 }
 
 }  // namespace

@@ -422,15 +422,18 @@ hipError_t whole_dispatch(const GnBwdArgs& p, const GnWhole& s, hipStream_t st) 
     case 256 * 32 + 4: whole_launch<T, 256, 4, S>(p, s, st); break;
     case 256 * 32 + 8:
         if constexpr (kBwdChunks<T, S> >= 8) whole_launch<T, 256, 8, S>(p, s, st);
+        else return hipErrorInvalidValue;   // (groupnorm_whole leaves these to the other kernels)
         break;
     case 512 * 32 + 4: whole_launch<T, 512, 4, S>(p, s, st); break;
     case 512 * 32 + 8:
         if constexpr (kBwdChunks<T, S> >= 8) whole_launch<T, 512, 8, S>(p, s, st);
+        else return hipErrorInvalidValue;   // (groupnorm_whole leaves these to the other kernels)
         break;
     case 1024 * 32 + 2: whole_launch<T, 1024, 2, S>(p, s, st); break;
     case 1024 * 32 + 4: whole_launch<T, 1024, 4, S>(p, s, st); break;
     case 1024 * 32 + 8:
         if constexpr (kBwdChunks<T, S> >= 8) whole_launch<T, 1024, 8, S>(p, s, st);
+        else return hipErrorInvalidValue;   // (groupnorm_whole leaves these to the other kernels)
         break;
     default: return hipErrorInvalidValue;
     }

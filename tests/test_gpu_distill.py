@@ -517,3 +517,33 @@ def test_distill_high_temperatures(T, rest):
             p = torch.softmax(values.double() / T, 1)
             q = torch.softmax(z.double() / T, 1).gather(1, index.long())
             near(loss, want, T * T * (2 * e * (p - q).abs().sum(1) + e * e) + 2 * e * want, "loss")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_every_length_is_launched(dtype):
+    """Lengths on both sides of each number of a thread's chunks, in one row and in many: all outputs are
+    written, whatever the temperature makes of the exponentials."""
+    V = 4 if dtype == "fp32" else 8
+    lanes = [16 * n for n in (1, 2)] + [64 * n for n in (1, 2, 4)] + [256 * n for n in (1, 2, 4, 6, 8, 10, 12, 16)] \
+        + [512 * n for n in (4, 5, 6, 8, 12, 16)] + [40000]
+    sizes = sorted({C for n in lanes for C in (n * V, n * V + 1) if C <= 41000})
+    most = torch.randn(2048 * 41000, generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(DT[dtype])
+    for C in sizes:
+        for rows in (1, 2048):
+            z = most[:rows * C].view(rows, C)
+            for k in (5, 33):
+                k = min(k, C)
+                v, i = torch.full((rows, k), math.nan, device="cuda"), torch.full((rows, k), -1, dtype=torch.int32, device="cuda")
+                r = torch.full((rows,), math.nan, device="cuda")
+                n = lpp.top_logits_ws(rows, C, k)
+                lpp.kernel_top_logits(z, v, i, r, 1.0, torch.empty(n, device="cuda") if n else None)
+                assert not v.isnan().any() and (i >= 0).all() and (i < C).all() and not r.isnan().any(), (C, rows, k)
+            labels = torch.zeros(rows, dtype=torch.int32, device="cuda")
+            n = lpp.distill_ws(rows, C)
+            ws = torch.empty(n, device="cuda") if n else None
+            dz = torch.empty_like(z)
+            for T in (1.0, 2.0, 3.0, 4.0):
+                loss = torch.full((rows,), math.nan, device="cuda")
+                dz.fill_(math.nan)
+                lpp.kernel_distill(z, v, i, loss, dz, r, labels, alpha=0.5, temperature=T, ws=ws)
+                assert torch.isfinite(loss).all() and torch.isfinite(dz).all(), (C, rows, T)
