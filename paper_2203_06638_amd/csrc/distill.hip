@@ -424,12 +424,11 @@ struct TopSpace {
     }
 };
 // The k largest of the m candidates, each placed by counting the larger ones: emit(i, key)
-// takes the i-th.  Returns the k-th, 0 where there are fewer; next: the (k + 1)-th or 0.
+// takes the i-th.  Returns the k-th, 0 where there are fewer.
 template <int TPR, class Emit>
-__device__ __forceinline__ u64 rank_candidates(int k, int t, int m, TopSpace<TPR>& s, u64& next, Emit emit) {
+__device__ __forceinline__ u64 rank_candidates(int k, int t, int m, TopSpace<TPR>& s, Emit emit) {
     if (t == 0) s.border = 0;
     row_sync<TPR>();
-    u64 mine = 0;
     for (int i = t; i < m; i += TPR) {
         const u64 key = s.cand[i];
         int larger = 0;
@@ -437,16 +436,9 @@ __device__ __forceinline__ u64 rank_candidates(int k, int t, int m, TopSpace<TPR
         for (int o = 0; o < m; ++o) larger += s.cand[o] > key;
         if (larger < k) emit(larger, key);
         if (larger == k - 1) s.border = key;
-        if (larger == k) mine = key;
     }
     row_sync<TPR>();
-    const u64 border = s.border;
-    row_sync<TPR>();
-    if (mine) s.border = mine;
-    else if (t == 0 && m <= k) s.border = 0;
-    row_sync<TPR>();
-    next = s.border;
-    return border;
+    return s.border;
 }
 
 // The same of the keys that TPR threads hold, whatever they are; each(f) calls f(key) for
@@ -454,7 +446,7 @@ __device__ __forceinline__ u64 rank_candidates(int k, int t, int m, TopSpace<TPR
 // k keys reach, k exactly where all values are equal.  Keys laid out against the threads can
 // leave too many; then the k largest are taken one by one.
 template <int TPR, class Each, class Emit>
-__device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slots, u64& next, Each each, Emit emit) {
+__device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slots, Each each, Emit emit) {
     constexpr int H = TPR < 256 ? TPR : 256;     // threads whose maxima are compared
     u64 best = 0;
     each([&](u64 key) { best = key > best ? key : best; });
@@ -482,14 +474,10 @@ __device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slo
         });
     row_sync<TPR>();
     const int m = s.count;
-    if (m <= kCandidates<TPR>) return rank_candidates<TPR>(k, t, m, s, next, emit);
+    if (m <= kCandidates<TPR>) return rank_candidates<TPR>(k, t, m, s, emit);
     u64 last = 0;
-    for (int i = 0; i <= k; ++i) {
+    for (int i = 0; i < k; ++i) {
         const u64 top = row_max64<TPR>(best, slots);
-        if (i == k) {
-            next = top;
-            break;
-        }
         if (best == top) {
             if (top) emit(i, top);
             best = 0;
@@ -677,9 +665,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves<T>(NC * 16 / (int)
     };
     if (MODE == PIECE_SUMS)
         for (int i = c1 - c0 + t; i < p.k; i += TPR) keys[i] = 0;
-    u64 next;
-    const u64 border = n <= kCandidates<TPR> ? rank_candidates<TPR>(p.k, t, n, space, next, emit)
-                                             : top_keys<TPR>(p.k, t, space, slots, next, each, emit);
+    const u64 border = n <= kCandidates<TPR> ? rank_candidates<TPR>(p.k, t, n, space, emit)
+                                             : top_keys<TPR>(p.k, t, space, slots, each, emit);
     if (!p.rest) return;
     float m = -INFINITY;
     s = 0.f;
@@ -741,10 +728,9 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
         p.values[r * p.k + i] = key_value(key);
         p.index[r * p.k + i] = (int)~(uint32_t)key;
     };
-    u64 next;
     const int m0 = space.count;
-    const u64 border = m0 <= kCandidates<TPR> ? rank_candidates<TPR>(p.k, t, m0, space, next, emit)
-                                              : top_keys<TPR>(p.k, t, space, slots, next, each, emit);
+    const u64 border = m0 <= kCandidates<TPR> ? rank_candidates<TPR>(p.k, t, m0, space, emit)
+                                              : top_keys<TPR>(p.k, t, space, slots, each, emit);
     if (!p.rest) return;
     const float eT = kLog2e / p.temp;
     float m = mine[0], s = 0.f;
