@@ -215,7 +215,9 @@ int lpp_step_distill(lpp_ctx* ctx, int worker, const lpp_batch* batch, const lpp
 /*
  * The k largest logits, their classes and the rest (NULL: not wanted) of every image of the
  * worker's last step, as lpp_kernel_top_logits, into device buffers: a teacher's answers to
- * that batch.  (A step with lr = 0 leaves a teacher's parameters as they are.)  Enqueued on
+ * that batch.  (A step with lr = 0 leaves a teacher's parameters as they are; it is a whole
+ * step all the same, with a backward pass, and moves the replica's counter and the worker's
+ * momentum.)  Enqueued on
  * the worker's stream; sequential mode waits for it, in async mode a student's step on
  * another stream needs lpp_sync or an event in between.  LPP_ESTATE before the worker's first
  * step.

@@ -459,3 +459,10 @@ def test_values_past_float32_sums(pixels):
         assert (rstd[:, 0] == 0).all() and (rstd[:, 1] > 0).all()
         assert torch.equal(y.cpu()[:, :4], beta[:4].expand(n * pixels, 4))
         assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(20000, 16, 32, 8), (30001, 5, 24, 3), (9000, 1, 64, 16)], ids=lambda s: "x".join(map(str, s)))
+def test_many_images(shape, dtype):
+    """dgamma and dbeta of tens of thousands of images, and every image's own statistics."""
+    test_large(shape, dtype)
