@@ -80,8 +80,9 @@ constexpr int kListPitch = kDistillMaxK + 4;   // floats of a row's list in the 
 
 // Waves a SIMD that the registers are kept to: the latencies of a row's steps, one after the
 // other, are covered by other rows.  A workgroup of 512 threads takes two of them.  (64 float32
-// values a thread, 2048 x 16000, T = 2: 61.2 us with three waves, 74.7 with four, which spill; as bf16,
-// 4096 rows: 78.0 and 76.3; two exponentials of 40 float32 values, 4096 x 10000, T = 3: 84.9 and 98.4.)
+// values a thread, 2048 x 16000, T = 2: 62.8 us with three waves, 72.5 with four, which spill; 64 as bf16,
+// 4096 x 16000: 80.5 and 76.6; two exponentials of 40 float32 values, 4096 x 10000, T = 3: 85.4 and 98.3.
+// These and row_plan's figures: inputs that change from call to call.)
 template <typename T>
 constexpr int distill_waves(int values, bool both, int tpr) {
     if (both) return values <= 16 ? 5 : values < 40 || (values == 40 && tpr > 256) ? 4 : tpr > 256 || values > 48 ? 2 : 3;
@@ -96,11 +97,11 @@ constexpr int distill_waves(int values, bool both, int tpr) {
 // works on: its teacher's side while the row is on its way, its student's side between
 // the sums and the gradient.  The exponentials stay in registers from the sums to the
 // gradient.
-// 4096 x 20000 bf16, 32 listed (328 MB, 64 us at a large copy's rate): 87 us with T = 1, 88.7 with
-// T = 2, 89.9 with T = 4, 113 with T = 3, where both exponentials of a value are kept (eight waves to a
+// 4096 x 20000 bf16, 32 listed (328 MB, 64 us at a large copy's rate): 88.5 us with T = 1, 91.4 with
+// T = 2 and T = 4, 118.6 with T = 3, where both exponentials of a value are kept (eight waves to a
 // row).  A compute unit holds three rows, each of which loads, sums and writes in turn: half of the
 // time its vector units wait.
-// 1024 x 1000 float32 7.8 us, 128 x 10 6.2: the latency of a row's steps, not its bytes (1.6, 0.002).
+// 1024 x 1000 float32 8.1 us, 128 x 10 6.2: the latency of a row's steps, not its bytes (1.6, 0.002).
 template <typename T, int TPR, int NC, int MODE, int EXPS, bool ST>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256, distill_waves<T>(NC * 16 / (int)sizeof(T), EXPS == TWO_EXPS, TPR)) void
 distill_k(DistillArgs p) {
@@ -495,7 +496,7 @@ __device__ __forceinline__ u64 top_keys(int k, int t, TopSpace<TPR>& s, u64* slo
 __device__ __forceinline__ float rest_base(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
 
 // Waves a SIMD that the registers are kept to (2048 x 16000 float32, 32 values a thread, five waves
-// are two workgroups of 512 threads, six are three: 38.5 and 31.6 us).
+// are two workgroups of 512 threads, six are three: 38.5 and 31.8 us).
 template <typename T>
 constexpr int top_waves(int values) { return values <= (sizeof(T) == 2 ? 40 : 32) ? 6 : values <= 40 ? 5 : 4; }
 
@@ -512,10 +513,10 @@ constexpr int kFew = 256;
 // the bound (equal values, or values laid out against the threads) top_keys takes over, and
 // where the values under it add up to less than 1, so that the bound may lie far above them,
 // they are summed again relative to their largest.
-// 4096 x 20000 bf16, k = 32 (164 MB, 32 us at a large copy's rate): 51.5 us, of which the vector
-// instructions (about 17 a value, an exponential among them) are issued for 40; k = 128: 95.7, whose
-// candidates the first wave places.  128 x 1000 float32 6.6 us, and 8 x 131072 in pieces 13.2 + 7.5 for the
-// merge: latency of 4 to 8 dependent steps.
+// 4096 x 20000 bf16, k = 32 (164 MB, 32 us at a large copy's rate): 50.9 us, of which the vector
+// instructions (about 17 a value, an exponential among them) are issued for 89%; k = 128: 95.0, whose
+// candidates, about 177, the first wave alone places, in passes over all of them.  128 x 1000 float32 6.3
+// us, and 8 x 131072 in pieces 12.2 + 6.6 for the merge: latency of 4 to 8 dependent steps.
 template <typename T, int TPR, int NC, int MODE, int G>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves<T>(NC * 16 / (int)sizeof(T))) void top_logits_k(TopArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -679,7 +680,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256, top_waves<T>(NC * 16 / (int)
 
 // A row's answer from its pieces' lists, which are in descending order.  With j = 2 k / P
 // (P pieces) at least k keys reach the ceil(k / j)-th largest of the pieces' j-th keys.  (8 rows of
-// 32 pieces, k = 64: 7.5 us, barriers.)
+// 32 pieces, k = 64: 6.6 us, barriers.)
 constexpr int kMergeThreads = 1024, kMergeKeys = 4;
 __global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
     constexpr int TPR = kMergeThreads;
@@ -751,10 +752,10 @@ __global__ __launch_bounds__(kMergeThreads) void top_merge_k(TopArgs p) {
 
 // Threads of a row and chunks of a thread.  Rows that the registers of 512 threads do not
 // hold are cut into pieces.  Where there are many rows, four waves to a row and more values a
-// thread: more rows of a compute unit at once, whose steps cover each other (distillation of the same
-// 4096 x 20000 bf16 again and again, T = 2: 76.6 us, 82.5 with eight waves; 1024 x 16000 float32: 37.8 and 30.4).
-// wide: values that a thread may keep there.  Top logits: 48 (4096 x 10000 bf16 32.1 us, 37.5 with
-// eight; 16000: 42.3 and 40.7); distillation: 80, with two exponentials kept 48.
+// thread: more rows of a compute unit at once, whose steps cover each other (distillation of 4096 x 20000
+// bf16, T = 2: 93.3 us, 101.1 with eight waves; 1024 x 16000 float32: 35.9 and 34.3).
+// wide: values that a thread may keep there.  Top logits: 48 (4096 x 10000 bf16 32.0 us, 37.9 with
+// eight; 16000: 41.8 and 40.8); distillation: 80, with two exponentials kept 48.
 struct RowPlan {
     int tpr, nc;
     int pieces, piece;    // piece: classes
@@ -764,7 +765,8 @@ constexpr int kThreadValues = 64, kWideRows = 2048, kTopWide = 48, kDistillWide 
 constexpr bool planned(int tpr, int values, int wide) { return tpr != 256 || values <= wide; }
 RowPlan row_plan(int V, long rows, int C, int k, int wide) {
     const int chunks = (C + V - 1) / V;
-    // (up to 128 classes; 16384 x 100 float32, distillation: 20 us with a wave to a row, 8.6 with 16 lanes)
+    // (up to 128 classes; 16384 x 100 float32, distillation, one buffer again and again: 20 us with a wave
+    // to a row, 8.6 with 16 lanes)
     if (C <= 128 && k < 16) return {16, chunks <= 16 ? 1 : 2, 1, C};
     if (k <= 32)
         for (int nc : {1, 2, 4})

@@ -17,7 +17,7 @@
 // This file's kernels spread an image over the chip: partial sums, then a second pass over the
 // data, which takes part of it from the caches.  Maps that a workgroup's registers hold take
 // groupnorm_whole.hip, which reads them once.  Both do about 8 operations a value forward, 16
-// backward: bandwidth bounds them.
+// backward, so that the bytes set the floor; how near they come is said at each kernel.
 #include <algorithm>
 
 #include "act8.h"
@@ -305,8 +305,8 @@ struct Channels {
 };
 
 // Sums over a split's rows of dz and dz * u: for every channel, into ws behind the
-// parts' [image][split][2][cp], and gamma times them for every part.  (32 x 784 x 250 float32: 13.2 us,
-// 50 MB at 3.8 TB/s.)
+// parts' [image][split][2][cp], and gamma times them for every part.  (32 x 784 x 250 float32: 13.4 us,
+// 50 MB at 3.7 TB/s.)
 template <typename T, int ACT>
 __global__ __launch_bounds__(TB) void gn_bwd_sums_k(GnBwdArgs p) {
     constexpr int V = 16 / (int)sizeof(T);
@@ -424,8 +424,8 @@ __global__ __launch_bounds__(TB) void gn_columns_k(GnBwdArgs p) {
 }
 
 // dx; the first `extra` workgroups sum dgamma and dbeta beside it.  Four waves a SIMD in float32: the 784
-// workgroups of 32 x 784 x 250 with a residual then run at once (18.8 us, 100 MB at 5.3 TB/s; 21.9 with
-// three); bf16's registers would spill.  With gn_bwd_sums_k 32 x 3136 x 256 bf16 takes 57 us
+// workgroups of 32 x 784 x 250 with a residual then run at once (19.2 us, 100 MB at 5.2 TB/s; 21.9 with
+// three); bf16's registers would spill.  With gn_bwd_sums_k 32 x 3136 x 256 bf16 takes 61.9 us
 // (30 at a large copy's rate if x and dy were read once).
 template <typename T, int ACT, bool ST>
 __global__ __launch_bounds__(TB, sizeof(T) == 4 ? 4 : 3) void gn_bwd_apply_k(GnBwdArgs p) {

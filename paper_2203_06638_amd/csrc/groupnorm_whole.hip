@@ -167,10 +167,12 @@ constexpr int whole_lds(int TB, int slots, int lw, int N) { return N * (TB / 64 
 
 // The mean comes from the values' sum, then once more from that of the deviations, whose
 // squares give the variance: rounding of large means stays out of both.
-// x is read once and y written once, so bandwidth is the bound; what keeps it from that is that a
-// workgroup loads, sums and writes in turn, all of them in step where they run in one round:
-// 32 x 3136 x 256 bf16 24.2 us (4.2 TB/s; the two kernels of groupnorm.hip 40), 75 x 729 x 90 of 96 float32,
-// SiLU, 225 workgroups, 18.4 (2.1 TB/s), one 64 x 64 map 4.0 (latency of its barriers).
+// x is read once and y written once, so the bytes set the floor.  A workgroup loads, sums and writes in
+// turn, all of them in step where they run in one round, and is about 70% of that time issuing
+// vector instructions: conversions, masks, and in every thread the divisions and the root of its
+// slots' statistics.  32 x 3136 x 256 bf16 24.7 us (4.2 TB/s; with inputs that no cache holds 33.3), 75 x
+// 729 x 90 of 96 float32, SiLU, 225 workgroups, 8 chunks a thread of which 5.7 are used, 18.3 (2.1 TB/s),
+// one 64 x 64 map 4.4 (latency of its barriers).
 // 128 registers: four waves a SIMD, so that one workgroup of 1024 threads, or several small ones,
 // fill a compute unit.  Runs of 32 bytes of a row a workgroup instead of 64: 53 us.
 template <typename T, int TB, int NC, int S, bool ST>
@@ -267,8 +269,8 @@ __global__ __launch_bounds__(TB, 4) void gn_whole_k(GnArgs p, GnWhole s) {
 
 // The gradient: the channels' sums of dz and dz * u over the image go to ws [image][2][cp], or,
 // of a single image, to dbeta and dgamma themselves.  x and dy stay in registers, which halves the
-// maps that fit: 128 x 1024 x 128 bf16 in 32 groups 22.8 us (4.4 TB/s; the two kernels of groupnorm.hip
-// 40), 8 x 64 x 64 float32 5.2 (latency).
+// maps that fit: 128 x 1024 x 128 bf16 in 32 groups 22.4 us (4.5 TB/s, vector units 73% busy; the two
+// kernels of groupnorm.hip 40), 8 x 64 x 64 float32 5.0 (latency).
 template <typename T, int TB, int NC, int S, bool ST>
 __global__ __launch_bounds__(TB, 4) void gn_whole_bwd_k(GnBwdArgs p, GnWhole s) {
     constexpr int V = 16 / (int)sizeof(T), Q = V / S;
@@ -376,8 +378,10 @@ template <typename T, int TB, int NC, int S>
 void whole_launch(const GnArgs& p, const GnWhole& s, hipStream_t st) {
     const unsigned lds = sizeof(float) * (whole_lds(TB, S, s.lw, 1) + whole_lds(TB, S, s.lw, 2));
     const dim3 grid(8 * s.per_xcd);
-    // (13 chunks: all workgroups run at once and write at once; 32 x 3136 x 256 bf16 23.8 us, 27.6
-    // streamed; 8, in several rounds: 64 x 784 x 512 float32 34.5 us, 32.5 streamed)
+    // 8 chunks are streamed: 60 x 480 x 512 float32 32.6 us, 29.8 streamed, 128 x 500 x 512 60.3 and 59.4,
+    // as bf16 38.0 and 38.2.  13 are not: 128 x 3136 x 256 bf16 114 us, 123 streamed, one buffer of 32
+    // images again and again 23.8 and 27.6 (but with inputs that no cache holds 33.4 and 31.5, 64 x 784 x 512
+    // float32 48.8 and 47.0).
     if (NC == 8 && s.images * s.pixels * (long)s.G * s.cg * (long)sizeof(T) >= kStreamBytes)
         launch((gn_whole_k<T, TB, NC, S, NC == 8>), grid, dim3(TB), lds, st, p, s);
     else
